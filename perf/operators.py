@@ -82,7 +82,7 @@ def _log(rng, low, high, step=1):
 def draw(rng):
     kind = rng.choice(("fwd", "fwd", "fwd_q8", "fwd_q8", "bwd", "bwd", "norm", "norm_bwd", "clip", "adamw"))
     if kind in ("fwd", "fwd_q8", "bwd"):
-        m, n = _log(rng, 64, 4096, 8), _log(rng, 64, 4096, 8)
+        m, n = _log(rng, 64, 4096, 8), _log(rng, 64, 4096, 16 if kind == "fwd_q8" else 8)
         M = _log(rng, 1, 12608)
         if kind != "bwd" and rng.random() < 0.4:       # single tokens
             M = _log(rng, 1, 128)
