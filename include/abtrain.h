@@ -8,8 +8,9 @@
  * "drop singular values below sigmaCutoff * sigma_max").  This library is that hot path on
  * one GPU: the factored layer's forward and backward, and the merge of G factor copies; beside
  * them the decomposition of a dense weight (ab_factorize), the optimiser step of the group phase
- * (ab_adamw_step), W <- A B (ab_reconstruct) and the factored layer for convolution weights
- * (lr_conv_fwd, lr_conv_bwd).
+ * (ab_adamw_step), W <- A B (ab_reconstruct), the factored layer for convolution weights
+ * (lr_conv_fwd, lr_conv_bwd), and the operators around a frozen layer whose rows have low-rank adapters of their own (lr_adapters_*,
+ * lr_rms_norm_*, ab_grad_norm, ab_clip_grads, ab_adamw_step_clipped).
  *
  * Conventions shared by every entry point
  *   - All matrices are row-major and contiguous (leading dimension = number of columns).
@@ -17,7 +18,7 @@
  *     caller; the library never allocates, frees or retains caller memory.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  lr_linear_fwd,
  *     lr_linear_bwd, lr_linear_bwd_static, lr_linear_fwd_grouped, lr_linear_bwd_grouped, lr_conv_fwd, lr_conv_bwd,
- *     ab_adamw_step and ab_reconstruct enqueue work on it and return without synchronising the host.  Calls that DO
+ *     ab_adamw_step, ab_reconstruct, lr_adapters_*, lr_rms_norm_*, ab_grad_norm, ab_clip_grads and ab_adamw_step_clipped enqueue work on it and return without synchronising the host.  Calls that DO
  *     block the host:
  *       ab_merge, ab_merge_batched, ab_factorize, ab_factorize_batched: once after uploading
  *         their layer tables (tables of up to 7680 bytes, which one or two layers may have, travel in
@@ -372,6 +373,102 @@ int lr_conv_bwd(const void* dY, const void* act, const void* T, const void* A, c
                 void* workspace, size_t workspace_bytes, void* stream);
 
 size_t lr_conv_bwd_workspace_bytes(const abt_conv_geom* geom, int64_t m, int64_t r, int dtype);
+
+/* -------------------------------------------------------------------------------------
+ * A frozen dense layer with low-rank adapters: `count` pairs of factors (Eq. 3's A and B, as a group phase or ab_factorize leaves
+ * them) beside one weight W [m, n] that is not trained.  Every row belongs to an adapter of its own choice:
+ *     T_i = B_a x_i          Y_i = W x_i + scale_a A_a T_i          a = row_adapter[i]
+ * row_adapter [M]: int32; an id outside [0, count), -1 by custom, is no adapter: Y_i = W x_i, T_i = 0.  The ids may come in any
+ * order; rows that lie together by adapter are the fast case (a tile of the result makes one short pass per adapter among its
+ * rows).  All tables are read by the kernels, so a captured graph can be replayed with other ids, ranks and scales.
+ *
+ * abt_adapters: A [count, m, r], B [count, r, n], bf16, stacked; ranks [count] int32 (NULL: all r): adapter a has
+ * ranks[a] columns of A and rows of B, taken as 0 .. r; what lies past them is not looked at.  scales [count] fp32 (NULL: 1).  r is a
+ * multiple of 8, at most ABT_ADAPTERS_MAX_RANK; count at most 65535.  M >= 1; m and n are multiples of 8, at most 2^20.
+ *
+ * lr_adapters_fwd: X [M, n], W, Y [M, m] bf16.  T_save [M, r] fp32, optional: T before the scale, columns past a row's rank zero.
+ *   scale_a T_i is rounded to bf16 once for the second product.
+ * lr_adapters_fwd_q8: the dense product from 8-bit floats (e4m3, OCP): X_i ~ x_scale[i] Xq_i, W_j ~ w_scale[j] Wq_j, Xq [M, n], Wq [m, n],
+ *   x_scale [M], w_scale [m] fp32, as lr_rms_norm_fwd writes them; the adapters see X itself (bf16).  n a multiple of 16.
+ * lr_adapters_bwd: dT_i = scale_a A_a^T dY_i,  dX_i = W^T dY_i + B_a^T dT_i (bf16),  dA_a = sum of scale_a dY_i T_i^T [count, m, r],
+ *   dB_a = sum of dT_i x_i^T [count, r, n] (fp32; adapters without rows and columns or rows past the rank get zeros).  T: the forward's T_save, or NULL
+ *   to have it computed again from X.  dX, dA, dB: any may be NULL; W may then be NULL without dX, X without dB (and with T or without dA).
+ *   accumulate != 0 adds into dA and dB.  dT and scale T enter dA and dB in full fp32 precision; dT is rounded to bf16 once for dX.
+ *   Fixed summation order: two calls on the same inputs give bit-identical results.
+ * The outputs must not overlap the inputs or each other.  Nothing blocks the host; all calls can be captured.
+ * Errors: ABT_EINVAL, ABT_EDTYPE (dt other than ABT_BF16), ABT_ESHAPE, ABT_EALIGN, ABT_EWORKSPACE, ABT_EHIP.
+ * ------------------------------------------------------------------------------------- */
+#define ABT_ADAPTERS_MAX_RANK 128
+typedef struct {
+    const void* A;                /* [count, m, r] bf16 */
+    const void* B;                /* [count, r, n] bf16 */
+    const int32_t* ranks;         /* [count], may be NULL */
+    const float* scales;          /* [count], may be NULL */
+    int32_t count;
+    int32_t r;
+} abt_adapters;
+
+int lr_adapters_fwd(const void* X, const void* W, const abt_adapters* adapters, const int32_t* row_adapter,
+                    void* Y, float* T_save, int64_t M, int64_t m, int64_t n, int dt,
+                    void* workspace, size_t workspace_bytes, void* stream);
+int lr_adapters_fwd_q8(const void* X, const void* Xq, const float* x_scale, const void* Wq, const float* w_scale,
+                       const abt_adapters* adapters, const int32_t* row_adapter, void* Y,
+                       int64_t M, int64_t m, int64_t n, void* workspace, size_t workspace_bytes, void* stream);
+/* of either forward; 0 for shapes that are refused */
+size_t lr_adapters_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n, int64_t r, int64_t count);
+
+int lr_adapters_bwd(const void* dY, const void* X, const float* T, const void* W, const abt_adapters* adapters,
+                    const int32_t* row_adapter, void* dX, float* dA, float* dB,
+                    int64_t M, int64_t m, int64_t n, int dt, int accumulate,
+                    void* workspace, size_t workspace_bytes, void* stream);
+size_t lr_adapters_bwd_workspace_bytes(int64_t M, int64_t m, int64_t n, int64_t r, int64_t count);
+
+/* -------------------------------------------------------------------------------------
+ * Root-mean-square norm of the rows, with the addition of the residual in front of it:
+ *     H = X + residual,   s_i = 1 / sqrt(mean_j H_ij^2 + eps),   Y = H s gain
+ * X, residual, H, Y [M, n] of type dt; gain [n] fp32.  residual may be NULL (H = X); H may be NULL (not kept; it may be X or residual itself);
+ * Y may be NULL where Yq is given.  Y comes from the sum before H is rounded.
+ * Yq [M, n], y_scale [M], both or neither: Y_ij ~ y_scale_i Yq_ij in 8-bit floats (e4m3, OCP), y_scale_i = max_j |Y_ij| / 448 (of Y before its
+ * rounding).  A row whose largest value is below 1e-30 has scale 0 and values 0; infinities and NaN in a row make the products of
+ * that row NaN.
+ * lr_rms_norm_bwd: from dY and H (the forward's H, or X where there was no residual), and dH, the gradient that reaches H past the norm (NULL:
+ * none): dX = dH + s (dY gain - H s^2 mean_j(dY gain H)) of type dt, the gradient of X and of the residual, and dgain [n] = sum_i dY H s
+ * (fp32; accumulate != 0 adds).  Either may be NULL; the workspace is only needed for dgain.  dX may be dH, dY or H itself.  Fixed summation order.
+ * Statistics in fp32.  M >= 1, n a multiple of 8, at most ABT_RMS_NORM_MAX_WIDTH; eps >= 0 and finite.  Nothing blocks the host; can be captured.
+ * ------------------------------------------------------------------------------------- */
+#define ABT_RMS_NORM_MAX_WIDTH 16384
+int lr_rms_norm_fwd(const void* X, const void* residual, const float* gain, double eps, void* H, void* Y,
+                    void* Yq, float* y_scale, int64_t M, int64_t n, int dt, void* stream);
+int lr_rms_norm_bwd(const void* dY, const void* H, const float* gain, double eps, const void* dH, void* dX, float* dgain,
+                    int64_t M, int64_t n, int dt, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+size_t lr_rms_norm_bwd_workspace_bytes(int64_t M, int64_t n, int dt);
+
+/* -------------------------------------------------------------------------------------
+ * Clipping by the global norm N = sqrt(sum of g^2 over all tensors), between the backward and ab_adamw_step:
+ *     g' = c g,   c = max_norm / N where N > max_norm, else 1
+ * Squares are summed in fp64 in a fixed order.  Where N is not finite nothing is scaled or stepped: the caller sees it in norm_out.
+ * `tensors` is a HOST array read before the call returns; per tensor grad (DEVICE, fp32 or bf16 by dt), out (DEVICE, the same type, NULL: in
+ * place), count (0 .. 2^40).  All pointers 16-byte aligned; outputs must not overlap but with their own grad, whole.
+ * norm_out: one fp32 in device memory receiving N (before clipping); may be NULL but for ab_grad_norm.
+ * ab_adamw_step_clipped: ab_adamw_step on the clipped gradients, which are not written; every other argument as there.
+ * Workspace: ab_grad_norm_workspace_bytes(n).  Nothing blocks the host; ab_grad_norm and ab_clip_grads can be captured.
+ * Errors: ABT_EINVAL (max_norm negative or not finite, NULL where a pointer is needed), ABT_EDTYPE, ABT_ESHAPE, ABT_EALIGN, ABT_EWORKSPACE, ABT_EHIP.
+ * ------------------------------------------------------------------------------------- */
+typedef struct {
+    const void* grad;
+    void* out;                    /* ab_clip_grads; may be NULL */
+    int64_t count;
+    int32_t dt;
+    int32_t reserved;             /* 0 */
+} abt_grad_tensor;
+
+int ab_grad_norm(const abt_grad_tensor* tensors, int n, float* norm_out, void* workspace, size_t workspace_bytes, void* stream);
+int ab_clip_grads(const abt_grad_tensor* tensors, int n, double max_norm, float* norm_out, void* workspace, size_t workspace_bytes, void* stream);
+int ab_adamw_step_clipped(const abt_adamw_tensor* tensors, int n, int64_t step,
+                          double lr, double lr_scale, double beta1, double beta2, double eps,
+                          double weight_decay, double max_norm, float* norm_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+size_t ab_grad_norm_workspace_bytes(int n);
 
 /* Work-group height of the bf16 chain kernel (T = X B^T, Y = T A^T and the dT / dX half of the
  * backward): 0 = chosen from the batch size (default), 64 or 128 = forced where the rank allows it.

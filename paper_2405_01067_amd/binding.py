@@ -29,6 +29,9 @@ EXPORTS = (
     "ab_factorize_batched", "ab_factorize_batched_workspace_bytes",
     "ab_adamw_step", "ab_lr_rebound_scale", "ab_reconstruct",
     "lr_conv_fwd", "lr_conv_fwd_wants_T", "lr_conv_bwd", "lr_conv_bwd_workspace_bytes",
+    "lr_adapters_fwd", "lr_adapters_fwd_q8", "lr_adapters_fwd_workspace_bytes", "lr_adapters_bwd", "lr_adapters_bwd_workspace_bytes",
+    "lr_rms_norm_fwd", "lr_rms_norm_bwd", "lr_rms_norm_bwd_workspace_bytes",
+    "ab_grad_norm", "ab_clip_grads", "ab_adamw_step_clipped", "ab_grad_norm_workspace_bytes",
 )
 
 
@@ -61,7 +64,19 @@ class LrGroup(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in ("X", "A", "B", "Y", "T_save", "dY", "T", "dX", "dA", "dB")]
 
 
+class Adapters(ctypes.Structure):
+    """abt_adapters"""
+    _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("ranks", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("count", ctypes.c_int32), ("r", ctypes.c_int32)]
+
+
+class GradTensor(ctypes.Structure):
+    """abt_grad_tensor"""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dt", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 MAX_GROUPS = 8   # ABT_MAX_GROUPS
+ADAPTERS_MAX_RANK = 128   # ABT_ADAPTERS_MAX_RANK
 
 
 class MergeDesc(ctypes.Structure):
@@ -164,6 +179,31 @@ def load():
     lib.lr_conv_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, pg, i64, i64, ci, ci, vp, sz, vp]
     lib.lr_conv_bwd_workspace_bytes.restype = sz
     lib.lr_conv_bwd_workspace_bytes.argtypes = [pg, i64, i64, ci]
+    pa, pgt, pat = ctypes.POINTER(Adapters), ctypes.POINTER(GradTensor), ctypes.POINTER(AdamwTensor)
+    lib.lr_adapters_fwd.restype = ci
+    lib.lr_adapters_fwd.argtypes = [vp, vp, pa, vp, vp, vp, i64, i64, i64, ci, vp, sz, vp]
+    lib.lr_adapters_fwd_q8.restype = ci
+    lib.lr_adapters_fwd_q8.argtypes = [vp, vp, vp, vp, vp, pa, vp, vp, i64, i64, i64, vp, sz, vp]
+    lib.lr_adapters_fwd_workspace_bytes.restype = sz
+    lib.lr_adapters_fwd_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.lr_adapters_bwd.restype = ci
+    lib.lr_adapters_bwd.argtypes = [vp, vp, vp, vp, pa, vp, vp, vp, vp, i64, i64, i64, ci, ci, vp, sz, vp]
+    lib.lr_adapters_bwd_workspace_bytes.restype = sz
+    lib.lr_adapters_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.lr_rms_norm_fwd.restype = ci
+    lib.lr_rms_norm_fwd.argtypes = [vp, vp, vp, cd, vp, vp, vp, vp, i64, i64, ci, vp]
+    lib.lr_rms_norm_bwd.restype = ci
+    lib.lr_rms_norm_bwd.argtypes = [vp, vp, vp, cd, vp, vp, vp, i64, i64, ci, ci, vp, sz, vp]
+    lib.lr_rms_norm_bwd_workspace_bytes.restype = sz
+    lib.lr_rms_norm_bwd_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.ab_grad_norm.restype = ci
+    lib.ab_grad_norm.argtypes = [pgt, ci, vp, vp, sz, vp]
+    lib.ab_clip_grads.restype = ci
+    lib.ab_clip_grads.argtypes = [pgt, ci, cd, vp, vp, sz, vp]
+    lib.ab_adamw_step_clipped.restype = ci
+    lib.ab_adamw_step_clipped.argtypes = [pat, ci, i64, cd, cd, cd, cd, cd, cd, cd, vp, vp, sz, vp]
+    lib.ab_grad_norm_workspace_bytes.restype = sz
+    lib.ab_grad_norm_workspace_bytes.argtypes = [ci]
     _lib = lib
     return lib
 
@@ -716,6 +756,223 @@ def ab_adamw_step(tensors, step: int, lr: float, lr_scale: float = 1.0, beta1: f
     plan = tensors if isinstance(tensors, AdamwPlan) else AdamwPlan(tensors)
     _check(load().ab_adamw_step(plan.table, plan.n, int(step), float(lr), float(lr_scale), float(beta1),
                                 float(beta2), float(eps), float(weight_decay), _stream()), "ab_adamw_step")
+
+
+class GradPlan:
+    """The tensor table of ab_grad_norm and ab_clip_grads, marshalled once, as AdamwPlan is: fp32 or bf16 GPU tensors, and
+    optionally as many of the same sizes and types that receive the clipped gradients (otherwise they are clipped in place).
+    Holds references to the tensors and the workspace: calls that share a plan must be stream-ordered."""
+
+    def __init__(self, grads: Sequence, out: Optional[Sequence] = None):
+        torch = _torch()
+        if out is not None and len(out) != len(grads):
+            raise AbtError("out must have one tensor per gradient")
+        self.n = len(grads)
+        self.table = (GradTensor * max(self.n, 1))()
+        self.tensors = (list(grads), list(out) if out is not None else None)
+        for i, g in enumerate(grads):
+            e = self.table[i]
+            e.grad, e.count, e.dt = _ptr(_dev_tensor(g, "grad")), g.numel(), _dt(g)
+            if out is not None:
+                o = _dev_tensor(out[i], "out")
+                if o.dtype != g.dtype or o.numel() != g.numel():
+                    raise AbtError("out must have the size and type of its gradient")
+                e.out = _ptr(o)
+        self.device = grads[0].device if self.n else torch.device("cuda", torch.cuda.current_device())
+        self.workspace = _workspace(load().ab_grad_norm_workspace_bytes(self.n), self.device)
+
+
+def ab_grad_norm(grads):
+    """The global norm (a 0-d fp32 GPU tensor) of a GradPlan or a list of fp32 or bf16 GPU tensors."""
+    plan = grads if isinstance(grads, GradPlan) else GradPlan(grads)
+    N = _torch().empty((), dtype=_torch().float32, device=plan.device)
+    _check(load().ab_grad_norm(plan.table, plan.n, N.data_ptr(), plan.workspace.data_ptr(), plan.workspace.numel(), _stream()), "ab_grad_norm")
+    return N
+
+
+def ab_clip_grads(grads, max_norm: float):
+    """Scales the gradients of a GradPlan or a list so that their global norm is max_norm at most (in place, or into the plan's
+    `out`); one that is not finite scales nothing.  Returns the norm before (a 0-d fp32 GPU tensor)."""
+    plan = grads if isinstance(grads, GradPlan) else GradPlan(grads)
+    N = _torch().empty((), dtype=_torch().float32, device=plan.device)
+    _check(load().ab_clip_grads(plan.table, plan.n, float(max_norm), N.data_ptr(), plan.workspace.data_ptr(), plan.workspace.numel(), _stream()), "ab_clip_grads")
+    return N
+
+
+def ab_adamw_step_clipped(tensors, max_norm: float, step: int, lr: float, lr_scale: float = 1.0, beta1: float = 0.9,
+                          beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01):
+    """ab_adamw_step on gradients scaled to a global norm of max_norm at most (they are not written).  A norm that is not finite
+    leaves everything as it was.  Returns the norm before clipping (a 0-d fp32 GPU tensor)."""
+    torch = _torch()
+    lib = load()
+    plan = tensors if isinstance(tensors, AdamwPlan) else AdamwPlan(tensors)
+    dev = plan.tensors[0]["param"].device if plan.n else torch.device("cuda", torch.cuda.current_device())
+    N = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _workspace(lib.ab_grad_norm_workspace_bytes(plan.n), dev)
+    _check(lib.ab_adamw_step_clipped(plan.table, plan.n, int(step), float(lr), float(lr_scale), float(beta1), float(beta2), float(eps),
+                                     float(weight_decay), float(max_norm), N.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "ab_adamw_step_clipped")
+    return N
+
+
+def _adapters(A, B, row_adapter, ranks, scales, M, m, n):
+    """The checks that the C side cannot make, and its struct."""
+    torch = _torch()
+    if A.dim() != 3 or B.dim() != 3 or A.shape[1] != m or B.shape[2] != n or A.shape[0] != B.shape[0] or A.shape[2] != B.shape[1]:
+        raise AbtError("adapters must be A [count, m, r] and B [count, r, n]")
+    count, r = A.shape[0], A.shape[2]
+    for t, nm, dtype, shape in ((A, "A", torch.bfloat16, A.shape), (B, "B", torch.bfloat16, B.shape), (row_adapter, "row_adapter", torch.int32, (M,)),
+                                (ranks, "ranks", torch.int32, (count,)), (scales, "scales", torch.float32, (count,))):
+        if t is None and nm in ("ranks", "scales"):
+            continue
+        if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+            raise AbtError(f"{nm} must be a contiguous GPU tensor {tuple(shape)} of {dtype}")
+    return Adapters(A.data_ptr(), B.data_ptr(), _ptr(ranks), _ptr(scales), count, r)
+
+
+def _plain_matrix(t, name, shape, dtype):
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise AbtError(f"{name} must be a contiguous GPU tensor {tuple(shape)} of {dtype}")
+
+
+def lr_adapters_fwd(X, W, A, B, row_adapter, ranks=None, scales=None, save_T: bool = True, Y=None, T=None, workspace=None):
+    """Y_i = W x_i + scales[a] A[a] T_i with T_i = B[a] x_i and a = row_adapter[i] (-1: no adapter): a frozen W [m, n] and stacked
+    adapters A [count, m, r], B [count, r, n] (bf16, GPU), row_adapter [M] int32, ranks [count] int32, scales [count] fp32.
+    Returns (Y, T), T [M, r] fp32 for lr_adapters_bwd (None without save_T)."""
+    torch = _torch()
+    lib = load()
+    bf16 = torch.bfloat16
+    if X.dim() != 2 or W.dim() != 2:
+        raise AbtError("X must be [M, n], W [m, n]")
+    M, n = X.shape
+    m = W.shape[0]
+    _plain_matrix(X, "X", (M, n), bf16), _plain_matrix(W, "W", (m, n), bf16)
+    ad = _adapters(A, B, row_adapter, ranks, scales, M, m, n)
+    if Y is None:
+        Y = X.new_empty((M, m))
+    else:
+        _plain_matrix(Y, "Y", (M, m), bf16)
+    if not save_T:
+        T = None
+    elif T is None:
+        T = torch.empty((M, ad.r), dtype=torch.float32, device=X.device)
+    else:
+        _plain_matrix(T, "T", (M, ad.r), torch.float32)
+    ws = _workspace(lib.lr_adapters_fwd_workspace_bytes(M, m, n, ad.r, ad.count), X.device, workspace)
+    _check(lib.lr_adapters_fwd(X.data_ptr(), W.data_ptr(), ctypes.byref(ad), row_adapter.data_ptr(), Y.data_ptr(), _ptr(T), M, m, n, ABT_BF16,
+                               ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "lr_adapters_fwd")
+    return Y, T
+
+
+def lr_adapters_fwd_q8(X, Xq, x_scale, Wq, w_scale, A, B, row_adapter, ranks=None, scales=None, Y=None, workspace=None):
+    """lr_adapters_fwd with the dense product from 8-bit floats: Xq [M, n] and Wq [m, n] (torch.float8_e4m3fn) with fp32 scales per
+    row, x_scale [M] and w_scale [m], as lr_rms_norm_fwd writes them; the adapters see X (bf16).  Returns Y [M, m] bf16."""
+    torch = _torch()
+    lib = load()
+    if X.dim() != 2 or Wq.dim() != 2:
+        raise AbtError("X must be [M, n], Wq [m, n]")
+    M, n = X.shape
+    m = Wq.shape[0]
+    for t, nm, shape, dtype in ((X, "X", (M, n), torch.bfloat16), (Xq, "Xq", (M, n), torch.float8_e4m3fn), (Wq, "Wq", (m, n), torch.float8_e4m3fn),
+                                (x_scale, "x_scale", (M,), torch.float32), (w_scale, "w_scale", (m,), torch.float32)):
+        _plain_matrix(t, nm, shape, dtype)
+    ad = _adapters(A, B, row_adapter, ranks, scales, M, m, n)
+    if Y is None:
+        Y = X.new_empty((M, m))
+    else:
+        _plain_matrix(Y, "Y", (M, m), torch.bfloat16)
+    ws = _workspace(lib.lr_adapters_fwd_workspace_bytes(M, m, n, ad.r, ad.count), X.device, workspace)
+    _check(lib.lr_adapters_fwd_q8(X.data_ptr(), Xq.data_ptr(), x_scale.data_ptr(), Wq.data_ptr(), w_scale.data_ptr(), ctypes.byref(ad),
+                                  row_adapter.data_ptr(), Y.data_ptr(), M, m, n, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()),
+           "lr_adapters_fwd_q8")
+    return Y
+
+
+def lr_adapters_bwd(dY, X, T, W, A, B, row_adapter, ranks=None, scales=None, need_dX: bool = True, need_dA: bool = True,
+                    need_dB: bool = True, dX=None, dA=None, dB=None, accumulate: bool = False, workspace=None):
+    """Gradients of lr_adapters_fwd: dX [M, n] bf16, dA [count, m, r] and dB [count, r, n] fp32 (W is frozen).  T: what the forward
+    returned, or None (computed again).  Returns (dX, dA, dB); skipped ones are None."""
+    torch = _torch()
+    lib = load()
+    bf16, f32 = torch.bfloat16, torch.float32
+    if X.dim() != 2 or W.dim() != 2:
+        raise AbtError("X must be [M, n], W [m, n]")
+    M, n = X.shape
+    m = W.shape[0]
+    _plain_matrix(dY, "dY", (M, m), bf16), _plain_matrix(X, "X", (M, n), bf16), _plain_matrix(W, "W", (m, n), bf16)
+    ad = _adapters(A, B, row_adapter, ranks, scales, M, m, n)
+    if T is not None:
+        _plain_matrix(T, "T", (M, ad.r), f32)
+    out = []
+    for t, nm, need, shape, dtype in ((dX, "dX", need_dX, (M, n), bf16), (dA, "dA", need_dA, A.shape, f32), (dB, "dB", need_dB, B.shape, f32)):
+        if not need:
+            t = None
+        elif t is not None:
+            _plain_matrix(t, nm, shape, dtype)
+        elif accumulate and nm != "dX":
+            raise AbtError(f"accumulate needs existing {nm}")
+        else:
+            t = torch.empty(shape, dtype=dtype, device=X.device)
+        out.append(t)
+    dX, dA, dB = out
+    ws = _workspace(lib.lr_adapters_bwd_workspace_bytes(M, m, n, ad.r, ad.count), X.device, workspace)
+    _check(lib.lr_adapters_bwd(dY.data_ptr(), X.data_ptr(), _ptr(T), W.data_ptr(), ctypes.byref(ad), row_adapter.data_ptr(), _ptr(dX), _ptr(dA), _ptr(dB),
+                               M, m, n, ABT_BF16, int(bool(accumulate)), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "lr_adapters_bwd")
+    return dX, dA, dB
+
+
+def lr_rms_norm_fwd(X, gain, eps: float = 1e-6, residual=None, quantize: bool = False, need_Y: bool = True, Y=None, H=None):
+    """H = X + residual, Y = gain H / sqrt(mean of H^2 over the columns + eps) for X [M, n] (bf16 or fp32), gain [n] fp32.
+    Returns (Y, H, Yq, y_scale): H is X itself without a residual; with quantize, Y ~ y_scale[i] Yq in torch.float8_e4m3fn (None
+    otherwise); Y is None without need_Y, which needs quantize."""
+    torch = _torch()
+    if X.dim() != 2:
+        raise AbtError("X must be [M, n]")
+    M, n = X.shape
+    _plain_matrix(X, "X", (M, n), X.dtype), _plain_matrix(gain, "gain", (n,), torch.float32)
+    if residual is not None:
+        _plain_matrix(residual, "residual", (M, n), X.dtype)
+    if Y is not None:
+        _plain_matrix(Y, "Y", (M, n), X.dtype)
+    elif need_Y:
+        Y = torch.empty_like(X)
+    if H is not None:
+        _plain_matrix(H, "H", (M, n), X.dtype)
+    elif residual is not None:
+        H = torch.empty_like(X)
+    Yq = torch.empty((M, n), dtype=torch.float8_e4m3fn, device=X.device) if quantize else None
+    y_scale = torch.empty((M,), dtype=torch.float32, device=X.device) if quantize else None
+    _check(load().lr_rms_norm_fwd(X.data_ptr(), _ptr(residual), gain.data_ptr(), float(eps), _ptr(H), _ptr(Y if need_Y else None), _ptr(Yq), _ptr(y_scale),
+                                  M, n, _dt(X), _stream()), "lr_rms_norm_fwd")
+    return (Y if need_Y else None), (H if H is not None else X), Yq, y_scale
+
+
+def lr_rms_norm_bwd(dY, H, gain, eps: float = 1e-6, dH=None, need_dX: bool = True, need_dgain: bool = True, dX=None, dgain=None,
+                    accumulate: bool = False, workspace=None):
+    """Gradients of lr_rms_norm_fwd at its H: dX [M, n], which is also the residual's gradient (dH, the gradient that reaches H past the
+    norm, is added), and dgain [n] fp32.  Returns (dX, dgain); skipped ones are None."""
+    torch = _torch()
+    lib = load()
+    if H.dim() != 2:
+        raise AbtError("H must be [M, n]")
+    M, n = H.shape
+    for t, nm in ((dY, "dY"), (H, "H"), (dH, "dH"), (dX, "dX")):
+        if t is not None:
+            _plain_matrix(t, nm, (M, n), H.dtype)
+    _plain_matrix(gain, "gain", (n,), torch.float32)
+    if dgain is not None:
+        _plain_matrix(dgain, "dgain", (n,), torch.float32)
+    if need_dX and dX is None:
+        dX = torch.empty_like(H)
+    if need_dgain and dgain is None:
+        if accumulate:
+            raise AbtError("accumulate needs existing dgain")
+        dgain = torch.empty((n,), dtype=torch.float32, device=H.device)
+    dt = _dt(H)
+    ws = _workspace(lib.lr_rms_norm_bwd_workspace_bytes(M, n, dt), H.device, workspace) if need_dgain else None
+    _check(lib.lr_rms_norm_bwd(dY.data_ptr(), H.data_ptr(), gain.data_ptr(), float(eps), _ptr(dH), _ptr(dX if need_dX else None),
+                               _ptr(dgain if need_dgain else None), M, n, dt, int(bool(accumulate)), _ptr(ws),
+                               ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "lr_rms_norm_bwd")
+    return (dX if need_dX else None), (dgain if need_dgain else None)
 
 
 def ab_reconstruct(A, B, W=None):

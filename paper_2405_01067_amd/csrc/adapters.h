@@ -1,0 +1,62 @@
+// A frozen dense layer with low-rank adapters, row by row another one (adapters.hip, adapters_few.hip, adapters_grad.hip): what
+// adapters_api.hip calls.
+#pragma once
+
+#include "common.h"
+
+namespace abt {
+
+// Out_i = Main_i . W^T + E_i . F_a^T for the rows i of adapter a = row_adapter[i]; an id outside [0, count) is no adapter.  Main or E may be absent.
+struct AdapterProduct {
+    const void* X; const void* W;          // [M, kmain], [Q, kmain], bf16 or 8-bit floats; X NULL: no main product
+    const float* x_scale; const float* w_scale;      // 8 bits: per row of X and of W
+    const uint16_t* E; const uint16_t* F;  // [M, e_pitch] of which ke columns count, [count, Q, ke]
+    const int32_t* row_adapter; const int32_t* ranks; const float* scales;   // ranks, scales may be NULL: r, 1
+    int64_t M;
+    int Q, kmain, ke, e_pitch, count, r;
+    // what is made of it:
+    uint16_t* Y;                           // [M, Q] rounded (E holds T, rank columns of ke)
+    float* T;                              // or, Q = r: T [M, r] fp32 (columns from the rank on zero), may be NULL
+    uint16_t* Tb;                          // and scale times it, rounded, [M, r], may be NULL
+    const float* T_in;                     // or, Q = r: planes of scale times the result, and of scale times T_in [M, r]: three bf16 values whose sum is the
+    uint16_t* dT_planes; uint16_t* T_planes;   // fp32 value, [M, 3, rp], rp = plane_columns(r)
+};
+// r padded to what the factor gradients work in: a power of two of blocks of 16
+inline __host__ __device__ int plane_columns(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
+
+hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s);
+hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s);         // X absent, Q = r <= 128
+hipError_t launch_adapters_planes(const AdapterProduct& p, hipStream_t s);    // the same
+
+// Few rows
+constexpr int kAdapterFewRows = 64, kAdapterFewT = 128;
+hipError_t launch_adapters_few_y(const AdapterProduct& p, bool fp8, hipStream_t s);       // M <= kAdapterFewRows
+hipError_t launch_adapters_few_t(const AdapterProduct& p, hipStream_t s);                 // M <= kAdapterFewT
+
+// What the backward prepares in one launch: W^T, the transposes of every adapter's A and B, the rows of each adapter one after the other in
+// `order` (rows ascending) with offsets[count + 1], and 256 bytes of zeros.
+struct AdapterPrep {
+    const uint16_t* W; uint16_t* Wt;       // [m, n] -> [n, m]; NULL: not wanted
+    const uint16_t* A; uint16_t* At;       // [count, m, r] -> [count, r, m]
+    const uint16_t* B; uint16_t* Bt;       // [count, r, n] -> [count, n, r]
+    const int32_t* row_adapter; int32_t* order; int32_t* offsets;
+    unsigned char* zeros;
+    int64_t M;
+    int m, n, r, count;
+};
+hipError_t launch_adapters_prep(const AdapterPrep& p, hipStream_t s);
+
+// dA[a] = sum of U_i V_i^T over the rows of adapter a, both sides in one launch, then their sums.
+struct AdapterGrads {
+    const uint16_t* dY; const uint16_t* T_planes; float* dA;      // dA [count, m, r], NULL: not wanted
+    const uint16_t* X; const uint16_t* dT_planes; float* dB;      // dB [count, r, n]
+    const int32_t* order; const int32_t* offsets; const unsigned char* zeros;
+    float* partials;
+    int64_t M;
+    int m, n, r, count, accumulate;
+};
+int adapters_grad_piece(int64_t M, int m, int n);      // rows of a piece
+size_t adapters_grad_partial_bytes(int64_t M, int m, int n, int r, int count);
+hipError_t launch_adapters_grads(const AdapterGrads& p, hipStream_t s);
+
+}  // namespace abt

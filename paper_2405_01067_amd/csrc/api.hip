@@ -6,7 +6,7 @@
 #include <new>
 #include <vector>
 
-#include "common.h"
+#include "api_util.h"
 
 using namespace abt;
 
@@ -343,21 +343,6 @@ hipError_t chain(const void* Xin, const void* P, const void* Q, void* Yout, void
     return launch_chain2_bf16(Xin, P, Q, Yout, Tout, M, p, q, R, s);
 }
 
-// The entry points promise not to throw: what the host-side tables of a call may throw (allocation
-// failure of a std::vector) becomes a status.
-template <class F>
-int guarded(F&& f) {
-    try { return f(); }
-    catch (const std::bad_alloc&) { return ABT_ENOMEM; }
-    catch (...) { return ABT_EHIP; }
-}
-template <class F>
-size_t guarded_size(F&& f) {
-    try { return f(); }
-    catch (...) { return 0; }
-}
-
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t esize(int dt) { return dt == ABT_BF16 ? 2 : 4; }
 
 int check_lr_shapes(int64_t M, int64_t m, int64_t n, int64_t r, int dt) {
@@ -486,6 +471,56 @@ hipError_t few_gradients(SmallBwd few, float* dA, float* dB, int64_t m, int64_t 
     if (dA) done[nd++] = TnJob{nullptr, nullptr, dA, (int)m, 0};
     if (dB) done[nd++] = TnJob{nullptr, nullptr, dB, (int)n, 1};
     return launch_tn_finish(done, nd, (int)r, acc, part, s);
+}
+
+struct ClipRequest { double max_norm; float* norm_out; void* workspace; size_t bytes; };
+
+int adamw_step(const abt_adamw_tensor* tensors, int n, int64_t step, double lr, double lr_scale, double beta1, double beta2, double eps,
+               double weight_decay, const ClipRequest* clip, void* stream) {
+    if (n < 0 || (n > 0 && !tensors) || step < 1) return ABT_EINVAL;
+    if (!std::isfinite(lr) || !std::isfinite(lr_scale) || !std::isfinite(eps) || !std::isfinite(weight_decay) ||
+        !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || eps < 0.0)
+        return ABT_EINVAL;
+    return guarded([&]() -> int {
+    std::vector<AdamwTensor> v;
+    v.reserve((size_t)n);
+    for (int i = 0; i < n; ++i) {
+        const abt_adamw_tensor& t = tensors[i];
+        if (t.count < 0) return ABT_ESHAPE;
+        if (t.count == 0) continue;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return ABT_EINVAL;
+        if (!aligned(t.param, 16) || !aligned(t.grad, 16) || !aligned(t.exp_avg, 16) ||
+            !aligned(t.exp_avg_sq, 16) || !aligned(t.param_bf16, 16))
+            return ABT_EALIGN;
+        v.push_back(AdamwTensor{t.param, t.grad, t.exp_avg, t.exp_avg_sq, (uint16_t*)t.param_bf16, t.count});
+    }
+    if (clip) {
+        if (!aligned(clip->norm_out, 4) || !aligned(clip->workspace, 256)) return ABT_EALIGN;
+        if (!clip->workspace || clip->bytes < ab_grad_norm_workspace_bytes(n)) return ABT_EWORKSPACE;
+        for (const AdamwTensor& t : v)
+            if (t.count > (1ll << 40)) return ABT_ESHAPE;
+        if (v.empty() && clip->norm_out)
+            return launch_grad_norm((const double*)clip->workspace, 0, clip->norm_out, (hipStream_t)stream) == hipSuccess ? ABT_OK : ABT_EHIP;
+    }
+    if (v.empty()) return ABT_OK;
+    AdamwHyper h;
+    const double b1 = beta1, b2 = beta2;
+    h.beta1 = (float)beta1; h.beta2 = (float)beta2;
+    h.one_minus_beta1 = (float)(1.0 - b1); h.one_minus_beta2 = (float)(1.0 - b2);
+    // 1 - beta^step, without cancellation when beta^step is close to 1
+    const double bc1 = b1 > 0.0 ? -std::expm1((double)step * std::log(b1)) : 1.0;
+    const double bc2 = b2 > 0.0 ? -std::expm1((double)step * std::log(b2)) : 1.0;
+    h.inv_bc1 = (float)(1.0 / bc1);
+    h.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
+    h.eps = (float)eps; h.eta = (float)(lr * lr_scale); h.weight_decay = (float)weight_decay;
+    if (!clip) return launch_adamw(v.data(), (int)v.size(), h, (hipStream_t)stream) == hipSuccess ? ABT_OK : ABT_EHIP;
+    std::vector<GradTensor> grads;
+    grads.reserve(v.size());
+    for (const AdamwTensor& t : v) grads.push_back(GradTensor{t.grad, nullptr, t.count, false});
+    AdamwClip c{(const double*)clip->workspace, clip->norm_out, clip->max_norm, 0};
+    if (launch_grad_sums(grads.data(), (int)grads.size(), (double*)clip->workspace, &c.nsums, (hipStream_t)stream) != hipSuccess) return ABT_EHIP;
+    return launch_adamw(v.data(), (int)v.size(), h, (hipStream_t)stream, &c) == hipSuccess ? ABT_OK : ABT_EHIP;
+    });
 }
 
 }  // namespace
@@ -847,36 +882,16 @@ int lr_conv_bwd(const void* dY, const void* act, const void* T, const void* A, c
 int ab_adamw_step(const abt_adamw_tensor* tensors, int n, int64_t step,
                   double lr, double lr_scale, double beta1, double beta2, double eps,
                   double weight_decay, void* stream) {
-    if (n < 0 || (n > 0 && !tensors) || step < 1) return ABT_EINVAL;
-    if (!std::isfinite(lr) || !std::isfinite(lr_scale) || !std::isfinite(eps) || !std::isfinite(weight_decay) ||
-        !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || eps < 0.0)
-        return ABT_EINVAL;
-    return guarded([&]() -> int {
-    std::vector<AdamwTensor> v;
-    v.reserve((size_t)n);
-    for (int i = 0; i < n; ++i) {
-        const abt_adamw_tensor& t = tensors[i];
-        if (t.count < 0) return ABT_ESHAPE;
-        if (t.count == 0) continue;
-        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return ABT_EINVAL;
-        if (!aligned(t.param, 16) || !aligned(t.grad, 16) || !aligned(t.exp_avg, 16) ||
-            !aligned(t.exp_avg_sq, 16) || !aligned(t.param_bf16, 16))
-            return ABT_EALIGN;
-        v.push_back(AdamwTensor{t.param, t.grad, t.exp_avg, t.exp_avg_sq, (uint16_t*)t.param_bf16, t.count});
-    }
-    if (v.empty()) return ABT_OK;
-    AdamwHyper h;
-    const double b1 = beta1, b2 = beta2;
-    h.beta1 = (float)beta1; h.beta2 = (float)beta2;
-    h.one_minus_beta1 = (float)(1.0 - b1); h.one_minus_beta2 = (float)(1.0 - b2);
-    // 1 - beta^step, without cancellation when beta^step is close to 1
-    const double bc1 = b1 > 0.0 ? -std::expm1((double)step * std::log(b1)) : 1.0;
-    const double bc2 = b2 > 0.0 ? -std::expm1((double)step * std::log(b2)) : 1.0;
-    h.inv_bc1 = (float)(1.0 / bc1);
-    h.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
-    h.eps = (float)eps; h.eta = (float)(lr * lr_scale); h.weight_decay = (float)weight_decay;
-    return launch_adamw(v.data(), (int)v.size(), h, (hipStream_t)stream) == hipSuccess ? ABT_OK : ABT_EHIP;
-    });
+    return adamw_step(tensors, n, step, lr, lr_scale, beta1, beta2, eps, weight_decay, nullptr, stream);
+}
+
+int ab_adamw_step_clipped(const abt_adamw_tensor* tensors, int n, int64_t step,
+                          double lr, double lr_scale, double beta1, double beta2, double eps,
+                          double weight_decay, double max_norm, float* norm_out,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    if (!(max_norm >= 0.0) || !std::isfinite(max_norm)) return ABT_EINVAL;
+    const ClipRequest clip{max_norm, norm_out, workspace, workspace_bytes};
+    return adamw_step(tensors, n, step, lr, lr_scale, beta1, beta2, eps, weight_decay, &clip, stream);
 }
 
 double ab_lr_rebound_scale(int64_t i, int64_t rebound_steps) {

@@ -326,6 +326,26 @@ struct AdamwHyper {   // everything the kernel needs, prepared on the host in do
     float inv_sqrt_bc2;   // 1 / sqrt(1 - beta2^step)
     float eps, eta, weight_decay;   // eta = lr * lr_scale
 };
-hipError_t launch_adamw(const AdamwTensor* tensors, int n, const AdamwHyper& h, hipStream_t s);
+struct AdamwClip { const double* sums; float* norm_out; double max_norm; int nsums; };     // from launch_grad_sums; norm_out may be NULL
+// clip: the gradients are scaled to a global norm of max_norm at most; nothing is written where the norm is not finite (at least one tensor with elements)
+hipError_t launch_adamw(const AdamwTensor* tensors, int n, const AdamwHyper& h, hipStream_t s, const AdamwClip* clip = nullptr);
+
+// ------------------------------------------------------------------ global norm of the gradients
+constexpr int kGradMaxTensors = 128;      // per launch
+struct GradTensor { const void* grad; void* out; int64_t count; bool bf16; };   // count up to 2^40
+int grad_sums_capacity(int n);            // values that launch_grad_sums may write for n tensors
+hipError_t launch_grad_sums(const GradTensor* t, int n, double* sums, int* nsums, hipStream_t s);
+hipError_t launch_grad_norm(const double* sums, int nsums, float* norm_out, hipStream_t s);
+// out = c grad, in place where out is grad; norm_out may be NULL
+hipError_t launch_grad_clip(const GradTensor* t, int n, const double* sums, int nsums, double max_norm, float* norm_out, hipStream_t s);
+
+// ------------------------------------------------------------------ root-mean-square norm
+// n a multiple of 8, at most 16384; R, H, Y (not with Yq NULL) and Yq with scale may be NULL.  H may be R or X.
+hipError_t launch_rms_norm_fwd(const void* X, const void* R, const float* gain, float eps, void* H, void* Y, void* Yq, float* scale, int64_t M, int n, bool bf16,
+                               hipStream_t s);
+// sums: rms_norm_bwd_blocks * n values, where dgain is wanted; dH, dX, dgain may be NULL
+int rms_norm_bwd_blocks(int64_t M, int n);
+hipError_t launch_rms_norm_bwd(const void* dY, const void* H, const float* gain, float eps, const void* dH, void* dX, float* dgain, float* sums, int64_t M, int n,
+                               bool bf16, int accumulate, hipStream_t s);
 
 }  // namespace abt

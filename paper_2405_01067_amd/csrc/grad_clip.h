@@ -1,0 +1,29 @@
+// What the two kernels share that use the global norm of the gradients: the norm from the partial sums, and the factor.
+#pragma once
+
+#include "common.h"
+
+namespace abt {
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// N from the sums, by every work-group of 256 threads for itself (all of its threads call)
+__device__ __forceinline__ double norm_of(const double* sums, int nsums) {
+    __shared__ double part[4];
+    double v = 0.0;
+    for (int i = threadIdx.x; i < nsums; i += 256) v += gload(sums + i);
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return sqrt(part[0] + part[1] + part[2] + part[3]);
+}
+
+__device__ __forceinline__ bool norm_finite(double N) { return N <= 1.7976931348623157e308; }      // false for NaN too
+// A norm that is not finite scales nothing.
+__device__ __forceinline__ float clip_factor(double N, double max_norm) { return N > max_norm && norm_finite(N) ? (float)(max_norm / N) : 1.0f; }
+
+}  // namespace abt

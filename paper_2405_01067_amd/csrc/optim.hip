@@ -6,7 +6,7 @@
 // kernels read.  Every work-group takes one chunk of 4096 consecutive elements of one tensor; a
 // table in the kernel arguments maps blockIdx.x to (tensor, chunk), so the many small factor
 // tensors of a model (a few hundred thousand elements each) fill the chip in one launch.
-#include "common.h"
+#include "grad_clip.h"
 
 namespace abt {
 namespace {
@@ -36,7 +36,17 @@ __device__ __forceinline__ AdamwOut adamw_element(float theta, float g, float m,
     return o;
 }
 
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTable a) {
+// CLIP: the gradients count c times, with c from the sums of their squares (grad_clip.hip); where their norm is not finite nothing is written but the norm.
+template <bool CLIP>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTable a, const AdamwClip clip) {
+    float c = 1.0f;
+    if constexpr (CLIP) {
+        const double N = norm_of(clip.sums, clip.nsums);
+        if (clip.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *clip.norm_out = (float)N;
+        if (!norm_finite(N)) return;
+        c = clip_factor(N, clip.max_norm);
+    }
+    const auto clipped = [c](float g) { return CLIP ? c * g : g; };
     // blockIdx.x -> tensor: the table is short and wave-uniform, a linear scan is enough
     int ti = 0;
     while (ti + 1 < a.n && (int)blockIdx.x >= a.first_block[ti + 1]) ++ti;
@@ -64,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTable a) {
             f32x4 th1, m1, v1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const AdamwOut o = adamw_element(th[j], g[j], m[j], v[j], a);
+                const AdamwOut o = adamw_element(th[j], clipped(g[j]), m[j], v[j], a);
                 th1[j] = o.theta; m1[j] = o.m; v1[j] = o.v;
             }
             *reinterpret_cast<f32x4*>(P + e) = th1;
@@ -78,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTable a) {
             }
         } else {
             for (int j = e; j < here; ++j) {   // ragged tail of the tensor: at most three elements
-                const AdamwOut o = adamw_element(P[j], G[j], Mo[j], V[j], a);
+                const AdamwOut o = adamw_element(P[j], clipped(G[j]), Mo[j], V[j], a);
                 P[j] = o.theta; Mo[j] = o.m; V[j] = o.v;
                 if (Pb) Pb[j] = (uint16_t)(pack2_bf16(o.theta, 0.0f) & 0xffffu);
             }
@@ -88,8 +98,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTable a) {
 
 }  // namespace
 
-hipError_t launch_adamw(const AdamwTensor* tensors, int n, const AdamwHyper& h, hipStream_t s) {
+hipError_t launch_adamw(const AdamwTensor* tensors, int n, const AdamwHyper& h, hipStream_t s, const AdamwClip* clip) {
     int done = 0;
+    AdamwClip once = clip ? *clip : AdamwClip{};
     while (done < n) {
         AdamwTable a{};
         int blocks = 0, k = 0;
@@ -114,7 +125,9 @@ hipError_t launch_adamw(const AdamwTensor* tensors, int n, const AdamwHyper& h, 
         a.one_minus_beta1 = h.one_minus_beta1; a.one_minus_beta2 = h.one_minus_beta2;
         a.inv_bc1 = h.inv_bc1; a.inv_sqrt_bc2 = h.inv_sqrt_bc2;
         a.eps = h.eps; a.eta = h.eta; a.weight_decay = h.weight_decay;
-        hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+        if (clip) hipLaunchKernelGGL(adamw_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, once);
+        else hipLaunchKernelGGL(adamw_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, once);
+        once.norm_out = nullptr;
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
