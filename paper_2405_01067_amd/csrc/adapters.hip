@@ -1,13 +1,12 @@
 // The products of a dense layer with adapters for many rows:
 //     Y_i = W x_i + A_a T_i          T_i = B_a x_i          a = adapter of row i, T scaled where it is an operand
-// One kernel makes all of them: a tile of the result sums over slabs of the contraction, first those of the dense product, then for
-// every adapter that occurs among its rows those of the low-rank one, with the rows of other adapters read as zeros.  Rows that
-// lie together by adapter therefore cost a tile one or two short passes, rows in any other order more passes, and the result is the same
-// but for the order of its sums.  T alone is the case without a dense product.
+// Y: a tile of the dense product, then in the same accumulators the adapters that occur among its rows, one after the other, with the T of other
+// adapters' rows as zeros.  Rows that lie together by adapter cost a tile one or two short passes; rows in any other order more of them.
+// T: 32 rows against the B of all adapters among them, side by side as columns of one product; every row keeps those of its own.
 //
 // A slab is 128 bytes of every row: 64 columns in bf16, 128 in 8 bits.  It comes straight to LDS, NS slots in a ring, one barrier per
-// slab; the operands of a step are read while the products of the step before run, across the barrier too.  Both types read LDS alike: two
-// 16-byte pieces are two bf16 operands of 32x32x16 or one 8-bit operand of 32x32x64, whose columns are taken in the same order on both sides.
+// slab.  Both types read LDS alike: two 16-byte pieces are two bf16 operands of 32x32x16 or one 8-bit operand of 32x32x64, whose columns are taken in
+// the same order on both sides.
 #include <atomic>
 #include <climits>
 
@@ -31,8 +30,21 @@ __device__ __forceinline__ u32x4 first_of(u32x4 v, int valid) {
     return v;
 }
 
-enum { kOutY, kOutT, kOutPlanes };
+// The smallest of the lanes' values, INT_MAX where none is left
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const int o = __shfl_xor(v, d);
+        v = o < v ? o : v;
+    }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int rank_of(const AdapterProduct& g, int a) {
+    const int k = g.ranks ? gload(g.ranks + a) : g.r;
+    return k < 0 ? 0 : k > g.r ? g.r : k;
+}
 
+// ------------------------------------------------------------------------------------------ Y
 // WM x WN waves, each RB x CB blocks of 32 x 32
 template <int TM_, int TN_, int WM_, int WN_, int NS_>
 struct Tile {
@@ -40,12 +52,11 @@ struct Tile {
     static constexpr int RB = TM / (32 * WM), CB = TN / (32 * WN);
     static constexpr int xpart = TM * 128, slab = (TM + TN) * 128;
     static constexpr int NX = TM / 8 / NW, NF = TN / 8 / NW, NL = NX + NF;       // load instructions per wave and slab: eight rows each
-    static constexpr int IDS = (TM + 63) / 64;
     static constexpr int opitch = TN * 2 + 16;
     static constexpr int out = TM * opitch;
-    static __host__ __device__ constexpr int lds(int kind) { return kind == kOutY && out > NS * slab ? out : NS * slab; }
+    static constexpr int lds = out > NS * slab ? out : NS * slab;
     static_assert(NX * 8 * NW == TM && NF * 8 * NW == TN && RB * 32 * WM == TM && CB * 32 * WN == TN, "");
-    static_assert(NW % 2 == 0 && (NS - 2) * NL < 64, "");
+    static_assert(NW % 2 == 0 && (NS - 2) * NL < 64 && lds <= 160 * 1024, "");
 };
 
 struct Order { int row_tiles, col_tiles; };
@@ -61,10 +72,9 @@ __device__ __forceinline__ void tile_of(const Order& o, int& rt, int& ct) {
     ct = at / rows;
 }
 
-template <class L, bool F8, int OUT>
-__global__ __launch_bounds__(64 * L::NW) void adapters_kernel(const AdapterProduct g, const Order order) {
+template <class L, bool F8>
+__global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterProduct g, const Order order) {
     constexpr int RB = L::RB, CB = L::CB, NW = L::NW, NS = L::NS;
-    constexpr int ES = F8 ? 1 : 2;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5;
@@ -76,100 +86,37 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_kernel(const AdapterProdu
     const int rows = g.M - row0 < L::TM ? (int)(g.M - row0) : L::TM;
     const int cols = g.Q - col0 < L::TN ? g.Q - col0 : L::TN;
 
-    // ---- loads: instruction j of a wave covers rows 8 (wave + NW j) .. + 7 of X, or of W; this lane's row among them and its chunk
+    // Load instruction j of a wave covers rows 8 (wave + NW j) .. + 7 of X, or of W: this lane's row among them and its chunk (NW is even, so the chunk
+    // is the same for all j).  Rows past the last one read zeros, and so do chunks past the end of a row.
     const int lrow = 8 * wave + (lane >> 3);
-    const int chunk = ((lane & 7) ^ ((lrow >> 1) & 7)) * 16;       // NW is even: the same for all j
-    const int main_bytes = g.kmain * ES;
-    const int nmain = OUT == kOutY ? (main_bytes + 127) / 128 : 0;
-    const rsrc_t xres = OUT == kOutY ? make_rsrc((const char*)g.X + row0 * main_bytes, (int64_t)rows * main_bytes) : make_rsrc(nullptr, 0);
-    const rsrc_t wres = OUT == kOutY ? make_rsrc((const char*)g.W + (int64_t)col0 * main_bytes, (int64_t)cols * main_bytes) : make_rsrc(nullptr, 0);
-    int issue_slot = 0;
-    auto issue_main = [&](int s) {
+    const int chunk = ((lane & 7) ^ ((lrow >> 1) & 7)) * 16;
+    const int bytes = g.kmain * (F8 ? 1 : 2), nmain = (bytes + 127) / 128;
+    const rsrc_t xres = make_rsrc((const char*)g.X + row0 * bytes, (int64_t)rows * bytes);
+    const rsrc_t wres = make_rsrc((const char*)g.W + (int64_t)col0 * bytes, (int64_t)cols * bytes);
+    int issue_slot = 0, issued = 0;
+    auto issue = [&]() {
         unsigned char* const dst = lds + issue_slot + wave * 1024;
         issue_slot = issue_slot == (NS - 1) * L::slab ? 0 : issue_slot + L::slab;
-        const int at = s * 128 + chunk;                   // chunks past the end of a row arrive as zeros
-        const int off = at < main_bytes ? lrow * main_bytes + at : kBufNowhere;
-        const int step = at < main_bytes ? 8 * NW * main_bytes : 0;
+        const int at = issued * 128 + chunk;
+        ++issued;
+        const int off = at < bytes ? lrow * bytes + at : kBufNowhere;
+        const int step = at < bytes ? 8 * NW * bytes : 0;
 #pragma unroll
         for (int j = 0; j < L::NX; ++j) load_lds16(xres, dst + j * (NW * 1024), off + j * step, 0);
 #pragma unroll
         for (int j = 0; j < L::NF; ++j) load_lds16(wres, dst + L::xpart + j * (NW * 1024), off + j * step, 0);
     };
-    int issued = 0;                                       // slabs
-    if constexpr (OUT == kOutY) {
-        for (; issued < NS - 1 && issued < nmain; ++issued) issue_main(issued);
+    while (issued < NS - 1 && issued < nmain) issue();
+
+    // the adapters of this lane's rows
+    int mine[RB];
+#pragma unroll
+    for (int a = 0; a < RB; ++a) {
+        const int r = (wr * RB + a) * 32 + lj;
+        const int id = gload(g.row_adapter + row0 + (r < rows ? r : 0));
+        mine[a] = r < rows && id >= 0 && id < g.count ? id : -1;
     }
 
-    // ---- adapters of the rows: of all rows of the tile (to find the next one), and of the rows this lane loads
-    const int K = g.count;
-    int ids[L::IDS], lid[L::NX];
-#pragma unroll
-    for (int i = 0; i < L::IDS; ++i) {
-        const int r = 64 * i + lane;
-        const int a = r < rows ? gload(g.row_adapter + row0 + r) : -1;
-        ids[i] = a >= 0 && a < K ? a : -1;
-    }
-#pragma unroll
-    for (int j = 0; j < L::NX; ++j) {
-        const int r = lrow + 8 * NW * j;
-        lid[j] = r < rows ? gload(g.row_adapter + row0 + r) : -1;
-    }
-    auto after = [&](int a) {                             // the smallest adapter above a that has rows here; INT_MAX: none
-        int best = INT_MAX;
-#pragma unroll
-        for (int i = 0; i < L::IDS; ++i) best = ids[i] > a && ids[i] < best ? ids[i] : best;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            const int o = __shfl_xor(best, d);
-            best = o < best ? o : best;
-        }
-        return __builtin_amdgcn_readfirstlane(best);
-    };
-    auto rank_of = [&](int a) {
-        if (a == INT_MAX) return 0;
-        int k = g.ranks ? __builtin_amdgcn_readfirstlane(gload(g.ranks + a)) : g.r;
-        return k < 0 ? 0 : k > g.r ? g.r : k;
-    };
-    // Y: the contraction is the rank; T and the planes: the rank counts columns
-    auto length_of = [&](int rank) { return OUT == kOutY ? rank : rank > col0 ? g.ke : 0; };
-    struct Walk { int a, rank, len, k; };                 // adapter, its rank, its contraction, the next column of it
-    auto settle = [&](Walk& w) {                          // to an adapter with something left to contract
-        while (w.a != INT_MAX && w.k >= w.len) {
-            w.a = after(w.a);
-            w.rank = rank_of(w.a);
-            w.len = w.a == INT_MAX ? 0 : length_of(w.rank);
-            w.k = 0;
-        }
-    };
-    Walk in{-1, 0, 0, 0};
-    settle(in);
-    Walk out = in;
-    const rsrc_t eres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
-    auto issue_low = [&]() {
-        unsigned char* const dst = lds + issue_slot + wave * 1024;
-        issue_slot = issue_slot == (NS - 1) * L::slab ? 0 : issue_slot + L::slab;
-        const int frows = OUT == kOutY ? cols : (in.rank - col0 < cols ? in.rank - col0 : cols);
-        const rsrc_t fres = make_rsrc(g.F + ((int64_t)in.a * g.Q + col0) * g.ke, (int64_t)frows * g.ke * 2);
-        const int at = in.k * 2 + chunk;
-        const bool ok = at < in.len * 2;
-#pragma unroll
-        for (int j = 0; j < L::NX; ++j)
-            load_lds16(eres, dst + j * (NW * 1024), ok && lid[j] == in.a ? (lrow + 8 * NW * j) * g.e_pitch * 2 + at : kBufNowhere, 0);
-#pragma unroll
-        for (int j = 0; j < L::NF; ++j)
-            load_lds16(fres, dst + L::xpart + j * (NW * 1024), ok ? (lrow + 8 * NW * j) * g.ke * 2 + at : kBufNowhere, 0);
-        in.k += 64;
-        settle(in);
-    };
-    auto issue = [&]() {                                  // the next slab, if there is one
-        if (issued < nmain) issue_main(issued);
-        else if (in.a != INT_MAX) issue_low();
-        else return;
-        ++issued;
-    };
-    while (issued < NS - 1 && in.a != INT_MAX) issue();
-
-    // ---- products
     f32x16 acc[RB][CB];
 #pragma unroll
     for (int a = 0; a < RB; ++a)
@@ -209,176 +156,136 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_kernel(const AdapterProdu
         else if (NS > 3 && behind == NS - 3) wait_newest<(NS > 3 ? NS - 3 : 0) * L::NL>();
         else wait_newest<0>();
         lds_barrier();
-        issue();                                          // into the slot whose reads ended before this barrier
+        if (issued < nmain) issue();                      // into the slot whose reads ended before this barrier
         const int at = slot;
         slot = slot == (NS - 1) * L::slab ? 0 : slot + L::slab;
         ++done;
         return at;
     };
-    if constexpr (OUT == kOutY) {
-        Ops o[2];
+    Ops o[2];
+    if constexpr (F8) {
         for (int s = 0; s < nmain; ++s) {
             const int at = next_slab();
-            if constexpr (F8) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    read(o[0], at, 2 * j);
-                    read(o[1], at, 2 * j + 1);
-                    mma8(o[0], o[1]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    read(o[j & 1], at, j);
-                    mma(o[j & 1]);
-                }
+            for (int j = 0; j < 2; ++j) {
+                read(o[0], at, 2 * j);
+                read(o[1], at, 2 * j + 1);
+                mma8(o[0], o[1]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if constexpr (F8) {                               // the dense product's scales
-#pragma unroll
-            for (int a = 0; a < RB; ++a) {
-                const int r = (wr * RB + a) * 32 + lj;
-                const float xs = r < rows ? gload(g.x_scale + row0 + r) : 0.0f;
-#pragma unroll
-                for (int b = 0; b < CB; ++b)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int c = (wc * CB + b) * 32 + 16 * lh + v;
-                        acc[a][b][v] *= xs * (c < cols ? gload(g.w_scale + col0 + c) : 0.0f);
-                    }
-            }
-        }
-    }
-    while (out.a != INT_MAX) {
-        const int at = next_slab();
-        const int left = out.len - out.k < 64 ? out.len - out.k : 64;
-        const bool ragged = (left & 7) != 0;
-        const int steps = (left + 15) / 16;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j >= steps) break;
-            Ops o;
-            read(o, at, j);
-            if (ragged) {                                 // columns past the rank are no part of the adapter, whatever they hold
-                const int valid = left - (2 * j + lh) * 8;
-#pragma unroll
-                for (int b = 0; b < CB; ++b)
-                    if (valid < 8) o.f[b] = first_of(o.f[b], valid);
-#pragma unroll
-                for (int a = 0; a < RB; ++a)
-                    if (valid < 8) o.x[a] = first_of(o.x[a], valid);
-            }
-            mma(o);
-        }
-        out.k += 64;
-        settle(out);
-    }
-
-    // ---- out
-    if constexpr (OUT == kOutY) {
-        lds_barrier();                                    // every wave has read its last slab, and nothing is on its way to LDS
-#pragma unroll
-        for (int a = 0; a < RB; ++a)
-#pragma unroll
-            for (int b = 0; b < CB; ++b) {
-                unsigned char* const d = lds + ((wr * RB + a) * 32 + lj) * L::opitch + ((wc * CB + b) * 32 + 16 * lh) * 2;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x4 v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = pack2_bf16(acc[a][b][8 * h + 2 * i], acc[a][b][8 * h + 2 * i + 1]);
-                    *reinterpret_cast<u32x4*>(d + 16 * h) = v;
-                }
-            }
-        lds_barrier();
-        constexpr int CPR = L::TN / 8;
-        const rsrc_t yres = make_rsrc(g.Y + row0 * g.Q + col0, ((int64_t)(rows - 1) * g.Q + cols) * 2);
-#pragma unroll
-        for (int i = 0; i < L::TM * CPR / (64 * NW); ++i) {
-            const int e = i * (64 * NW) + (int)threadIdx.x, r = e / CPR, c = e % CPR;
-            buf_store16(*reinterpret_cast<const u32x4*>(lds + r * L::opitch + c * 16), yres, r < rows && c * 8 < cols ? (r * g.Q + c * 8) * 2 : kBufNowhere, 0);
-        }
-    } else {
+        // the dense product's scales
+        float xs[RB];
 #pragma unroll
         for (int a = 0; a < RB; ++a) {
             const int r = (wr * RB + a) * 32 + lj;
-            if (r >= rows) continue;
-            const int64_t row = row0 + r;
-            int id = gload(g.row_adapter + row);
-            if (id < 0 || id >= K) id = -1;
-            const float s = id < 0 ? 0.0f : g.scales ? gload(g.scales + id) : 1.0f;
-            int rank = id < 0 ? 0 : g.ranks ? gload(g.ranks + id) : g.r;
-            rank = rank > g.r ? g.r : rank;
-#pragma unroll
-            for (int b = 0; b < CB; ++b)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int c = col0 + (wc * CB + b) * 32 + 16 * lh + 8 * h;      // eight columns
-                    if constexpr (OUT == kOutT) {
-                        if (c >= g.r) continue;
-                        float v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = c + i < rank ? acc[a][b][8 * h + i] : 0.0f;
-                        if (g.T) {
-                            gstore(reinterpret_cast<f32x4*>(g.T + row * g.r + c), f32x4{v[0], v[1], v[2], v[3]});
-                            gstore(reinterpret_cast<f32x4*>(g.T + row * g.r + c + 4), f32x4{v[4], v[5], v[6], v[7]});
-                        }
-                        // T as an operand of the second product: one rounding to bf16, of the scaled value
-                        if (g.Tb) {
-                            u32x4 w;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(c + 2 * i < rank ? s * v[2 * i] : 0.0f, c + 2 * i + 1 < rank ? s * v[2 * i + 1] : 0.0f);
-                            gstore(reinterpret_cast<u32x4*>(g.Tb + row * g.r + c), w);
-                        }
-                    } else {
-                        const int rp = plane_columns(g.r);
-                        if (c >= rp) continue;
-                        // Three bf16 values that add up to the fp32 one (each takes eight bits of what the ones before left): the factor gradients are
-                        // fp32 sums of exact products, as they would be of fp32 operands.
-                        auto planes = [&](uint16_t* to, const float (&v)[8]) {
-                            u32x4 w[3];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                float x = v[2 * i], y = v[2 * i + 1];
-#pragma unroll
-                                for (int p = 0; p < 3; ++p) {
-                                    const uint32_t q = pack2_bf16(x, y);
-                                    w[p][i] = q;
-                                    x -= __builtin_bit_cast(float, q << 16);
-                                    y -= __builtin_bit_cast(float, q & 0xffff0000u);
-                                }
-                            }
-#pragma unroll
-                            for (int p = 0; p < 3; ++p) gstore(reinterpret_cast<u32x4*>(to + (row * 3 + p) * rp + c), w[p]);
-                        };
-                        float v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = c + i < rank ? s * acc[a][b][8 * h + i] : 0.0f;
-                        planes(g.dT_planes, v);
-                        if (g.T_planes) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) v[i] = c + i < rank ? s * gload(g.T_in + row * g.r + c + i) : 0.0f;
-                            planes(g.T_planes, v);
-                        }
-                    }
-                }
+            xs[a] = gload(g.x_scale + row0 + (r < rows ? r : 0));
         }
+#pragma unroll
+        for (int b = 0; b < CB; ++b) {
+            const int c = (wc * CB + b) * 32 + 16 * lh;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {                 // eight columns, all there or none (m is a multiple of 8)
+                f32x4 w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                if (c + 8 * h < cols)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) w[q][v] = gload(g.w_scale + col0 + c + 8 * h + 4 * q + v);
+#pragma unroll
+                for (int a = 0; a < RB; ++a)
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) acc[a][b][8 * h + v] *= xs[a] * w[v >> 2][v & 3];
+            }
+        }
+    } else {
+        // the operands of a step are read while the products of the step before run, across the barrier too
+#pragma unroll
+        for (int a = 0; a < RB; ++a) o[1].x[a] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < CB; ++b) o[1].f[b] = u32x4{0, 0, 0, 0};
+        for (int s = 0; s < nmain; ++s) {
+            const int at = next_slab();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                read(o[j & 1], at, j);
+                __builtin_amdgcn_sched_barrier(0);
+                mma(o[(j + 1) & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        mma(o[1]);
+    }
+
+    // The adapters of this wave's rows, in ascending order.  Their operands come straight from memory: 16 columns of 32 rows are one piece of it
+    // where the rank is 16, and there is little of it.
+    auto after = [&](int a) {
+        int best = INT_MAX;
+#pragma unroll
+        for (int i = 0; i < RB; ++i) best = mine[i] > a && mine[i] < best ? mine[i] : best;
+        return wave_min(best);
+    };
+    const rsrc_t eres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
+    const int eoff = ((wr * RB * 32 + lj) * g.e_pitch + 8 * lh) * 2, foff = ((wc * CB * 32 + frow) * g.ke + 8 * lh) * 2;
+    for (int a = after(-1); a != INT_MAX; a = after(a)) {
+        const int rank = __builtin_amdgcn_readfirstlane(rank_of(g, a));
+        const rsrc_t fres = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * g.ke, (int64_t)cols * g.ke * 2);
+#pragma unroll 1
+        for (int k = 0; k < rank; k += 16) {
+            const int valid = rank - k - 8 * lh;          // columns past the rank are no part of the adapter, whatever they hold
+#pragma unroll
+            for (int b = 0; b < CB; ++b) o[0].f[b] = buf_load16(fres, valid > 0 ? foff + b * 64 * g.ke + 2 * k : kBufNowhere, 0);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) o[0].x[i] = buf_load16(eres, valid > 0 && mine[i] == a ? eoff + i * 64 * g.e_pitch + 2 * k : kBufNowhere, 0);
+            if (rank - k < 16 && (rank & 7)) {
+                if (valid < 8) {
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) o[0].f[b] = first_of(o[0].f[b], valid);
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) o[0].x[i] = first_of(o[0].x[i], valid);
+                }
+            }
+            mma(o[0]);
+        }
+    }
+
+    // out through LDS as whole rows
+    lds_barrier();                                        // every wave has read its last slab, and nothing is on its way to LDS
+#pragma unroll
+    for (int a = 0; a < RB; ++a)
+#pragma unroll
+        for (int b = 0; b < CB; ++b) {
+            unsigned char* const d = lds + ((wr * RB + a) * 32 + lj) * L::opitch + ((wc * CB + b) * 32 + 16 * lh) * 2;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = pack2_bf16(acc[a][b][8 * h + 2 * i], acc[a][b][8 * h + 2 * i + 1]);
+                *reinterpret_cast<u32x4*>(d + 16 * h) = v;
+            }
+        }
+    lds_barrier();
+    constexpr int CPR = L::TN / 8;
+    const rsrc_t yres = make_rsrc(g.Y + row0 * g.Q + col0, ((int64_t)(rows - 1) * g.Q + cols) * 2);
+#pragma unroll
+    for (int i = 0; i < L::TM * CPR / (64 * NW); ++i) {
+        const int e = i * (64 * NW) + (int)threadIdx.x, r = e / CPR, c = e % CPR;
+        buf_store16(*reinterpret_cast<const u32x4*>(lds + r * L::opitch + c * 16), yres, r < rows && c * 8 < cols ? (r * g.Q + c * 8) * 2 : kBufNowhere, 0);
     }
 }
 
-template <class L, bool F8, int OUT>
+template <class L, bool F8>
 hipError_t launch_tile(const AdapterProduct& p, hipStream_t s) {
-    const void* const fn = reinterpret_cast<const void*>(&adapters_kernel<L, F8, OUT>);
-    static_assert(L::lds(OUT) <= 160 * 1024, "");
+    const void* const fn = reinterpret_cast<const void*>(&adapters_y_kernel<L, F8>);
     static std::atomic<bool> attr_set{false};
     if (!attr_set.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, L::lds(OUT));
+        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, L::lds);
         if (e != hipSuccess) return e;
         attr_set.store(true, std::memory_order_release);
     }
-    const int64_t rt = ceil_div(p.M, L::TM), ct = ceil_div(OUT == kOutPlanes ? plane_columns(p.r) : p.Q, L::TN);
+    const int64_t rt = ceil_div(p.M, L::TM), ct = ceil_div(p.Q, L::TN);
     if (rt * ct > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((adapters_kernel<L, F8, OUT>), dim3((unsigned)(rt * ct)), dim3(64 * L::NW), L::lds(OUT), s, p, Order{(int)rt, (int)ct});
+    hipLaunchKernelGGL((adapters_y_kernel<L, F8>), dim3((unsigned)(rt * ct)), dim3(64 * L::NW), L::lds, s, p, Order{(int)rt, (int)ct});
     return hipGetLastError();
 }
 
@@ -389,22 +296,215 @@ using T64 = Tile<64, 64, 2, 2, 6>;
 template <bool F8>
 hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
     const int64_t big = ceil_div(p.M, 256) * ceil_div(p.Q, 256), mid = ceil_div(p.M, 128) * ceil_div(p.Q, 128);
-    if (big >= 192) return launch_tile<T256, F8, kOutY>(p, s);
-    if (mid >= 192) return launch_tile<T128, F8, kOutY>(p, s);
-    return launch_tile<T64, F8, kOutY>(p, s);
+    if (big >= 192) return launch_tile<T256, F8>(p, s);
+    if (mid >= 192) return launch_tile<T128, F8>(p, s);
+    return launch_tile<T64, F8>(p, s);
 }
 
-template <int OUT>
+// ------------------------------------------------------------------------------------------ T
+// 32 rows a work-group; its four waves share out the four steps of a slab and add their sums at the end, in order.  CB blocks of 32 columns hold
+// 32 CB / r adapters; rows of more adapters than that take another pass over their x.
+template <int CB_, int NS_>
+struct Low {
+    static constexpr int CB = CB_, NS = NS_, TN = 32 * CB;
+    static constexpr int xpart = 4096, slab = xpart + TN * 128, NF = CB, NL = 1 + NF;
+    static constexpr int sums = 3 * CB * 4096;
+    static constexpr int ring = NS * slab > sums ? NS * slab : sums;
+    static constexpr int lds = ring + 32 * 3 * 4;         // and the adapters, their ranks, the rows' places among them
+    static_assert((NS - 2) * NL < 64 && lds <= 160 * 1024, "");
+};
+
+template <class L, bool PLANES>
+__global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g) {
+    constexpr int CB = L::CB, NS = L::NS;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    int* const list = reinterpret_cast<int*>(lds + L::ring);
+    int* const ranks = list + 32;
+    int* const place = ranks + 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lj = lane & 31, lh = lane >> 5;
+    const int64_t row0 = (int64_t)blockIdx.x * 32;
+    const int rows = g.M - row0 < 32 ? (int)(g.M - row0) : 32;
+    const int n = g.ke, r = g.r;
+
+    // which adapters the rows have, in ascending order, and which of them each row has
+    int id = gload(g.row_adapter + row0 + (lj < rows ? lj : 0));
+    id = lj < rows && id >= 0 && id < g.count ? id : -1;
+    int count = 0, at = -1;
+    for (int a = wave_min(id >= 0 ? id : INT_MAX); a != INT_MAX; a = wave_min(id > a ? id : INT_MAX)) {
+        if (id == a) at = count;
+        if (threadIdx.x == 0) list[count] = a;
+        ++count;
+    }
+    if (threadIdx.x < 32) place[lj] = at;
+    __syncthreads();
+    if ((int)threadIdx.x < count) ranks[threadIdx.x] = rank_of(g, list[threadIdx.x]);
+    __syncthreads();
+
+    const int slots = L::TN / r;
+    const int lrow = lane >> 3;
+    const int ns = (n * 2 + 127) / 128;
+    const int xrow = 8 * wave + lrow, xchunk = ((lane & 7) ^ ((xrow >> 1) & 7)) * 16;
+    const rsrc_t xres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
+    const int frow = out_row(lj);
+    const int xsw = (lj >> 1) & 7, fsw = (frow >> 1) & 7;
+    const int xread = lj * 128 + (((2 * wave + lh) ^ xsw) * 16), fread = L::xpart + frow * 128 + (((2 * wave + lh) ^ fsw) * 16);
+    for (int first = 0; first == 0 || first < count; first += slots) {
+        // Load instruction j covers eight columns, of one adapter (r is a multiple of 8): rows 8 (wave + 4 j) .. of the side-by-side B
+        rsrc_t fres[L::NF];
+        int used = 0;                                     // columns of this pass
+#pragma unroll
+        for (int j = 0; j < L::NF; ++j) {
+            const int c = 8 * (wave + 4 * j), p = first + c / r, k = c % r;
+            const bool have = c / r < slots && p < count;
+            const int a = have ? __builtin_amdgcn_readfirstlane(list[p]) : 0, rank = have ? __builtin_amdgcn_readfirstlane(ranks[p]) : 0;
+            fres[j] = make_rsrc(g.F + ((int64_t)a * r + k) * n, rank > k ? (int64_t)(rank - k) * n * 2 : 0);
+        }
+        used = (count - first < slots ? count - first : slots) * r;
+        int issue_slot = 0, issued = 0;
+        auto issue = [&]() {
+            unsigned char* const dst = lds + issue_slot + wave * 1024;
+            issue_slot = issue_slot == (NS - 1) * L::slab ? 0 : issue_slot + L::slab;
+            const int x = issued * 128 + xchunk;          // (the same chunk of eight rows further on)
+            ++issued;
+            load_lds16(xres, dst, x < 2 * n ? xrow * g.e_pitch * 2 + x : kBufNowhere, 0);
+#pragma unroll
+            for (int j = 0; j < L::NF; ++j) load_lds16(fres[j], dst + L::xpart + j * 4096, x < 2 * n ? lrow * n * 2 + x : kBufNowhere, 0);
+        };
+        while (issued < NS - 1 && issued < ns) issue();
+        f32x16 acc[CB];
+#pragma unroll
+        for (int b = 0; b < CB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[b][v] = 0.0f;
+        int slot = 0;
+        for (int s = 0; s < ns; ++s) {
+            const int behind = issued - s - 1;
+            if (behind >= NS - 2) wait_newest<(NS - 2) * L::NL>();
+            else if (NS > 3 && behind == NS - 3) wait_newest<(NS > 3 ? NS - 3 : 0) * L::NL>();
+            else wait_newest<0>();
+            lds_barrier();
+            if (issued < ns) issue();
+            const unsigned char* const x = lds + slot;
+            slot = slot == (NS - 1) * L::slab ? 0 : slot + L::slab;
+            const u32x4 xo = *reinterpret_cast<const u32x4*>(x + xread);
+            u32x4 fo[CB];
+#pragma unroll
+            for (int b = 0; b < CB; ++b) fo[b] = *reinterpret_cast<const u32x4*>(x + fread + b * 4096);
+#pragma unroll
+            for (int b = 0; b < CB; ++b) acc[b] = mfma_bf16(fo[b], xo, acc[b]);
+        }
+        // the waves' sums: blocks of 32 columns in turn, b by wave b % 4
+        lds_barrier();
+#pragma unroll
+        for (int b = 0; b < CB; ++b)
+            if (wave != b % 4) {
+                unsigned char* const d = lds + ((wave > b % 4 ? wave - 1 : wave) * CB + b) * 4096 + lane * 16;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) *reinterpret_cast<f32x4*>(d + v * 1024) = f32x4{acc[b][4 * v], acc[b][4 * v + 1], acc[b][4 * v + 2], acc[b][4 * v + 3]};
+            }
+        lds_barrier();
+#pragma unroll
+        for (int b = 0; b < CB; ++b) {
+            if (wave != b % 4 || (32 * b >= used && 32 * b >= r)) continue;
+#pragma unroll
+            for (int w = 0; w < 3; ++w) {
+                const unsigned char* const d = lds + (w * CB + b) * 4096 + lane * 16;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const f32x4 o = *reinterpret_cast<const f32x4*>(d + v * 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[b][4 * v + i] += o[i];
+                }
+            }
+            if (lj >= rows) continue;
+            const int64_t row = row0 + lj;
+            const int p = place[lj];
+            const float scale = p < 0 || !g.scales ? 1.0f : gload(g.scales + list[p]);
+            const int rank = p < 0 ? 0 : ranks[p];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c = 32 * b + 16 * lh + 8 * h, of = c / r, k = c % r;       // eight columns, those of this row's adapter?
+                if (of >= slots || (p < 0 ? first != 0 || of != 0 : p - first != of)) continue;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = k + i < rank ? acc[b][8 * h + i] : 0.0f;
+                if constexpr (!PLANES) {
+                    if (g.T) {
+                        gstore(reinterpret_cast<f32x4*>(g.T + row * r + k), f32x4{v[0], v[1], v[2], v[3]});
+                        gstore(reinterpret_cast<f32x4*>(g.T + row * r + k + 4), f32x4{v[4], v[5], v[6], v[7]});
+                    }
+                    // T as an operand of the second product: one rounding to bf16, of the scaled value
+                    if (g.Tb) {
+                        u32x4 w;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(k + 2 * i < rank ? scale * v[2 * i] : 0.0f, k + 2 * i + 1 < rank ? scale * v[2 * i + 1] : 0.0f);
+                        gstore(reinterpret_cast<u32x4*>(g.Tb + row * r + k), w);
+                    }
+                } else {
+                    // Three bf16 values that add up to the fp32 one (each takes eight bits of what the ones before left): the factor gradients are
+                    // fp32 sums of exact products, as they would be of fp32 operands.
+                    const int rp = plane_columns(r);
+                    auto planes = [&](uint16_t* to, const float (&u)[8]) {
+                        u32x4 w[3];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float x = u[2 * i], y = u[2 * i + 1];
+#pragma unroll
+                            for (int q = 0; q < 3; ++q) {
+                                const uint32_t t = pack2_bf16(x, y);
+                                w[q][i] = t;
+                                x -= __builtin_bit_cast(float, t << 16);
+                                y -= __builtin_bit_cast(float, t & 0xffff0000u);
+                            }
+                        }
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) {
+                            uint16_t* const d = to + (row * 3 + q) * rp;
+                            gstore(reinterpret_cast<u32x4*>(d + k), w[q]);
+                            if (k + 8 == r)               // the columns that the gradients' blocks have beyond r
+                                for (int z = r; z < rp; z += 8) gstore(reinterpret_cast<u32x4*>(d + z), u32x4{0, 0, 0, 0});
+                        }
+                    };
+                    float u[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[i] = k + i < rank ? scale * v[i] : 0.0f;
+                    planes(g.dT_planes, u);
+                    if (g.T_planes) {
+                        const f32x4 t0 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k)), t1 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k + 4));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) u[i] = k + i < rank ? scale * (i < 4 ? t0[i & 3] : t1[i & 3]) : 0.0f;
+                        planes(g.T_planes, u);
+                    }
+                }
+            }
+        }
+        lds_barrier();                                    // the ring is free for another pass
+    }
+}
+
+template <class L, bool PLANES>
+hipError_t launch_low_tile(const AdapterProduct& p, hipStream_t s) {
+    const void* const fn = reinterpret_cast<const void*>(&adapters_t_kernel<L, PLANES>);
+    static std::atomic<bool> attr_set{false};
+    if (!attr_set.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, L::lds);
+        if (e != hipSuccess) return e;
+        attr_set.store(true, std::memory_order_release);
+    }
+    hipLaunchKernelGGL((adapters_t_kernel<L, PLANES>), dim3((unsigned)ceil_div(p.M, 32)), dim3(256), L::lds, s, p);
+    return hipGetLastError();
+}
+
+template <bool PLANES>
 hipError_t launch_low(const AdapterProduct& p, hipStream_t s) {
-    if (p.r <= 32) return launch_tile<Tile<64, 32, 2, 1, 8>, false, OUT>(p, s);
-    if (p.r <= 64) return launch_tile<Tile<64, 64, 2, 2, 6>, false, OUT>(p, s);
-    return launch_tile<Tile<64, 128, 2, 2, 5>, false, OUT>(p, s);
+    return p.r <= 32 ? launch_low_tile<Low<2, 6>, PLANES>(p, s) : launch_low_tile<Low<4, 4>, PLANES>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s) { return fp8 ? launch_y<true>(p, s) : launch_y<false>(p, s); }
-hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return launch_low<kOutT>(p, s); }
-hipError_t launch_adapters_planes(const AdapterProduct& p, hipStream_t s) { return launch_low<kOutPlanes>(p, s); }
+hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return launch_low<false>(p, s); }
+hipError_t launch_adapters_planes(const AdapterProduct& p, hipStream_t s) { return launch_low<true>(p, s); }
 
 }  // namespace abt
