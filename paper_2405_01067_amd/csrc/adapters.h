@@ -28,10 +28,10 @@ hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s);
 hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s);         // X absent, Q = r <= 128
 hipError_t launch_adapters_planes(const AdapterProduct& p, hipStream_t s);    // the same
 
-// Few rows
-constexpr int kAdapterFewRows = 64, kAdapterFewT = 128;
-hipError_t launch_adapters_few_y(const AdapterProduct& p, bool fp8, hipStream_t s);       // M <= kAdapterFewRows
-hipError_t launch_adapters_few_t(const AdapterProduct& p, hipStream_t s);                 // M <= kAdapterFewT
+// Few rows: T (p.T, p.Tb, either may be NULL but for Tb = p.E) from X [M, n] and B, and Y, together.  sums: adapters_few_sums_bytes.
+constexpr int kAdapterFewRows = 128;
+size_t adapters_few_sums_bytes(int64_t M, int m, int n);
+hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s);
 
 // What the backward prepares in one launch: W^T, the transposes of every adapter's A and B, the rows of each adapter one after the other in
 // `order` (rows ascending) with offsets[count + 1], and 256 bytes of zeros.

@@ -45,18 +45,19 @@ __device__ __forceinline__ int rank_of(const AdapterProduct& g, int a) {
 }
 
 // ------------------------------------------------------------------------------------------ Y
-// WM x WN waves, each RB x CB blocks of 32 x 32
-template <int TM_, int TN_, int WM_, int WN_, int NS_>
+// WM x WN waves, each RB x CB blocks of 32 x 32.  X's parts of slabs are requested LX slabs ahead, W's LW ahead (they come from L2): at most LX.
+template <int TM_, int TN_, int WM_, int WN_, int LX_, int LW_>
 struct Tile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NS = NS_, NW = WM * WN;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, LX = LX_, LW = LW_, NW = WM * WN;
     static constexpr int RB = TM / (32 * WM), CB = TN / (32 * WN);
-    static constexpr int xpart = TM * 128, slab = (TM + TN) * 128;
+    static constexpr int xpart = TM * 128, wpart = TN * 128, wbase = (LX + 1) * xpart, ring = wbase + (LW + 1) * wpart;
     static constexpr int NX = TM / 8 / NW, NF = TN / 8 / NW, NL = NX + NF;       // load instructions per wave and slab: eight rows each
     static constexpr int opitch = TN * 2 + 16;
     static constexpr int out = TM * opitch;
-    static constexpr int lds = out > NS * slab ? out : NS * slab;
+    static constexpr int lds = out > ring ? out : ring;
+    static constexpr int behind = (LX - 1) * NX + (LW - 1) * NF + (LX > LW ? NX : 0);       // loads issued after the last one of a slab
     static_assert(NX * 8 * NW == TM && NF * 8 * NW == TN && RB * 32 * WM == TM && CB * 32 * WN == TN, "");
-    static_assert(NW % 2 == 0 && (NS - 2) * NL < 64 && lds <= 160 * 1024, "");
+    static_assert(NW % 2 == 0 && LW >= 1 && (LX == LW || LX == LW + 1) && behind < 64 && lds <= 160 * 1024, "");
 };
 
 struct Order { int row_tiles, col_tiles; };
@@ -74,7 +75,7 @@ __device__ __forceinline__ void tile_of(const Order& o, int& rt, int& ct) {
 
 template <class L, bool F8>
 __global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterProduct g, const Order order) {
-    constexpr int RB = L::RB, CB = L::CB, NW = L::NW, NS = L::NS;
+    constexpr int RB = L::RB, CB = L::CB, NW = L::NW;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5;
@@ -93,20 +94,27 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterPro
     const int bytes = g.kmain * (F8 ? 1 : 2), nmain = (bytes + 127) / 128;
     const rsrc_t xres = make_rsrc((const char*)g.X + row0 * bytes, (int64_t)rows * bytes);
     const rsrc_t wres = make_rsrc((const char*)g.W + (int64_t)col0 * bytes, (int64_t)cols * bytes);
-    int issue_slot = 0, issued = 0;
-    auto issue = [&]() {
-        unsigned char* const dst = lds + issue_slot + wave * 1024;
-        issue_slot = issue_slot == (NS - 1) * L::slab ? 0 : issue_slot + L::slab;
-        const int at = issued * 128 + chunk;
-        ++issued;
-        const int off = at < bytes ? lrow * bytes + at : kBufNowhere;
-        const int step = at < bytes ? 8 * NW * bytes : 0;
+    int xslot = 0, wslot = L::wbase;                      // of the next parts to be requested
+    auto offset = [&](int s) { return s * 128 + chunk < bytes ? lrow * bytes + s * 128 + chunk : kBufNowhere; };
+    auto issue_x = [&](int s) {
+        unsigned char* const dst = lds + xslot + wave * 1024;
+        xslot = xslot == L::LX * L::xpart ? 0 : xslot + L::xpart;
+        const int off = offset(s), step = off == kBufNowhere ? 0 : 8 * NW * bytes;
 #pragma unroll
         for (int j = 0; j < L::NX; ++j) load_lds16(xres, dst + j * (NW * 1024), off + j * step, 0);
-#pragma unroll
-        for (int j = 0; j < L::NF; ++j) load_lds16(wres, dst + L::xpart + j * (NW * 1024), off + j * step, 0);
     };
-    while (issued < NS - 1 && issued < nmain) issue();
+    auto issue_w = [&](int s) {
+        unsigned char* const dst = lds + wslot + wave * 1024;
+        wslot = wslot == L::wbase + L::LW * L::wpart ? L::wbase : wslot + L::wpart;
+        const int off = offset(s), step = off == kBufNowhere ? 0 : 8 * NW * bytes;
+#pragma unroll
+        for (int j = 0; j < L::NF; ++j) load_lds16(wres, dst + j * (NW * 1024), off + j * step, 0);
+    };
+#pragma unroll
+    for (int s = 0; s < L::LX; ++s) {                     // in the order of the loop below
+        if (s >= L::LX - L::LW && s - L::LX + L::LW < nmain) issue_w(s - L::LX + L::LW);
+        if (s < nmain) issue_x(s);
+    }
 
     // the adapters of this lane's rows
     int mine[RB];
@@ -126,11 +134,12 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterPro
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
     const int frow = out_row(lj);
     const int xsw = (lj >> 1) & 7, fsw = (frow >> 1) & 7;
-    const int xbase = (wr * RB * 32 + lj) * 128, fbase = L::xpart + (wc * CB * 32 + frow) * 128;
+    const int xbase = (wr * RB * 32 + lj) * 128, fbase = (wc * CB * 32 + frow) * 128;
     struct Ops { u32x4 x[RB], f[CB]; };
-    auto read = [&](Ops& o, int slot, int j) {            // chunk 2 j + lh of this lane's rows
-        const unsigned char* const x = lds + slot + xbase + (((2 * j + lh) ^ xsw) * 16);
-        const unsigned char* const f = lds + slot + fbase + (((2 * j + lh) ^ fsw) * 16);
+    int xat = 0, wat = L::wbase;                          // the slab that is read
+    auto read = [&](Ops& o, int j) {                      // chunk 2 j + lh of this lane's rows
+        const unsigned char* const x = lds + xat + xbase + (((2 * j + lh) ^ xsw) * 16);
+        const unsigned char* const f = lds + wat + fbase + (((2 * j + lh) ^ fsw) * 16);
 #pragma unroll
         for (int b = 0; b < CB; ++b) o.f[b] = *reinterpret_cast<const u32x4*>(f + b * 4096);
 #pragma unroll
@@ -148,31 +157,31 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterPro
 #pragma unroll
             for (int b = 0; b < CB; ++b) acc[a][b] = mfma_f8(o.f[b], p.f[b], o.x[a], p.x[a], acc[a][b]);
     };
-    int done = 0, slot = 0;                               // slabs consumed, the slot of the next
-    // Slab `done` has landed: loads come back in the order of issue, and NS - 2 slabs at most were requested after it.
-    auto next_slab = [&]() {
-        const int behind = issued - done - 1;
-        if (behind >= NS - 2) wait_newest<(NS - 2) * L::NL>();
-        else if (NS > 3 && behind == NS - 3) wait_newest<(NS > 3 ? NS - 3 : 0) * L::NL>();
-        else wait_newest<0>();
+    // Slab s has landed: loads come back in the order of issue.
+    auto slab = [&](int s) {
+        if (s + L::LX > nmain) wait_newest<0>();
+        else wait_newest<L::behind>();
         lds_barrier();
-        if (issued < nmain) issue();                      // into the slot whose reads ended before this barrier
-        const int at = slot;
-        slot = slot == (NS - 1) * L::slab ? 0 : slot + L::slab;
-        ++done;
-        return at;
+        // into the slots whose reads ended before this barrier
+        if (s + L::LW < nmain) issue_w(s + L::LW);
+        if (s + L::LX < nmain) issue_x(s + L::LX);
+    };
+    auto next = [&]() {
+        xat = xat == L::LX * L::xpart ? 0 : xat + L::xpart;
+        wat = wat == L::wbase + L::LW * L::wpart ? L::wbase : wat + L::wpart;
     };
     Ops o[2];
     if constexpr (F8) {
         for (int s = 0; s < nmain; ++s) {
-            const int at = next_slab();
+            slab(s);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                read(o[0], at, 2 * j);
-                read(o[1], at, 2 * j + 1);
+                read(o[0], 2 * j);
+                read(o[1], 2 * j + 1);
                 mma8(o[0], o[1]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            next();
         }
         // the dense product's scales
         float xs[RB];
@@ -205,14 +214,15 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterPro
 #pragma unroll
         for (int b = 0; b < CB; ++b) o[1].f[b] = u32x4{0, 0, 0, 0};
         for (int s = 0; s < nmain; ++s) {
-            const int at = next_slab();
+            slab(s);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                read(o[j & 1], at, j);
+                read(o[j & 1], j);
                 __builtin_amdgcn_sched_barrier(0);
                 mma(o[(j + 1) & 1]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            next();
         }
         mma(o[1]);
     }
@@ -289,9 +299,9 @@ hipError_t launch_tile(const AdapterProduct& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-using T256 = Tile<256, 256, 2, 4, 2>;
-using T128 = Tile<128, 128, 2, 2, 4>;
-using T64 = Tile<64, 64, 2, 2, 6>;
+using T256 = Tile<256, 256, 2, 4, 1, 1>;
+using T128 = Tile<128, 128, 2, 2, 3, 3>;
+using T64 = Tile<64, 64, 2, 2, 5, 5>;
 
 template <bool F8>
 hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {

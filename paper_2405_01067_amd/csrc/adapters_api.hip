@@ -31,21 +31,26 @@ AdapterProduct product(const abt_adapters* ad, const int32_t* row_adapter, int64
     return p;
 }
 
+size_t t_bytes(int64_t M, int64_t r) { return align_up((size_t)M * (size_t)r * 2, 256); }
+
 // T = X B^T; Tb: scaled and rounded, T: as it is, either may be NULL
 hipError_t make_t(const abt_adapters* ad, const int32_t* row_adapter, const void* X, float* T, uint16_t* Tb, int64_t M, int64_t n, hipStream_t s) {
     AdapterProduct p = product(ad, row_adapter, M);
     p.E = (const uint16_t*)X; p.F = (const uint16_t*)ad->B; p.Q = ad->r; p.ke = (int)n; p.e_pitch = (int)n; p.T = T; p.Tb = Tb;
-    return M <= kAdapterFewT ? launch_adapters_few_t(p, s) : launch_adapters_t(p, s);
+    return launch_adapters_t(p, s);
 }
 
 int adapters_fwd(const void* X, const void* main, const float* x_scale, const void* W, const float* w_scale, const abt_adapters* ad, const int32_t* row_adapter,
                  void* Y, float* T, int64_t M, int64_t m, int64_t n, bool fp8, void* ws, hipStream_t s) {
     uint16_t* const Tb = (uint16_t*)ws;
-    if (make_t(ad, row_adapter, X, T, Tb, M, n, s) != hipSuccess) return ABT_EHIP;
+    const bool few = M <= kAdapterFewRows;
+    if (!few && make_t(ad, row_adapter, X, T, Tb, M, n, s) != hipSuccess) return ABT_EHIP;
     AdapterProduct p = product(ad, row_adapter, M);
     p.X = main; p.W = W; p.x_scale = x_scale; p.w_scale = w_scale;
     p.E = Tb; p.F = (const uint16_t*)ad->A; p.Q = (int)m; p.kmain = (int)n; p.ke = ad->r; p.e_pitch = ad->r; p.Y = (uint16_t*)Y;
-    const hipError_t e = M <= kAdapterFewRows ? launch_adapters_few_y(p, fp8, s) : launch_adapters_y(p, fp8, s);
+    if (few) { p.T = T; p.Tb = Tb; }
+    const hipError_t e = few ? launch_adapters_few(p, (const uint16_t*)X, (const uint16_t*)ad->B, (float*)((char*)ws + t_bytes(M, ad->r)), fp8, s)
+                             : launch_adapters_y(p, fp8, s);
     return e == hipSuccess ? ABT_OK : ABT_EHIP;
 }
 
@@ -97,7 +102,7 @@ extern "C" {
 size_t lr_adapters_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n, int64_t r, int64_t count) {
     if (M < 1 || M > INT_MAX || m < 1 || m > kMaxWidth || m % 8 || n < 1 || n > kMaxWidth || n % 8 || r < 8 || r > ABT_ADAPTERS_MAX_RANK || r % 8 || count < 1 || count > 65535)
         return 0;
-    return align_up((size_t)M * (size_t)r * 2, 256);
+    return t_bytes(M, r) + (M <= kAdapterFewRows ? align_up(adapters_few_sums_bytes(M, (int)m, (int)n), 256) : 0);
 }
 
 int lr_adapters_fwd(const void* X, const void* W, const abt_adapters* adapters, const int32_t* row_adapter, void* Y, float* T_save,

@@ -1,10 +1,11 @@
 // The layer with adapters for a few rows, as single tokens of many requests are: T_i = B_a x_i, then Y_i = W x_i + A_a T_i.
-// Nothing is reused but the rows themselves, so the operands go from memory to registers: bound by the bytes of W and of the adapters in use, and
-// by the latency of two launches where these are few.
-//   T: a work-group per row and eight of its rank's rows of B, two rows a wave; lanes share out the columns.
-//   Y: a work-group per 16 columns; eight waves share out the contraction (128 bytes of every row at a time) and the adapters, and their
-//      sums are added through LDS in order.
-#include <climits>
+// Little is reused, so the operands go from memory to registers.  Two launches:
+//   first    T beside the dense product.  T: a work-group per row and sixteen of its rank's rows of B, two rows a wave.  The dense product: 64 columns, up to
+//            64 rows and a part of the contraction, which eight waves share out, 128 bytes of every row at a time; with 16 columns and the whole
+//            contraction per work-group the rows of X, read by every work-group, were several times the bytes of W.
+//   second   adds the parts in order, and the adapters: 16 columns a work-group, eight waves that share out the adapters of the rows.
+// Bound by the bytes of W and of the adapters in use, and by the latency of two launches where these are few.
+#include <type_traits>
 
 #include "adapters.h"
 
@@ -24,42 +25,55 @@ __device__ __forceinline__ f32x4 mfma16_f8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b
 __device__ __forceinline__ float lo(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
 __device__ __forceinline__ float hi(uint32_t v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
 
+// the first `valid` of eight bf16 values, zeros behind them (all of them from eight on, none below one)
 __device__ __forceinline__ u32x4 first_of(u32x4 v, int valid) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] &= valid >= 2 * i + 2 ? 0xffffffffu : valid == 2 * i + 1 ? 0xffffu : 0u;
     return v;
 }
 
-__global__ __launch_bounds__(256) void few_t_kernel(const AdapterProduct g) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x;
-    const int n = g.ke;
-    int a = __builtin_amdgcn_readfirstlane(gload(g.row_adapter + row));
+// T of one row: rows j0, j0 + 1 of its adapter's B by each wave
+__device__ __forceinline__ void t_of_row(const AdapterProduct& g, const uint16_t* X, const uint16_t* B, int n, int64_t row, int j0) {
+    const int lane = threadIdx.x & 63;
+    if (j0 >= g.r) return;
+    const int a = __builtin_amdgcn_readfirstlane(gload(g.row_adapter + row));
     const bool have = a >= 0 && a < g.count;
-    const int rank0 = have ? (g.ranks ? __builtin_amdgcn_readfirstlane(gload(g.ranks + a)) : g.r) : 0;
-    const int rank = rank0 > g.r ? g.r : rank0;
-    const int j0 = (int)blockIdx.y * 8 + 2 * wave;        // two rows of B; r is a multiple of 8
     float sum[2] = {0.0f, 0.0f};
-    if (j0 < rank) {
-        const uint16_t* const x = g.E + row * g.e_pitch;
-        const uint16_t* const b = g.F + ((int64_t)a * g.r + j0) * n;
-#pragma unroll 4
-        for (int c = lane * 8; c < n; c += 512) {
-            const u32x4 xv = gload(reinterpret_cast<const u32x4*>(x + c)), b0 = gload(reinterpret_cast<const u32x4*>(b + c)),
-                        b1 = gload(reinterpret_cast<const u32x4*>(b + n + c));
+    int rank = 0;
+    if (have) {
+        // (rows past the rank are there: they are read beside the rank and not used)
+        const int k = g.ranks ? gload(g.ranks + a) : g.r;
+        const uint16_t* const x = X + row * n;
+        const uint16_t* const b = B + ((int64_t)a * g.r + j0) * n;
+        float other[2] = {0.0f, 0.0f};
+        const auto add = [&](u32x4 xv, u32x4 b0, u32x4 b1) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 sum[0] += lo(xv[i]) * lo(b0[i]);
-                sum[0] += hi(xv[i]) * hi(b0[i]);
+                other[0] += hi(xv[i]) * hi(b0[i]);
                 sum[1] += lo(xv[i]) * lo(b1[i]);
-                sum[1] += hi(xv[i]) * hi(b1[i]);
+                other[1] += hi(xv[i]) * hi(b1[i]);
             }
+        };
+        const auto at = [&](const uint16_t* p, int c) { return gload(reinterpret_cast<const u32x4*>(p + c)); };
+        int c = lane * 8;
+        for (; c + 1536 < n; c += 2048) {                 // four pieces on their way at a time
+            u32x4 v[4][3];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i][0] = at(x, c + 512 * i); v[i][1] = at(b, c + 512 * i); v[i][2] = at(b + n, c + 512 * i); }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add(v[i][0], v[i][1], v[i][2]);
         }
+        for (; c < n; c += 512) add(at(x, c), at(b, c), at(b + n, c));
+        sum[0] += other[0];
+        sum[1] += other[1];
 #pragma unroll
         for (int d = 32; d; d >>= 1) {
             sum[0] += __shfl_xor(sum[0], d);
             sum[1] += __shfl_xor(sum[1], d);
         }
+        rank = k > g.r ? g.r : k;
+        if (j0 >= rank) sum[0] = 0.0f;
         if (j0 + 1 >= rank) sum[1] = 0.0f;
     }
     if (lane) return;
@@ -72,123 +86,207 @@ __global__ __launch_bounds__(256) void few_t_kernel(const AdapterProduct g) {
     if (g.Tb) gstore(reinterpret_cast<uint32_t*>(g.Tb + row * g.r + j0), pack2_bf16(j0 < rank ? s * sum[0] : 0.0f, j0 + 1 < rank ? s * sum[1] : 0.0f));
 }
 
+struct FewParts { int col_blocks, row_groups, splits, units; float* sums; const uint16_t* X; const uint16_t* B; };   // X as the adapters see it
+
 // RB blocks of 16 rows
 template <int RB, bool F8>
-__global__ __launch_bounds__(512) void few_y_kernel(const AdapterProduct g) {
-    __shared__ __align__(16) f32x4 sums[8 * RB * 64];
+__global__ __launch_bounds__(512) void few_first_kernel(const AdapterProduct g, const FewParts f) {
+    constexpr int CB = 4;
+    __shared__ __align__(16) f32x4 sums[4 * RB * CB * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nbase = f.col_blocks * f.row_groups * f.splits;
+    int w = blockIdx.x;
+    if (w >= nbase) {
+        w -= nbase;
+        const int per = (g.r + 15) / 16;
+        t_of_row(g, f.X, f.B, g.kmain, w / per, (w % per) * 16 + 2 * wave);
+        return;
+    }
+    const int cb = w % f.col_blocks;
+    w /= f.col_blocks;
+    const int split = w % f.splits, row0 = w / f.splits * 64;
     const int li = lane & 15, lq = lane >> 4;
-    const int M = (int)g.M, col0 = blockIdx.x * 16;
-    const int bytes = g.kmain * (F8 ? 1 : 2), units = (bytes + 127) / 128;
+    const int rows = (int)g.M - row0 < 64 ? (int)g.M - row0 : 64, col0 = cb * 64;
+    const int cols = g.Q - col0 < 64 ? g.Q - col0 : 64;
+    const int bytes = g.kmain * (F8 ? 1 : 2);
     // a unit is 128 bytes of every row; lanes past the last row, column or byte read zeros
-    const rsrc_t xres = make_rsrc(g.X, (int64_t)M * bytes);
-    const int wrows = g.Q - col0 < 16 ? g.Q - col0 : 16;
-    const rsrc_t wres = make_rsrc((const char*)g.W + (int64_t)col0 * bytes, (int64_t)wrows * bytes);
-    f32x4 acc[RB];
+    const rsrc_t xres = make_rsrc((const char*)g.X + (int64_t)row0 * bytes, (int64_t)rows * bytes);
+    const rsrc_t wres = make_rsrc((const char*)g.W + (int64_t)col0 * bytes, (int64_t)cols * bytes);
+    f32x4 acc[RB][CB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) acc[b] = f32x4{0, 0, 0, 0};
-    auto unit = [&](int u) {
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) acc[b][c] = f32x4{0, 0, 0, 0};
+    const int end = (split + 1) * f.units;
+    for (int u = split * f.units + wave; u < end; u += 8) {
         const int at0 = u * 128 + lq * 16, at1 = at0 + 64;
-        const u32x4 w0 = buf_load16(wres, at0 < bytes ? li * bytes + at0 : kBufNowhere, 0);
-        const u32x4 w1 = buf_load16(wres, at1 < bytes ? li * bytes + at1 : kBufNowhere, 0);
-        u32x4 x0[RB], x1[RB];
+        u32x4 w0[CB], w1[CB], x0[RB], x1[RB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            w0[c] = buf_load16(wres, at0 < bytes ? (16 * c + li) * bytes + at0 : kBufNowhere, 0);
+            w1[c] = buf_load16(wres, at1 < bytes ? (16 * c + li) * bytes + at1 : kBufNowhere, 0);
+        }
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             x0[b] = buf_load16(xres, at0 < bytes ? (16 * b + li) * bytes + at0 : kBufNowhere, 0);
             x1[b] = buf_load16(xres, at1 < bytes ? (16 * b + li) * bytes + at1 : kBufNowhere, 0);
         }
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            if constexpr (F8) {
-                acc[b] = mfma16_f8(w0, w1, x0[b], x1[b], acc[b]);
-            } else {
-                acc[b] = mfma16(w0, x0[b], acc[b]);
-                acc[b] = mfma16(w1, x1[b], acc[b]);
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                if constexpr (F8) {
+                    acc[b][c] = mfma16_f8(w0[c], w1[c], x0[b], x1[b], acc[b][c]);
+                } else {
+                    acc[b][c] = mfma16(w0[c], x0[b], acc[b][c]);
+                    acc[b][c] = mfma16(w1[c], x1[b], acc[b][c]);
+                }
             }
-        }
-    };
-    int u = wave;
-    for (; u + 24 < units; u += 32) {                     // four at a time, their loads together
-        unit(u);
-        unit(u + 8);
-        unit(u + 16);
-        unit(u + 24);
     }
-    for (; u < units; u += 8) unit(u);
-    if constexpr (F8) {
-        float ws[4];
+    // the waves' sums: those of waves w and w + 4 first, then the four in order
+    auto at = [&](int who, int t) -> f32x4& { return sums[(who * RB * CB + t) * 64 + lane]; };
+    if (wave >= 4)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ws[i] = 4 * lq + i < wrows ? gload(g.w_scale + col0 + 4 * lq + i) : 0.0f;
+        for (int t = 0; t < RB * CB; ++t) at(wave - 4, t) = acc[t / CB][t % CB];
+    __syncthreads();
+    if (wave < 4)
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            const float xs = 16 * b + li < M ? gload(g.x_scale + 16 * b + li) : 0.0f;
+        for (int t = 0; t < RB * CB; ++t) at(wave, t) = acc[t / CB][t % CB] + at(wave, t);
+    __syncthreads();
+    float* const out = f.sums + (int64_t)split * g.M * g.Q;
+    for (int t = wave; t < RB * CB; t += 8) {
+        const f32x4 v = (at(0, t) + at(1, t)) + (at(2, t) + at(3, t));
+        const int row = 16 * (t / CB) + li, c = 16 * (t % CB) + 4 * lq;      // lane: row li of the block, four columns
+        if (row < rows && c < cols) gstore(reinterpret_cast<f32x4*>(out + (int64_t)(row0 + row) * g.Q + col0 + c), v);
+    }
+}
+
+template <int RB, bool F8>
+__global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g, const FewParts f) {
+    __shared__ __align__(16) f32x4 sums[8 * RB * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 15, lq = lane >> 4;
+    const int row0 = blockIdx.y * 64, rows = (int)g.M - row0 < 64 ? (int)g.M - row0 : 64;
+    const int col0 = blockIdx.x * 16, cols = g.Q - col0 < 16 ? g.Q - col0 : 16;
+    const int id0 = gload(g.row_adapter + row0 + (lane < rows ? lane : 0));
+    // the dense product of this lane's row and four columns, by the waves that finish a block of rows
+    const int row = 16 * wave + li, c0 = 4 * lq;
+    const bool out = wave < RB && row < rows && c0 < cols;
+    f32x4 v = {0, 0, 0, 0};
+    float xs = 1.0f, ws[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (out) {
+        const float* const from = f.sums + (int64_t)(row0 + row) * g.Q + col0 + c0;
+        const int64_t step = g.M * g.Q;
+        for (int s = 0; s < f.splits; ++s) v += gload(reinterpret_cast<const f32x4*>(from + s * step));
+        if constexpr (F8) {
+            xs = gload(g.x_scale + row0 + row);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[b][i] *= xs * ws[i];
+            for (int i = 0; i < 4; ++i) ws[i] = gload(g.w_scale + col0 + c0 + i);
         }
     }
-    // the adapters of the rows, every eighth of those that occur
-    int ids = lane < M ? gload(g.row_adapter + lane) : -1;
-    if (ids >= g.count) ids = -1;
-    int mine[RB];
+    f32x4 acc[RB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) mine[b] = 16 * b + li < M ? gload(g.row_adapter + 16 * b + li) : -1;
-    const rsrc_t eres = make_rsrc(g.E, (int64_t)M * g.r * 2);
-    int a = -1;
-    for (int k = 0;; ++k) {
-        int best = ids > a ? ids : INT_MAX;
+    for (int b = 0; b < RB; ++b) acc[b] = f32x4{0, 0, 0, 0};
+    // The adapters of the rows in the order in which they occur, every eighth of them by this wave, four at a time with their loads together.
+    const int id = lane < rows && id0 >= 0 && id0 < g.count ? id0 : -1;
+    const int rank0 = g.ranks && id >= 0 ? gload(g.ranks + id) : g.r;
+    const rsrc_t eres = make_rsrc(g.E + (int64_t)row0 * g.r, (int64_t)rows * g.r * 2);
+    uint64_t left = __ballot(id >= 0);
+    for (int k = 0; left;) {
+        uint64_t of[4] = {0, 0, 0, 0};             // its rows
+        rsrc_t fres[4];
+        int who[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            const int o = __shfl_xor(best, d);
-            best = o < best ? o : best;
+        for (int q = 0; q < 4; ++q) {
+            int a = 0;
+            while (left && !of[q]) {
+                const int first = __builtin_ctzll(left);
+                a = __builtin_amdgcn_readlane(id, first);
+                const uint64_t same = __ballot(id == a);
+                left &= ~same;
+                if ((k++ & 7) == wave) { of[q] = same; who[q] = first; }
+            }
+            fres[q] = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * g.r, of[q] ? (int64_t)cols * g.r * 2 : 0);
         }
-        a = __builtin_amdgcn_readfirstlane(best);
-        if (a == INT_MAX) break;
-        if ((k & 7) != wave) continue;
-        int rank = g.ranks ? __builtin_amdgcn_readfirstlane(gload(g.ranks + a)) : g.r;
-        rank = rank > g.r ? g.r : rank;
-        const rsrc_t fres = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * g.r, (int64_t)wrows * g.r * 2);
-        for (int j = 0; j < rank; j += 32) {
+        if (!of[0]) break;
+        for (int j = 0; j < g.r; j += 32) {
             const int c = j + lq * 8;
-            u32x4 f = buf_load16(fres, c < rank ? (li * g.r + c) * 2 : kBufNowhere, 0);
-            u32x4 t[RB];
+            u32x4 f[4], t[4][RB];
 #pragma unroll
-            for (int b = 0; b < RB; ++b) t[b] = buf_load16(eres, c < rank && mine[b] == a ? ((16 * b + li) * g.r + c) * 2 : kBufNowhere, 0);
-            if (rank - j < 32 && (rank & 7)) f = first_of(f, rank - c);            // (T is zero there)
+            for (int q = 0; q < 4; ++q) {                 // (columns past the rank are there: they are read beside it and masked)
+                f[q] = buf_load16(fres[q], c < g.r ? (li * g.r + c) * 2 : kBufNowhere, 0);
 #pragma unroll
-            for (int b = 0; b < RB; ++b) acc[b] = mfma16(f, t[b], acc[b]);
+                for (int b = 0; b < RB; ++b)
+                    t[q][b] = buf_load16(eres, c < g.r && ((of[q] >> (16 * b + li)) & 1) ? ((16 * b + li) * g.r + c) * 2 : kBufNowhere, 0);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (!of[q]) break;
+                const int rank = __builtin_amdgcn_readlane(rank0, who[q]);
+                if (rank - j < 32) f[q] = first_of(f[q], rank - c);            // (T is zero there)
+#pragma unroll
+                for (int b = 0; b < RB; ++b) acc[b] = mfma16(f[q], t[q][b], acc[b]);
+            }
         }
     }
     // lane: row 16 b + li, columns 4 lq .. + 3
 #pragma unroll
     for (int b = 0; b < RB; ++b) sums[(wave * RB + b) * 64 + lane] = acc[b];
     __syncthreads();
-    if (wave >= RB) return;
-    f32x4 v = sums[wave * 64 + lane];
+    if (!out) return;
 #pragma unroll
-    for (int w = 1; w < 8; ++w) v += sums[(w * RB + wave) * 64 + lane];
-    const int row = 16 * wave + li, c = 4 * lq;
-    if (row < M && c < wrows) gstore(reinterpret_cast<u32x2*>(g.Y + (int64_t)row * g.Q + col0 + c), u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])});
+    for (int i = 0; i < 4; ++i) v[i] *= xs * ws[i];
+    f32x4 low = sums[wave * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) low += sums[(w * RB + wave) * 64 + lane];
+    v += low;
+    gstore(reinterpret_cast<u32x2*>(g.Y + (int64_t)(row0 + row) * g.Q + col0 + c0), u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])});
+}
+
+FewParts few_parts(int64_t M, int Q, int n, bool fp8) {
+    FewParts f{};
+    f.col_blocks = (Q + 63) / 64;
+    f.row_groups = (int)((M + 63) / 64);
+    const int units = (n * (fp8 ? 1 : 2) + 127) / 128;
+    // one work-group per compute unit, but for each of its eight waves at least one unit
+    int splits = 256 / (f.col_blocks * f.row_groups);
+    const int most = (units + 7) / 8;
+    splits = splits > most ? most : splits;
+    splits = splits < 1 ? 1 : splits;
+    f.units = (units + splits - 1) / splits;
+    f.splits = (units + f.units - 1) / f.units;
+    return f;
 }
 
 template <bool F8>
-hipError_t few_y(const AdapterProduct& p, hipStream_t s) {
-    const dim3 grid((unsigned)ceil_div(p.Q, 16));
-    if (p.M <= 16) hipLaunchKernelGGL((few_y_kernel<1, F8>), grid, dim3(512), 0, s, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((few_y_kernel<2, F8>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((few_y_kernel<4, F8>), grid, dim3(512), 0, s, p);
-    return hipGetLastError();
+hipError_t few(const AdapterProduct& p, const FewParts& f, hipStream_t s) {
+    const dim3 first((unsigned)(f.col_blocks * f.row_groups * f.splits + p.M * ((p.r + 15) / 16))), second((unsigned)ceil_div(p.Q, 16), (unsigned)f.row_groups);
+    const auto launch = [&](auto rb) {
+        constexpr int RB = decltype(rb)::value;
+        hipLaunchKernelGGL((few_first_kernel<RB, F8>), first, dim3(512), 0, s, p, f);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((few_second_kernel<RB, F8>), second, dim3(512), 0, s, p, f);
+        return hipGetLastError();
+    };
+    if (p.M <= 16) return launch(std::integral_constant<int, 1>{});
+    if (p.M <= 32) return launch(std::integral_constant<int, 2>{});
+    if (p.M <= 48) return launch(std::integral_constant<int, 3>{});
+    return launch(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
 
-hipError_t launch_adapters_few_t(const AdapterProduct& p, hipStream_t s) {
-    if (p.M > kAdapterFewT) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(few_t_kernel, dim3((unsigned)p.M, (unsigned)ceil_div(p.r, 8)), dim3(256), 0, s, p);
-    return hipGetLastError();
+size_t adapters_few_sums_bytes(int64_t M, int m, int n) {
+    const int s8 = few_parts(M, m, n, true).splits, s16 = few_parts(M, m, n, false).splits;
+    return (size_t)(s8 > s16 ? s8 : s16) * (size_t)M * (size_t)m * 4;
 }
-hipError_t launch_adapters_few_y(const AdapterProduct& p, bool fp8, hipStream_t s) {
-    if (p.M > kAdapterFewRows || p.e_pitch != p.r) return hipErrorInvalidValue;
-    return fp8 ? few_y<true>(p, s) : few_y<false>(p, s);
+
+hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s) {
+    if (p.M > kAdapterFewRows || p.e_pitch != p.r || p.ke != p.r) return hipErrorInvalidValue;
+    FewParts f = few_parts(p.M, p.Q, p.kmain, fp8);
+    f.sums = sums; f.X = X; f.B = B;
+    return fp8 ? few<true>(p, f, s) : few<false>(p, f, s);
 }
 
 }  // namespace abt

@@ -187,11 +187,21 @@ __device__ void list_rows(const AdapterPrep& p, int a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t each = (p.M + 1023) / 1024 * 64;       // whole waves of rows
     const int64_t r0 = wave * each, r1 = r0 + each < p.M ? r0 + each : p.M;
-    int m = 0, b = 0;
-    for (int64_t r = r0 + lane; r < r1; r += 64) {
-        const int id = gload(p.row_adapter + r);
-        m += id == a;
-        b += id >= 0 && id < a;
+    // sixteen loads on their way at a time; ids past the wave's rows count as no adapter
+    const auto ids_of = [&](int64_t r, int (&id)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) id[i] = gload(p.row_adapter + (r + 64 * i + lane < r1 ? r + 64 * i + lane : 0));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) id[i] = r + 64 * i + lane < r1 ? id[i] : -1;
+    };
+    int m = 0, b = 0, id[16];
+    for (int64_t r = r0; r < r1; r += 1024) {
+        ids_of(r, id);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            m += id[i] == a;
+            b += id[i] >= 0 && id[i] < a;
+        }
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) {
@@ -211,11 +221,14 @@ __device__ void list_rows(const AdapterPrep& p, int a) {
         if (a == p.count - 1) gstore(p.offsets + a + 1, before + all);
     }
     at += before;
-    for (int64_t r = r0; r < r1; r += 64) {
-        const bool is = r + lane < r1 && gload(p.row_adapter + r + lane) == a;
-        const uint64_t who = __ballot(is);
-        if (is) gstore(p.order + at + __builtin_popcountll(who & ((1ull << lane) - 1)), (int)(r + lane));
-        at += __builtin_popcountll(who);
+    for (int64_t r = r0; r < r1; r += 1024) {
+        if (r1 - r0 > 1024) ids_of(r, id);                // (else they are still here)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t who = __ballot(id[i] == a);
+            if (id[i] == a) gstore(p.order + at + __builtin_popcountll(who & ((1ull << lane) - 1)), (int)(r + 64 * i + lane));
+            at += __builtin_popcountll(who);
+        }
     }
 }
 

@@ -207,8 +207,17 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* sums, in
     __shared__ float part[16][64];
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + l;
     float v = 0.0f;
-    if (c < n)
-        for (int b = w; b < rows; b += 16) v += gload(sums + (int64_t)b * n + c);
+    if (c < n) {
+        int b = w;
+        for (; b + 112 < rows; b += 128) {                // eight loads on their way at a time
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = gload(sums + (int64_t)(b + 16 * i) * n + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += x[i];
+        }
+        for (; b < rows; b += 16) v += gload(sums + (int64_t)b * n + c);
+    }
     part[w][l] = v;
     __syncthreads();
     if (w || c >= n) return;
