@@ -264,26 +264,38 @@ def _torch():
     return torch
 
 
-@functools.lru_cache(maxsize=None)
-def layer_call():
-    """The native code of lr_linear_fwd and lr_linear_bwd, or None (and a warning) where it is not there or was built for another
-    Python or torch: the Python code makes the same calls of the library, some 5 us later.  Needs no GPU."""
+def _native_calls(name, functions):
+    """lib/<name>.so, handed the addresses of the library's functions, or None (and a warning) where it is not there or was built for another Python
+    or torch: the Python code makes the same calls of the library, some 5 us later."""
     import importlib.machinery
     import importlib.util
     torch = _torch()
     lib = load()
-    path = os.path.join(os.path.dirname(_LIB_PATH), "layer_call.so")
+    path = os.path.join(os.path.dirname(_LIB_PATH), name + ".so")
     try:
-        loader = importlib.machinery.ExtensionFileLoader("layer_call", path)
-        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("layer_call", loader))
+        loader = importlib.machinery.ExtensionFileLoader(name, path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader(name, loader))
         loader.exec_module(module)
     except ImportError as e:
         import warnings
-        warnings.warn(f"{path} does not load ({e}): calls of a single layer go through Python; `python __graft_entry__.py` builds it", RuntimeWarning)
+        warnings.warn(f"{path} does not load ({e}): its calls go through Python; `python __graft_entry__.py` builds it", RuntimeWarning)
         return None
-    addr = (ctypes.cast(f, ctypes.c_void_p).value for f in (lib.lr_linear_fwd, lib.lr_linear_fwd_wants_T, lib.lr_linear_bwd, lib.lr_linear_bwd_workspace_bytes))
+    addr = (ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in functions)
     module.setup(*addr, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, _check)
     return module
+
+
+@functools.lru_cache(maxsize=None)
+def layer_call():
+    """The native code of lr_linear_fwd and lr_linear_bwd, or None.  Needs no GPU."""
+    return _native_calls("layer_call", ("lr_linear_fwd", "lr_linear_fwd_wants_T", "lr_linear_bwd", "lr_linear_bwd_workspace_bytes"))
+
+
+@functools.lru_cache(maxsize=None)
+def adapter_call():
+    """The native code of lr_adapters_fwd, lr_adapters_fwd_q8, lr_adapters_bwd, lr_rms_norm_fwd and lr_rms_norm_bwd, or None.  Needs no GPU."""
+    return _native_calls("adapter_call", ("lr_adapters_fwd", "lr_adapters_fwd_q8", "lr_adapters_fwd_workspace_bytes", "lr_adapters_bwd", "lr_adapters_bwd_workspace_bytes",
+                                          "lr_rms_norm_fwd", "lr_rms_norm_bwd", "lr_rms_norm_bwd_workspace_bytes"))
 
 
 def _dt(t):
@@ -838,6 +850,11 @@ def lr_adapters_fwd(X, W, A, B, row_adapter, ranks=None, scales=None, save_T: bo
     """Y_i = W x_i + scales[a] A[a] T_i with T_i = B[a] x_i and a = row_adapter[i] (-1: no adapter): a frozen W [m, n] and stacked
     adapters A [count, m, r], B [count, r, n] (bf16, GPU), row_adapter [M] int32, ranks [count] int32, scales [count] fp32.
     Returns (Y, T), T [M, r] fp32 for lr_adapters_bwd (None without save_T)."""
+    if Y is None and T is None and workspace is None:
+        native = adapter_call()
+        done = native.fwd(X, W, A, B, row_adapter, ranks, scales, save_T) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     bf16 = torch.bfloat16
@@ -866,6 +883,11 @@ def lr_adapters_fwd(X, W, A, B, row_adapter, ranks=None, scales=None, save_T: bo
 def lr_adapters_fwd_q8(X, Xq, x_scale, Wq, w_scale, A, B, row_adapter, ranks=None, scales=None, Y=None, workspace=None):
     """lr_adapters_fwd with the dense product from 8-bit floats: Xq [M, n] and Wq [m, n] (torch.float8_e4m3fn) with fp32 scales per
     row, x_scale [M] and w_scale [m], as lr_rms_norm_fwd writes them; the adapters see X (bf16).  Returns Y [M, m] bf16."""
+    if Y is None and workspace is None:
+        native = adapter_call()
+        done = native.fwd_q8(X, Xq, x_scale, Wq, w_scale, A, B, row_adapter, ranks, scales) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     if X.dim() != 2 or Wq.dim() != 2:
@@ -891,6 +913,11 @@ def lr_adapters_bwd(dY, X, T, W, A, B, row_adapter, ranks=None, scales=None, nee
                     need_dB: bool = True, dX=None, dA=None, dB=None, accumulate: bool = False, workspace=None):
     """Gradients of lr_adapters_fwd: dX [M, n] bf16, dA [count, m, r] and dB [count, r, n] fp32 (W is frozen).  T: what the forward
     returned, or None (computed again).  Returns (dX, dA, dB); skipped ones are None."""
+    if dX is None and dA is None and dB is None and not accumulate and workspace is None:
+        native = adapter_call()
+        done = native.bwd(dY, X, T, W, A, B, row_adapter, ranks, scales, need_dX, need_dA, need_dB) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     bf16, f32 = torch.bfloat16, torch.float32
@@ -924,6 +951,11 @@ def lr_rms_norm_fwd(X, gain, eps: float = 1e-6, residual=None, quantize: bool = 
     """H = X + residual, Y = gain H / sqrt(mean of H^2 over the columns + eps) for X [M, n] (bf16 or fp32), gain [n] fp32.
     Returns (Y, H, Yq, y_scale): H is X itself without a residual; with quantize, Y ~ y_scale[i] Yq in torch.float8_e4m3fn (None
     otherwise); Y is None without need_Y, which needs quantize."""
+    if need_Y and Y is None and H is None:
+        native = adapter_call()
+        done = native.norm_fwd(X, gain, eps, residual, quantize) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     if X.dim() != 2:
         raise AbtError("X must be [M, n]")
@@ -950,6 +982,11 @@ def lr_rms_norm_bwd(dY, H, gain, eps: float = 1e-6, dH=None, need_dX: bool = Tru
                     accumulate: bool = False, workspace=None):
     """Gradients of lr_rms_norm_fwd at its H: dX [M, n], which is also the residual's gradient (dH, the gradient that reaches H past the
     norm, is added), and dgain [n] fp32.  Returns (dX, dgain); skipped ones are None."""
+    if need_dX and need_dgain and dX is None and dgain is None and not accumulate and workspace is None:
+        native = adapter_call()
+        done = native.norm_bwd(dY, H, gain, eps, dH) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     if H.dim() != 2:
