@@ -26,31 +26,29 @@ inline __host__ __device__ int plane_columns(int r) { return r <= 16 ? 16 : r <=
 
 hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s);
 hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s);         // X absent, Q = r <= 128
-hipError_t launch_adapters_planes(const AdapterProduct& p, hipStream_t s);    // the same
 
 // Few rows: T (p.T, p.Tb, either may be NULL but for Tb = p.E) from X [M, n] and B, and Y, together.  sums: adapters_few_sums_bytes.
 constexpr int kAdapterFewRows = 128;
 size_t adapters_few_sums_bytes(int64_t M, int m, int n);
 hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s);
 
-// What the backward prepares in one launch: W^T, the transposes of every adapter's A and B, the rows of each adapter one after the other in
-// `order` (rows ascending) with offsets[count + 1], and 256 bytes of zeros.
+// What the backward prepares beside dT: W^T, the transposes of every adapter's B, the rows of each adapter one after the other in
+// `order` (rows ascending) with offsets[count + 1].
 struct AdapterPrep {
     const uint16_t* W; uint16_t* Wt;       // [m, n] -> [n, m]; NULL: not wanted
-    const uint16_t* A; uint16_t* At;       // [count, m, r] -> [count, r, m]
-    const uint16_t* B; uint16_t* Bt;       // [count, r, n] -> [count, n, r]
-    const int32_t* row_adapter; int32_t* order; int32_t* offsets;
-    unsigned char* zeros;
+    const uint16_t* B; uint16_t* Bt;       // [count, r, n] -> [count, n, r]; NULL: not wanted
+    const int32_t* row_adapter; int32_t* order; int32_t* offsets;     // order NULL: not wanted
     int64_t M;
     int m, n, r, count;
 };
-hipError_t launch_adapters_prep(const AdapterPrep& p, hipStream_t s);
+// E = dY [M, m], F = A [count, m, r], ke = m, and the planes
+hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream_t s);
 
 // dA[a] = sum of U_i V_i^T over the rows of adapter a, both sides in one launch, then their sums.
 struct AdapterGrads {
     const uint16_t* dY; const uint16_t* T_planes; float* dA;      // dA [count, m, r], NULL: not wanted
     const uint16_t* X; const uint16_t* dT_planes; float* dB;      // dB [count, r, n]
-    const int32_t* order; const int32_t* offsets; const unsigned char* zeros;
+    const int32_t* order; const int32_t* offsets;
     float* partials;
     int64_t M;
     int m, n, r, count, accumulate;
@@ -58,5 +56,8 @@ struct AdapterGrads {
 int adapters_grad_piece(int64_t M, int m, int n);      // rows of a piece
 size_t adapters_grad_partial_bytes(int64_t M, int m, int n, int r, int count);
 hipError_t launch_adapters_grads(const AdapterGrads& p, hipStream_t s);
+// Few rows: no partials, and dX (or NULL) in the same launch
+constexpr int kAdapterFewGradRows = 1024;
+hipError_t launch_adapters_dx_grads(const AdapterProduct* x, const AdapterGrads& p, hipStream_t s);
 
 }  // namespace abt

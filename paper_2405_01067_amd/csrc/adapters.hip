@@ -10,7 +10,7 @@
 #include <atomic>
 #include <climits>
 
-#include "adapters.h"
+#include "adapters_grad.h"
 
 namespace abt {
 namespace {
@@ -64,8 +64,8 @@ struct Order { int row_tiles, col_tiles; };
 
 // Tiles in panels of four row tiles, down the panel first; each XCD gets a contiguous eighth: the tiles that run at the same time on one
 // XCD share rows of X and rows of W in its L2.
-__device__ __forceinline__ void tile_of(const Order& o, int& rt, int& ct) {
-    const int nb = gridDim.x, xcd = blockIdx.x & 7, i = blockIdx.x >> 3, per = nb >> 3, rem = nb & 7;
+__device__ __forceinline__ void tile_of(const Order& o, int block, int& rt, int& ct) {
+    const int nb = o.row_tiles * o.col_tiles, xcd = block & 7, i = block >> 3, per = nb >> 3, rem = nb & 7;
     const int w = xcd * per + (xcd < rem ? xcd : rem) + i;
     const int panel = w / (4 * o.col_tiles), rows = o.row_tiles - 4 * panel < 4 ? o.row_tiles - 4 * panel : 4;
     const int at = w - panel * 4 * o.col_tiles;
@@ -74,14 +74,13 @@ __device__ __forceinline__ void tile_of(const Order& o, int& rt, int& ct) {
 }
 
 template <class L, bool F8>
-__global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterProduct g, const Order order) {
+__device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& order, int block, unsigned char* lds) {
     constexpr int RB = L::RB, CB = L::CB, NW = L::NW;
-    extern __shared__ __align__(1024) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5;
     const int wr = wave / L::WN, wc = wave % L::WN;
     int rt, ct;
-    tile_of(order, rt, ct);
+    tile_of(order, block, rt, ct);
     const int64_t row0 = (int64_t)rt * L::TM;
     const int col0 = ct * L::TN;
     const int rows = g.M - row0 < L::TM ? (int)(g.M - row0) : L::TM;
@@ -285,14 +284,16 @@ __global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterPro
 }
 
 template <class L, bool F8>
+__global__ __launch_bounds__(64 * L::NW) void adapters_y_kernel(const AdapterProduct g, const Order order) {
+    extern __shared__ __align__(1024) unsigned char lds[];
+    y_tile<L, F8>(g, order, blockIdx.x, lds);
+}
+
+template <class L, bool F8>
 hipError_t launch_tile(const AdapterProduct& p, hipStream_t s) {
-    const void* const fn = reinterpret_cast<const void*>(&adapters_y_kernel<L, F8>);
     static std::atomic<bool> attr_set{false};
-    if (!attr_set.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, L::lds);
-        if (e != hipSuccess) return e;
-        attr_set.store(true, std::memory_order_release);
-    }
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_y_kernel<L, F8>), L::lds, attr_set);
+    if (e != hipSuccess) return e;
     const int64_t rt = ceil_div(p.M, L::TM), ct = ceil_div(p.Q, L::TN);
     if (rt * ct > INT_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((adapters_y_kernel<L, F8>), dim3((unsigned)(rt * ct)), dim3(64 * L::NW), L::lds, s, p, Order{(int)rt, (int)ct});
@@ -303,17 +304,48 @@ using T256 = Tile<256, 256, 2, 4, 1, 1>;
 using T128 = Tile<128, 128, 2, 2, 3, 3>;
 using T64 = Tile<64, 64, 2, 2, 5, 5>;
 
+// The largest tile of which there are three for four compute units
+int y_tile_rows(const AdapterProduct& p) {
+    if (ceil_div(p.M, 256) * ceil_div(p.Q, 256) >= 192) return 256;
+    return ceil_div(p.M, 128) * ceil_div(p.Q, 128) >= 192 ? 128 : 64;
+}
 template <bool F8>
 hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
-    const int64_t big = ceil_div(p.M, 256) * ceil_div(p.Q, 256), mid = ceil_div(p.M, 128) * ceil_div(p.Q, 128);
-    if (big >= 192) return launch_tile<T256, F8>(p, s);
-    if (mid >= 192) return launch_tile<T128, F8>(p, s);
-    return launch_tile<T64, F8>(p, s);
+    switch (y_tile_rows(p)) {
+        case 256: return launch_tile<T256, F8>(p, s);
+        case 128: return launch_tile<T128, F8>(p, s);
+        default: return launch_tile<T64, F8>(p, s);
+    }
+}
+
+// dX and the factor gradients of few rows in one launch: neither fills the chip
+template <int VB>
+__global__ __launch_bounds__(256) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b) {
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tiles = order.row_tiles * order.col_tiles, blocks = a.blocks + b.blocks, i = (int)blockIdx.x - tiles;
+    if (i < 0) y_tile<T64, false>(x, order, blockIdx.x, lds);
+    else grad_block<VB>(g, a, b, i % blocks, 0, i / blocks, lds);
+}
+template <int VB>
+hipError_t launch_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
+    constexpr int lds = T64::lds > Grad<VB>::lds ? T64::lds : Grad<VB>::lds;
+    static std::atomic<bool> attr_set{false};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_dx_grad_kernel<VB>), lds, attr_set);
+    if (e != hipSuccess) return e;
+    Side a, b;
+    grad_sides(g, 0, a, b);
+    const Order order{x ? (int)ceil_div(g.M, 64) : 0, x ? (int)ceil_div(x->Q, 64) : 0};
+    const int64_t blocks = (int64_t)order.row_tiles * order.col_tiles + (int64_t)(a.blocks + b.blocks) * g.count;
+    if (blocks > INT_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((adapters_dx_grad_kernel<VB>), dim3((unsigned)blocks), dim3(256), lds, s, x ? *x : AdapterProduct{}, order, g, a, b);
+    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------------ T
 // 32 rows a work-group; its four waves share out the four steps of a slab and add their sums at the end, in order.  CB blocks of 32 columns hold
 // 32 CB / r adapters; rows of more adapters than that take another pass over their x.
+// PLANES: the backward's dT_i = A_a^T dY_i.  A lies with the contraction first, [m, r]: slabs of 64 rows of the adapters' A, one behind the other as they lie
+// in memory, read with the transposing load.
 template <int CB_, int NS_>
 struct Low {
     static constexpr int CB = CB_, NS = NS_, TN = 32 * CB;
@@ -325,17 +357,31 @@ struct Low {
 };
 
 template <class L, bool PLANES>
-__global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g) {
+__device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsigned char* lds) {
     constexpr int CB = L::CB, NS = L::NS;
-    extern __shared__ __align__(1024) unsigned char lds[];
     int* const list = reinterpret_cast<int*>(lds + L::ring);
     int* const ranks = list + 32;
     int* const place = ranks + 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5;
-    const int64_t row0 = (int64_t)blockIdx.x * 32;
+    const int64_t row0 = (int64_t)tile * 32;
     const int rows = g.M - row0 < 32 ? (int)(g.M - row0) : 32;
     const int n = g.ke, r = g.r;
+
+    const int slots = L::TN / r;
+    const int lrow = lane >> 3;
+    const int ns = (n * 2 + 127) / 128;
+    const int xrow = 8 * wave + lrow, xchunk = ((lane & 7) ^ ((xrow >> 1) & 7)) * 16;
+    const rsrc_t xres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
+    int xslot = 0, xissued = 0;
+    auto issue_x = [&]() {
+        unsigned char* const dst = lds + xslot + wave * 1024;
+        xslot = xslot == (NS - 1) * L::slab ? 0 : xslot + L::slab;
+        const int x = xissued * 128 + xchunk;
+        ++xissued;
+        load_lds16(xres, dst, x < 2 * n ? xrow * g.e_pitch * 2 + x : kBufNowhere, 0);
+    };
+    while (xissued < NS - 1 && xissued < ns) issue_x();   // before anything is known of the adapters
 
     // which adapters the rows have, in ascending order, and which of them each row has
     int id = gload(g.row_adapter + row0 + (lj < rows ? lj : 0));
@@ -348,40 +394,64 @@ __global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g)
     }
     if (threadIdx.x < 32) place[lj] = at;
     __syncthreads();
-    if ((int)threadIdx.x < count) ranks[threadIdx.x] = rank_of(g, list[threadIdx.x]);
-    __syncthreads();
+    int rank = 0;                                         // (what lies past a rank is read beside it and masked at the end)
+    if ((int)threadIdx.x < count) rank = rank_of(g, list[threadIdx.x]);
 
-    const int slots = L::TN / r;
-    const int lrow = lane >> 3;
-    const int ns = (n * 2 + 127) / 128;
-    const int xrow = 8 * wave + lrow, xchunk = ((lane & 7) ^ ((xrow >> 1) & 7)) * 16;
-    const rsrc_t xres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
     const int frow = out_row(lj);
     const int xsw = (lj >> 1) & 7, fsw = (frow >> 1) & 7;
     const int xread = lj * 128 + (((2 * wave + lh) ^ xsw) * 16), fread = L::xpart + frow * 128 + (((2 * wave + lh) ^ fsw) * 16);
+    // the transposing load: sixteen lanes read four rows of sixteen columns, four columns an address; this lane's row of the step and its four columns
+    int kread[CB];
+#pragma unroll
+    for (int b = 0; b < CB; ++b) {
+        const int c = 32 * b + out_row(16 * ((lane >> 4) & 1) + 4 * (lane & 3)), of = c / r < slots ? c / r : 0;      // (columns of no adapter: anything)
+        kread[b] = L::xpart + of * 128 * r + (16 * wave + 8 * (lane >> 5) + ((lane & 15) >> 2)) * 2 * r + (c % r) * 2;
+    }
     for (int first = 0; first == 0 || first < count; first += slots) {
-        // Load instruction j covers eight columns, of one adapter (r is a multiple of 8): rows 8 (wave + 4 j) .. of the side-by-side B
+        const int used = (count - first < slots ? count - first : slots) * r;      // columns of this pass
+        // B: load instruction j covers eight columns, of one adapter (r is a multiple of 8): rows 8 (wave + 4 j) .. of the side-by-side B
         rsrc_t fres[L::NF];
-        int used = 0;                                     // columns of this pass
+        // A: this lane's 16 bytes of the first slab, and where in its adapter's they lie
+        const uint16_t* apart[L::NF];
+        int at_a[L::NF];
+        if constexpr (PLANES) {
 #pragma unroll
-        for (int j = 0; j < L::NF; ++j) {
-            const int c = 8 * (wave + 4 * j), p = first + c / r, k = c % r;
-            const bool have = c / r < slots && p < count;
-            const int a = have ? __builtin_amdgcn_readfirstlane(list[p]) : 0, rank = have ? __builtin_amdgcn_readfirstlane(ranks[p]) : 0;
-            fres[j] = make_rsrc(g.F + ((int64_t)a * r + k) * n, rank > k ? (int64_t)(rank - k) * n * 2 : 0);
+            for (int j = 0; j < L::NF; ++j) {
+                const int pos = 64 * (wave + 4 * j) + lane, p = pos / (8 * r);
+                at_a[j] = (pos - p * 8 * r) * 8;
+                apart[j] = p < slots && first + p < count ? g.F + (int64_t)list[first + p] * n * r + at_a[j] : nullptr;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < L::NF; ++j) {
+                const int c = 8 * (wave + 4 * j), p = first + c / r, k = c % r;
+                const bool have = c / r < slots && p < count;
+                const int a = have ? __builtin_amdgcn_readfirstlane(list[p]) : 0;
+                fres[j] = make_rsrc(g.F + ((int64_t)a * r + k) * n, have ? (int64_t)8 * n * 2 : 0);
+            }
         }
-        used = (count - first < slots ? count - first : slots) * r;
-        int issue_slot = 0, issued = 0;
-        auto issue = [&]() {
-            unsigned char* const dst = lds + issue_slot + wave * 1024;
-            issue_slot = issue_slot == (NS - 1) * L::slab ? 0 : issue_slot + L::slab;
-            const int x = issued * 128 + xchunk;          // (the same chunk of eight rows further on)
-            ++issued;
-            load_lds16(xres, dst, x < 2 * n ? xrow * g.e_pitch * 2 + x : kBufNowhere, 0);
+        int fslot = 0, fissued = 0;
+        auto issue_f = [&]() {
+            unsigned char* const dst = lds + fslot + L::xpart + wave * 1024;
+            fslot = fslot == (NS - 1) * L::slab ? 0 : fslot + L::slab;
+            if constexpr (PLANES) {
 #pragma unroll
-            for (int j = 0; j < L::NF; ++j) load_lds16(fres[j], dst + L::xpart + j * 4096, x < 2 * n ? lrow * n * 2 + x : kBufNowhere, 0);
+                for (int j = 0; j < L::NF; ++j) {
+                    const int64_t k = (int64_t)64 * r * fissued;
+                    load_lds16_at(apart[j] && k + at_a[j] < (int64_t)n * r ? (const void*)(apart[j] + k) : (const void*)zero_line, dst + j * 4096);
+                }
+            } else {
+                const int x = fissued * 128 + xchunk;     // (the same chunk of eight rows further on)
+#pragma unroll
+                for (int j = 0; j < L::NF; ++j) load_lds16(fres[j], dst + j * 4096, x < 2 * n ? lrow * n * 2 + x : kBufNowhere, 0);
+            }
+            ++fissued;
         };
-        while (issued < NS - 1 && issued < ns) issue();
+        if (first) {
+            xslot = xissued = 0;
+            while (xissued < NS - 1 && xissued < ns) issue_x();
+        }
+        while (fissued < NS - 1 && fissued < ns) issue_f();
         f32x16 acc[CB];
 #pragma unroll
         for (int b = 0; b < CB; ++b)
@@ -389,22 +459,30 @@ __global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g)
             for (int v = 0; v < 16; ++v) acc[b][v] = 0.0f;
         int slot = 0;
         for (int s = 0; s < ns; ++s) {
-            const int behind = issued - s - 1;
-            if (behind >= NS - 2) wait_newest<(NS - 2) * L::NL>();
-            else if (NS > 3 && behind == NS - 3) wait_newest<(NS > 3 ? NS - 3 : 0) * L::NL>();
-            else wait_newest<0>();
+            // Slab s has landed.  Behind its last load: F of NS - 2 slabs at least, and from slab NS - 2 on X of as many.
+            if (s + NS - 1 > ns) wait_newest<0>();
+            else if (s < NS - 2) wait_newest<(NS - 2) * L::NF>();
+            else wait_newest<(NS - 2) * L::NL>();
             lds_barrier();
-            if (issued < ns) issue();
+            if (xissued < ns) { issue_x(); issue_f(); }
             const unsigned char* const x = lds + slot;
             slot = slot == (NS - 1) * L::slab ? 0 : slot + L::slab;
             const u32x4 xo = *reinterpret_cast<const u32x4*>(x + xread);
             u32x4 fo[CB];
+            if constexpr (PLANES) {
+                const uint32_t base = lds_address(x);
 #pragma unroll
-            for (int b = 0; b < CB; ++b) fo[b] = *reinterpret_cast<const u32x4*>(x + fread + b * 4096);
+                for (int b = 0; b < CB; b += 2)
+                    read_tr2(base + kread[b], base + kread[b] + 8 * r, base + kread[b + 1], base + kread[b + 1] + 8 * r, fo[b], fo[b + 1]);
+            } else {
+#pragma unroll
+                for (int b = 0; b < CB; ++b) fo[b] = *reinterpret_cast<const u32x4*>(x + fread + b * 4096);
+            }
 #pragma unroll
             for (int b = 0; b < CB; ++b) acc[b] = mfma_bf16(fo[b], xo, acc[b]);
         }
         // the waves' sums: blocks of 32 columns in turn, b by wave b % 4
+        if (first == 0 && (int)threadIdx.x < count) ranks[threadIdx.x] = rank;
         lds_barrier();
 #pragma unroll
         for (int b = 0; b < CB; ++b)
@@ -431,14 +509,14 @@ __global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g)
             const int64_t row = row0 + lj;
             const int p = place[lj];
             const float scale = p < 0 || !g.scales ? 1.0f : gload(g.scales + list[p]);
-            const int rank = p < 0 ? 0 : ranks[p];
+            const int mine = p < 0 ? 0 : ranks[p];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int c = 32 * b + 16 * lh + 8 * h, of = c / r, k = c % r;       // eight columns, those of this row's adapter?
                 if (of >= slots || (p < 0 ? first != 0 || of != 0 : p - first != of)) continue;
                 float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = k + i < rank ? acc[b][8 * h + i] : 0.0f;
+                for (int i = 0; i < 8; ++i) v[i] = k + i < mine ? acc[b][8 * h + i] : 0.0f;
                 if constexpr (!PLANES) {
                     if (g.T) {
                         gstore(reinterpret_cast<f32x4*>(g.T + row * r + k), f32x4{v[0], v[1], v[2], v[3]});
@@ -448,7 +526,7 @@ __global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g)
                     if (g.Tb) {
                         u32x4 w;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(k + 2 * i < rank ? scale * v[2 * i] : 0.0f, k + 2 * i + 1 < rank ? scale * v[2 * i + 1] : 0.0f);
+                        for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(k + 2 * i < mine ? scale * v[2 * i] : 0.0f, k + 2 * i + 1 < mine ? scale * v[2 * i + 1] : 0.0f);
                         gstore(reinterpret_cast<u32x4*>(g.Tb + row * r + k), w);
                     }
                 } else {
@@ -478,12 +556,12 @@ __global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g)
                     };
                     float u[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) u[i] = k + i < rank ? scale * v[i] : 0.0f;
+                    for (int i = 0; i < 8; ++i) u[i] = k + i < mine ? scale * v[i] : 0.0f;
                     planes(g.dT_planes, u);
                     if (g.T_planes) {
                         const f32x4 t0 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k)), t1 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k + 4));
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) u[i] = k + i < rank ? scale * (i < 4 ? t0[i & 3] : t1[i & 3]) : 0.0f;
+                        for (int i = 0; i < 8; ++i) u[i] = k + i < mine ? scale * (i < 4 ? t0[i & 3] : t1[i & 3]) : 0.0f;
                         planes(g.T_planes, u);
                     }
                 }
@@ -493,28 +571,62 @@ __global__ __launch_bounds__(256) void adapters_t_kernel(const AdapterProduct g)
     }
 }
 
-template <class L, bool PLANES>
-hipError_t launch_low_tile(const AdapterProduct& p, hipStream_t s) {
-    const void* const fn = reinterpret_cast<const void*>(&adapters_t_kernel<L, PLANES>);
-    static std::atomic<bool> attr_set{false};
-    if (!attr_set.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, L::lds);
-        if (e != hipSuccess) return e;
-        attr_set.store(true, std::memory_order_release);
-    }
-    hipLaunchKernelGGL((adapters_t_kernel<L, PLANES>), dim3((unsigned)ceil_div(p.M, 32)), dim3(256), L::lds, s, p);
-    return hipGetLastError();
+template <class L>
+__global__ __launch_bounds__(256, 2) void adapters_t_kernel(const AdapterProduct g) {
+    extern __shared__ __align__(1024) unsigned char lds[];
+    t_tile<L, false>(g, blockIdx.x, lds);
 }
 
-template <bool PLANES>
-hipError_t launch_low(const AdapterProduct& p, hipStream_t s) {
-    return p.r <= 32 ? launch_low_tile<Low<2, 6>, PLANES>(p, s) : launch_low_tile<Low<4, 4>, PLANES>(p, s);
+// dT, and beside it what only later launches need
+template <class L>
+__global__ __launch_bounds__(256, 2) void adapters_dt_kernel(const AdapterProduct g, const AdapterPrep p, const PrepBlocks n) {
+    extern __shared__ __align__(1024) unsigned char lds[];
+    if ((int)blockIdx.x < n.all) prepare(p, n, blockIdx.x, lds);
+    else t_tile<L, true>(g, (int)blockIdx.x - n.all, lds);
+}
+
+template <class L>
+hipError_t launch_t(const AdapterProduct& p, hipStream_t s) {
+    static std::atomic<bool> attr_set{false};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_t_kernel<L>), L::lds, attr_set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((adapters_t_kernel<L>), dim3((unsigned)ceil_div(p.M, 32)), dim3(256), L::lds, s, p);
+    return hipGetLastError();
+}
+template <class L>
+hipError_t launch_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream_t s) {
+    static std::atomic<bool> attr_set{false};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_dt_kernel<L>), L::lds, attr_set);
+    if (e != hipSuccess) return e;
+    static_assert(L::lds >= kPrepLds, "");
+    const PrepBlocks n = prep_blocks(prep);
+    const int64_t tiles = ceil_div(p.M, 32), blocks = tiles + n.all;
+    if (blocks > INT_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((adapters_dt_kernel<L>), dim3((unsigned)blocks), dim3(256), L::lds, s, p, prep, n);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s) { return fp8 ? launch_y<true>(p, s) : launch_y<false>(p, s); }
-hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return launch_low<false>(p, s); }
-hipError_t launch_adapters_planes(const AdapterProduct& p, hipStream_t s) { return launch_low<true>(p, s); }
+hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return p.r <= 32 ? launch_t<Low<2, 6>>(p, s) : launch_t<Low<4, 4>>(p, s); }
+hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream_t s) {
+    return p.r <= 32 ? launch_dt<Low<2, 6>>(p, prep, s) : launch_dt<Low<4, 4>>(p, prep, s);
+}
+
+hipError_t launch_adapters_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
+    if (g.M > kAdapterFewGradRows) return hipErrorInvalidValue;
+    if (x && y_tile_rows(*x) != 64) {
+        const hipError_t e = launch_adapters_y(*x, false, s);
+        if (e != hipSuccess) return e;
+        x = nullptr;
+    }
+    switch (plane_columns(g.r)) {
+        case 16: return launch_dx_grads<1>(x, g, s);
+        case 32: return launch_dx_grads<2>(x, g, s);
+        case 64: return launch_dx_grads<4>(x, g, s);
+        default: return launch_dx_grads<8>(x, g, s);
+    }
+}
 
 }  // namespace abt

@@ -55,7 +55,7 @@ int adapters_fwd(const void* X, const void* main, const float* x_scale, const vo
 }
 
 struct BwdPlaces {
-    size_t Wt, At, Bt, T, dT_planes, T_planes, order, offsets, zeros, partials, bytes;
+    size_t Wt, Bt, T, dT_planes, T_planes, order, offsets, partials, bytes;
 };
 BwdPlaces bwd_places(int64_t M, int64_t m, int64_t n, int64_t r, int64_t count) {
     BwdPlaces p{};
@@ -66,14 +66,12 @@ BwdPlaces bwd_places(int64_t M, int64_t m, int64_t n, int64_t r, int64_t count) 
     };
     const int64_t rp = plane_columns((int)r);
     take(p.Wt, m * n * 2);
-    take(p.At, count * m * r * 2);
     take(p.Bt, count * n * r * 2);
     take(p.T, M * r * 4);
     take(p.dT_planes, M * 3 * rp * 2);
     take(p.T_planes, M * 3 * rp * 2);
     take(p.order, M * 4);
     take(p.offsets, (count + 1) * 4);
-    take(p.zeros, 256);
     take(p.partials, (int64_t)adapters_grad_partial_bytes(M, (int)m, (int)n, (int)r, (int)count));
     p.bytes = at;
     return p;
@@ -150,37 +148,32 @@ int lr_adapters_bwd(const void* dY, const void* X, const float* T, const void* W
         const hipStream_t s = (hipStream_t)stream;
         char* const ws = (char*)workspace;
         const bool grads = dA || dB;
-        AdapterPrep prep{};
-        if (dX) { prep.W = (const uint16_t*)W; prep.B = (const uint16_t*)adapters->B; }
-        prep.A = (const uint16_t*)adapters->A;
-        prep.Wt = (uint16_t*)(ws + at.Wt); prep.At = (uint16_t*)(ws + at.At); prep.Bt = (uint16_t*)(ws + at.Bt);
-        prep.row_adapter = row_adapter; prep.zeros = (unsigned char*)ws + at.zeros; prep.offsets = (int32_t*)(ws + at.offsets);
-        if (grads) prep.order = (int32_t*)(ws + at.order);
-        prep.M = M; prep.m = (int)m; prep.n = (int)n; prep.r = (int)r; prep.count = (int)count;
-        if (launch_adapters_prep(prep, s) != hipSuccess) return ABT_EHIP;
         if (dA && !T) {
             float* const again = (float*)(ws + at.T);
             if (make_t(adapters, row_adapter, X, again, nullptr, M, n, s) != hipSuccess) return ABT_EHIP;
             T = again;
         }
+        AdapterPrep prep{};
+        if (dX) { prep.W = (const uint16_t*)W; prep.B = (const uint16_t*)adapters->B; }
+        prep.Wt = (uint16_t*)(ws + at.Wt); prep.Bt = (uint16_t*)(ws + at.Bt);
+        prep.row_adapter = row_adapter; prep.offsets = (int32_t*)(ws + at.offsets);
+        if (grads) prep.order = (int32_t*)(ws + at.order);
+        prep.M = M; prep.m = (int)m; prep.n = (int)n; prep.r = (int)r; prep.count = (int)count;
         AdapterProduct p = product(adapters, row_adapter, M);
-        p.E = (const uint16_t*)dY; p.F = prep.At; p.Q = (int)r; p.ke = (int)m; p.e_pitch = (int)m;
+        p.E = (const uint16_t*)dY; p.F = (const uint16_t*)adapters->A; p.Q = (int)r; p.ke = (int)m; p.e_pitch = (int)m;
         p.dT_planes = (uint16_t*)(ws + at.dT_planes);
         if (dA) { p.T_in = T; p.T_planes = (uint16_t*)(ws + at.T_planes); }
-        if (launch_adapters_planes(p, s) != hipSuccess) return ABT_EHIP;
-        if (dX) {
-            AdapterProduct x = product(adapters, row_adapter, M);
-            x.X = dY; x.W = prep.Wt; x.E = p.dT_planes; x.F = prep.Bt; x.Q = (int)n; x.kmain = (int)m; x.ke = (int)r;
-            x.e_pitch = 3 * plane_columns((int)r); x.Y = (uint16_t*)dX;     // the first plane is dT rounded to bf16
-            if (launch_adapters_y(x, false, s) != hipSuccess) return ABT_EHIP;
-        }
-        if (grads) {
-            AdapterGrads g{};
-            g.dY = (const uint16_t*)dY; g.T_planes = p.T_planes; g.dA = dA; g.X = (const uint16_t*)X; g.dT_planes = p.dT_planes; g.dB = dB;
-            g.order = prep.order; g.offsets = prep.offsets; g.zeros = prep.zeros; g.partials = (float*)(ws + at.partials);
-            g.M = M; g.m = (int)m; g.n = (int)n; g.r = (int)r; g.count = (int)count; g.accumulate = accumulate;
-            if (launch_adapters_grads(g, s) != hipSuccess) return ABT_EHIP;
-        }
+        if (launch_adapters_dt(p, prep, s) != hipSuccess) return ABT_EHIP;
+        AdapterProduct x = product(adapters, row_adapter, M);
+        x.X = dY; x.W = prep.Wt; x.E = p.dT_planes; x.F = prep.Bt; x.Q = (int)n; x.kmain = (int)m; x.ke = (int)r;
+        x.e_pitch = 3 * plane_columns((int)r); x.Y = (uint16_t*)dX;         // the first plane is dT rounded to bf16
+        AdapterGrads g{};
+        g.dY = (const uint16_t*)dY; g.T_planes = p.T_planes; g.dA = dA; g.X = (const uint16_t*)X; g.dT_planes = p.dT_planes; g.dB = dB;
+        g.order = prep.order; g.offsets = prep.offsets; g.partials = (float*)(ws + at.partials);
+        g.M = M; g.m = (int)m; g.n = (int)n; g.r = (int)r; g.count = (int)count; g.accumulate = accumulate;
+        if (grads && M <= kAdapterFewGradRows) return launch_adapters_dx_grads(dX ? &x : nullptr, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
+        if (dX && launch_adapters_y(x, false, s) != hipSuccess) return ABT_EHIP;
+        if (grads && launch_adapters_grads(g, s) != hipSuccess) return ABT_EHIP;
         return ABT_OK;
     });
 }
