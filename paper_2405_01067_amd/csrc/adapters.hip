@@ -156,6 +156,32 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
 #pragma unroll
             for (int b = 0; b < CB; ++b) acc[a][b] = mfma_f8(o.f[b], p.f[b], o.x[a], p.x[a], acc[a][b]);
     };
+    // The adapters of this wave's rows, in ascending order.  Their operands come straight from memory, there is little of them: the first before the last slab, each
+    // of the others behind the one before.
+    struct Piece { int a, rank, k; };                     // sixteen columns from k on
+    auto after = [&](int a) {
+        int best = INT_MAX;
+#pragma unroll
+        for (int i = 0; i < RB; ++i) best = mine[i] > a && mine[i] < best ? mine[i] : best;
+        return wave_min(best);
+    };
+    auto adapter = [&](int a) {                           // the next one that has a rank, from a on
+        int rank = 0;
+        while (a != INT_MAX && (rank = __builtin_amdgcn_readfirstlane(rank_of(g, a))) == 0) a = after(a);
+        return Piece{a, rank, 0};
+    };
+    const rsrc_t eres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
+    const int eoff = ((wr * RB * 32 + lj) * g.e_pitch + 8 * lh) * 2, foff = ((wc * CB * 32 + frow) * g.ke + 8 * lh) * 2;
+    Ops ahead;
+    auto fetch = [&](const Piece& l) {
+        const rsrc_t fres = make_rsrc(g.F + ((int64_t)l.a * g.Q + col0) * g.ke, (int64_t)cols * g.ke * 2);
+        const bool there = l.k + 8 * lh < l.rank;
+#pragma unroll
+        for (int b = 0; b < CB; ++b) ahead.f[b] = buf_load16(fres, there ? foff + b * 64 * g.ke + 2 * l.k : kBufNowhere, 0);
+#pragma unroll
+        for (int i = 0; i < RB; ++i) ahead.x[i] = buf_load16(eres, there && mine[i] == l.a ? eoff + i * 64 * g.e_pitch + 2 * l.k : kBufNowhere, 0);
+    };
+    Piece piece = adapter(after(-1)), coming = piece.a == INT_MAX ? piece : adapter(after(piece.a));
     // Slab s has landed: loads come back in the order of issue.
     auto slab = [&](int s) {
         if (s + L::LX > nmain) wait_newest<0>();
@@ -164,6 +190,7 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
         // into the slots whose reads ended before this barrier
         if (s + L::LW < nmain) issue_w(s + L::LW);
         if (s + L::LX < nmain) issue_x(s + L::LX);
+        if (s + 1 == nmain && piece.a != INT_MAX) fetch(piece);
     };
     auto next = [&]() {
         xat = xat == L::LX * L::xpart ? 0 : xat + L::xpart;
@@ -217,8 +244,12 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 read(o[j & 1], j);
-                __builtin_amdgcn_sched_barrier(0);
                 mma(o[(j + 1) & 1]);
+#pragma unroll
+                for (int i = 0; i < RB + CB; ++i) {       // a read behind every product
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             next();
@@ -226,36 +257,21 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
         mma(o[1]);
     }
 
-    // The adapters of this wave's rows, in ascending order.  Their operands come straight from memory: 16 columns of 32 rows are one piece of it
-    // where the rank is 16, and there is little of it.
-    auto after = [&](int a) {
-        int best = INT_MAX;
+    // what is left of the adapters
+    while (piece.a != INT_MAX) {
+        const Piece now = piece;
+        Ops m = ahead;
+        piece.k += 16;
+        if (piece.k >= piece.rank) piece = coming;
+        if (piece.a != INT_MAX) fetch(piece);
+        if (now.a != piece.a && piece.a != INT_MAX) coming = adapter(after(piece.a));
+        if (now.rank - now.k < 16 && (now.rank & 7)) {    // columns past the rank are no part of the adapter, whatever they hold (T is zero there)
+            const int valid = now.rank - now.k - 8 * lh;
+            if (valid < 8)
 #pragma unroll
-        for (int i = 0; i < RB; ++i) best = mine[i] > a && mine[i] < best ? mine[i] : best;
-        return wave_min(best);
-    };
-    const rsrc_t eres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
-    const int eoff = ((wr * RB * 32 + lj) * g.e_pitch + 8 * lh) * 2, foff = ((wc * CB * 32 + frow) * g.ke + 8 * lh) * 2;
-    for (int a = after(-1); a != INT_MAX; a = after(a)) {
-        const int rank = __builtin_amdgcn_readfirstlane(rank_of(g, a));
-        const rsrc_t fres = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * g.ke, (int64_t)cols * g.ke * 2);
-#pragma unroll 1
-        for (int k = 0; k < rank; k += 16) {
-            const int valid = rank - k - 8 * lh;          // columns past the rank are no part of the adapter, whatever they hold
-#pragma unroll
-            for (int b = 0; b < CB; ++b) o[0].f[b] = buf_load16(fres, valid > 0 ? foff + b * 64 * g.ke + 2 * k : kBufNowhere, 0);
-#pragma unroll
-            for (int i = 0; i < RB; ++i) o[0].x[i] = buf_load16(eres, valid > 0 && mine[i] == a ? eoff + i * 64 * g.e_pitch + 2 * k : kBufNowhere, 0);
-            if (rank - k < 16 && (rank & 7)) {
-                if (valid < 8) {
-#pragma unroll
-                    for (int b = 0; b < CB; ++b) o[0].f[b] = first_of(o[0].f[b], valid);
-#pragma unroll
-                    for (int i = 0; i < RB; ++i) o[0].x[i] = first_of(o[0].x[i], valid);
-                }
-            }
-            mma(o[0]);
+                for (int b = 0; b < CB; ++b) m.f[b] = first_of(m.f[b], valid);
         }
+        mma(m);
     }
 
     // out through LDS as whole rows
@@ -300,21 +316,49 @@ hipError_t launch_tile(const AdapterProduct& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-using T256 = Tile<256, 256, 2, 4, 1, 1>;
-using T128 = Tile<128, 128, 2, 2, 3, 3>;
-using T64 = Tile<64, 64, 2, 2, 5, 5>;
+// The tiles.  Two or three work-groups of the smaller ones share a compute unit, and while one starts or stores the others compute.
+using T256x256 = Tile<256, 256, 2, 4, 1, 1>;
+using T192x256 = Tile<192, 256, 2, 4, 1, 1>;
+using T128x192 = Tile<128, 192, 2, 2, 1, 1>;
+using T128x128 = Tile<128, 128, 2, 2, 1, 1>;
+using T64x128 = Tile<64, 128, 2, 2, 1, 1>;
+using T64x64 = Tile<64, 64, 2, 2, 2, 2>;
 
-// The largest tile of which there are three for four compute units
-int y_tile_rows(const AdapterProduct& p) {
-    if (ceil_div(p.M, 256) * ceil_div(p.Q, 256) >= 192) return 256;
-    return ceil_div(p.M, 128) * ceil_div(p.Q, 128) >= 192 ? 128 : 64;
+// What a tile costs, us: a slab and the rest of a tile where the compute unit is shared by as many as fit, and where it has the unit to itself.  Fitted to
+// launches of all six at 54 shapes in both types (140 to 12608 rows, 768 to 4096 columns and contractions; r = 16, runs of 197 rows): the rule takes
+// the fastest or one 8 % slower at all but one of them, 0.8 % on average.  The ends of the range, us:
+//                      256x256   192x256   128x192   128x128   64x128    64x64
+//   140 x 768 x 768       20.4      16.6      12.4       9.7      8.0      7.5
+//   1379 x 2304 x 768     22.6      18.5      14.1      11.6     11.6     16.9
+//   12608 x 768 x 2304    53.8      45.5      47.5      61.3     56.3     74.0
+//   12608 x 2304 x 768    51.6      59.8      53.4      58.0     68.3     89.5
+//   8190 x 4096 x 4096   208.9     252.0     252.6     237.3    317.2    418.0        1320 TFLOP/s; 8 bits 110 us, 2490
+struct TileCost { int tm, tn, per_cu; float slab, rest, alone_slab, alone_rest; };
+constexpr TileCost kTiles[] = {{256, 256, 1, 1.27f, 5.86f, 1.27f, 5.86f}, {192, 256, 1, 0.94f, 6.01f, 0.94f, 6.01f}, {128, 192, 2, 0.55f, 2.79f, 0.61f, 5.85f},
+                               {128, 128, 2, 0.46f, 2.66f, 0.56f, 5.33f}, {64, 128, 3, 0.27f, 1.36f, 0.56f, 2.22f},  {64, 64, 3, 0.27f, 1.30f, 0.33f, 2.65f}};
+constexpr int kTile64 = 5;
+float tile_cost(int i, const AdapterProduct& p, bool fp8) {
+    const TileCost& t = kTiles[i];
+    const int64_t tiles = ceil_div(p.M, t.tm) * ceil_div(p.Q, t.tn);
+    const float slabs = (float)ceil_div((int64_t)p.kmain * (fp8 ? 1 : 2), 128);
+    const float shared = (float)ceil_div(tiles, 256) * (slabs * t.slab + t.rest), alone = (float)ceil_div(tiles, 256 * t.per_cu) * (slabs * t.alone_slab + t.alone_rest);
+    return shared > alone ? shared : alone;
+}
+int best_tile(const AdapterProduct& p, bool fp8) {
+    int best = 0;
+    for (int i = 1; i <= kTile64; ++i)
+        if (tile_cost(i, p, fp8) < tile_cost(best, p, fp8)) best = i;
+    return best;
 }
 template <bool F8>
 hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
-    switch (y_tile_rows(p)) {
-        case 256: return launch_tile<T256, F8>(p, s);
-        case 128: return launch_tile<T128, F8>(p, s);
-        default: return launch_tile<T64, F8>(p, s);
+    switch (best_tile(p, F8)) {
+        case 0: return launch_tile<T256x256, F8>(p, s);
+        case 1: return launch_tile<T192x256, F8>(p, s);
+        case 2: return launch_tile<T128x192, F8>(p, s);
+        case 3: return launch_tile<T128x128, F8>(p, s);
+        case 4: return launch_tile<T64x128, F8>(p, s);
+        default: return launch_tile<T64x64, F8>(p, s);
     }
 }
 
@@ -323,12 +367,12 @@ template <int VB>
 __global__ __launch_bounds__(256) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b) {
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tiles = order.row_tiles * order.col_tiles, blocks = a.blocks + b.blocks, i = (int)blockIdx.x - tiles;
-    if (i < 0) y_tile<T64, false>(x, order, blockIdx.x, lds);
+    if (i < 0) y_tile<T64x64, false>(x, order, blockIdx.x, lds);
     else grad_block<VB>(g, a, b, i % blocks, 0, i / blocks, lds);
 }
 template <int VB>
 hipError_t launch_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
-    constexpr int lds = T64::lds > Grad<VB>::lds ? T64::lds : Grad<VB>::lds;
+    constexpr int lds = T64x64::lds > Grad<VB>::lds ? T64x64::lds : Grad<VB>::lds;
     static std::atomic<bool> attr_set{false};
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_dx_grad_kernel<VB>), lds, attr_set);
     if (e != hipSuccess) return e;
@@ -616,7 +660,8 @@ hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, 
 
 hipError_t launch_adapters_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
     if (g.M > kAdapterFewGradRows) return hipErrorInvalidValue;
-    if (x && y_tile_rows(*x) != 64) {
+    // (a launch of its own costs some 4 us)
+    if (x && tile_cost(kTile64, *x, false) > tile_cost(best_tile(*x, false), *x, false) + 4.0f) {
         const hipError_t e = launch_adapters_y(*x, false, s);
         if (e != hipSuccess) return e;
         x = nullptr;
