@@ -55,9 +55,13 @@ struct AdapterGrads {
 };
 int adapters_grad_piece(int64_t M, int m, int n);      // rows of a piece
 size_t adapters_grad_partial_bytes(int64_t M, int m, int n, int r, int count);
-hipError_t launch_adapters_grads(const AdapterGrads& p, hipStream_t s);
+// With x, dX beside them in the same launch
+hipError_t launch_adapters_grads(const AdapterGrads& p, const AdapterProduct* x, hipStream_t s);
 // Few rows: no partials, and dX (or NULL) in the same launch
 constexpr int kAdapterFewGradRows = 1024;
-hipError_t launch_adapters_dx_grads(const AdapterProduct* x, const AdapterGrads& p, hipStream_t s);
+hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGrads& p, hipStream_t s);
+// Many rows and a narrow rank: is dX faster beside the gradients than before them?  And that launch.
+bool adapters_dx_beside_grads(const AdapterProduct& x, const AdapterGrads& p);
+hipError_t launch_adapters_dx_grad_pieces(const AdapterProduct& x, const AdapterGrads& p, int piece, hipStream_t s);
 
 }  // namespace abt

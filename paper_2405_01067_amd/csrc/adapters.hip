@@ -336,7 +336,7 @@ using T64x64 = Tile<64, 64, 2, 2, 2, 2>;
 struct TileCost { int tm, tn, per_cu; float slab, rest, alone_slab, alone_rest; };
 constexpr TileCost kTiles[] = {{256, 256, 1, 1.27f, 5.86f, 1.27f, 5.86f}, {192, 256, 1, 0.94f, 6.01f, 0.94f, 6.01f}, {128, 192, 2, 0.55f, 2.79f, 0.61f, 5.85f},
                                {128, 128, 2, 0.46f, 2.66f, 0.56f, 5.33f}, {64, 128, 3, 0.27f, 1.36f, 0.56f, 2.22f},  {64, 64, 3, 0.27f, 1.30f, 0.33f, 2.65f}};
-constexpr int kTile64 = 5;
+constexpr int kTile128x192 = 2, kTile64 = 5;
 float tile_cost(int i, const AdapterProduct& p, bool fp8) {
     const TileCost& t = kTiles[i];
     const int64_t tiles = ceil_div(p.M, t.tm) * ceil_div(p.Q, t.tn);
@@ -362,26 +362,29 @@ hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
     }
 }
 
-// dX and the factor gradients of few rows in one launch: neither fills the chip
-template <int VB>
-__global__ __launch_bounds__(256) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b) {
+// dX and the factor gradients in one launch, the tiles of dX first: of few rows neither fills the chip; of many one is bound by the matrix unit and the
+// other by memory, and a work-group of each fits a compute unit beside the other.
+template <class L, int VB>
+__global__ __launch_bounds__(256, 2) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b, int piece) {
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tiles = order.row_tiles * order.col_tiles, blocks = a.blocks + b.blocks, i = (int)blockIdx.x - tiles;
-    if (i < 0) y_tile<T64x64, false>(x, order, blockIdx.x, lds);
-    else grad_block<VB>(g, a, b, i % blocks, 0, i / blocks, lds);
+    if (i < 0) y_tile<L, false>(x, order, blockIdx.x, lds);
+    else grad_block<VB>(g, a, b, i % blocks, piece, i / blocks, lds);
 }
-template <int VB>
-hipError_t launch_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
-    constexpr int lds = T64x64::lds > Grad<VB>::lds ? T64x64::lds : Grad<VB>::lds;
+// piece = 0: whole adapters
+template <class L, int VB>
+hipError_t launch_dx_grads(const AdapterProduct* x, const AdapterGrads& g, int piece, hipStream_t s) {
+    constexpr int lds = L::lds > Grad<VB>::lds ? L::lds : Grad<VB>::lds;
     static std::atomic<bool> attr_set{false};
-    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_dx_grad_kernel<VB>), lds, attr_set);
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_dx_grad_kernel<L, VB>), lds, attr_set);
     if (e != hipSuccess) return e;
+    const int64_t pieces = piece ? ceil_div(g.M, piece) : g.count;
     Side a, b;
-    grad_sides(g, 0, a, b);
-    const Order order{x ? (int)ceil_div(g.M, 64) : 0, x ? (int)ceil_div(x->Q, 64) : 0};
-    const int64_t blocks = (int64_t)order.row_tiles * order.col_tiles + (int64_t)(a.blocks + b.blocks) * g.count;
+    grad_sides(g, pieces + g.count, a, b);
+    const Order order{x ? (int)ceil_div(g.M, L::TM) : 0, x ? (int)ceil_div(x->Q, L::TN) : 0};
+    const int64_t blocks = (int64_t)order.row_tiles * order.col_tiles + (a.blocks + b.blocks) * pieces;
     if (blocks > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((adapters_dx_grad_kernel<VB>), dim3((unsigned)blocks), dim3(256), lds, s, x ? *x : AdapterProduct{}, order, g, a, b);
+    hipLaunchKernelGGL((adapters_dx_grad_kernel<L, VB>), dim3((unsigned)blocks), dim3(256), lds, s, x ? *x : AdapterProduct{}, order, g, a, b, piece);
     return hipGetLastError();
 }
 
@@ -396,7 +399,7 @@ struct Low {
     static constexpr int xpart = 4096, slab = xpart + TN * 128, NF = CB, NL = 1 + NF;
     static constexpr int sums = 3 * CB * 4096;
     static constexpr int ring = NS * slab > sums ? NS * slab : sums;
-    static constexpr int lds = ring + 32 * 3 * 4;         // and the adapters, their ranks, the rows' places among them
+    static constexpr int lds = ring + 32 * 4 * 4;         // and the adapters, their ranks and scales, the rows' places among them
     static_assert((NS - 2) * NL < 64 && lds <= 160 * 1024, "");
 };
 
@@ -406,6 +409,7 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
     int* const list = reinterpret_cast<int*>(lds + L::ring);
     int* const ranks = list + 32;
     int* const place = ranks + 32;
+    float* const scales = reinterpret_cast<float*>(place + 32);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5;
     const int64_t row0 = (int64_t)tile * 32;
@@ -439,7 +443,11 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
     if (threadIdx.x < 32) place[lj] = at;
     __syncthreads();
     int rank = 0;                                         // (what lies past a rank is read beside it and masked at the end)
-    if ((int)threadIdx.x < count) rank = rank_of(g, list[threadIdx.x]);
+    float my_scale = 1.0f;
+    if ((int)threadIdx.x < count) {
+        rank = rank_of(g, list[threadIdx.x]);
+        if (g.scales) my_scale = gload(g.scales + list[threadIdx.x]);
+    }
 
     const int frow = out_row(lj);
     const int xsw = (lj >> 1) & 7, fsw = (frow >> 1) & 7;
@@ -526,7 +534,10 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
             for (int b = 0; b < CB; ++b) acc[b] = mfma_bf16(fo[b], xo, acc[b]);
         }
         // the waves' sums: blocks of 32 columns in turn, b by wave b % 4
-        if (first == 0 && (int)threadIdx.x < count) ranks[threadIdx.x] = rank;
+        if (first == 0 && (int)threadIdx.x < count) {
+            ranks[threadIdx.x] = rank;
+            scales[threadIdx.x] = my_scale;
+        }
         lds_barrier();
 #pragma unroll
         for (int b = 0; b < CB; ++b)
@@ -552,7 +563,7 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
             if (lj >= rows) continue;
             const int64_t row = row0 + lj;
             const int p = place[lj];
-            const float scale = p < 0 || !g.scales ? 1.0f : gload(g.scales + list[p]);
+            const float scale = p < 0 ? 1.0f : scales[p];
             const int mine = p < 0 ? 0 : ranks[p];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -658,7 +669,7 @@ hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, 
     return p.r <= 32 ? launch_dt<Low<2, 6>>(p, prep, s) : launch_dt<Low<4, 4>>(p, prep, s);
 }
 
-hipError_t launch_adapters_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
+hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
     if (g.M > kAdapterFewGradRows) return hipErrorInvalidValue;
     // (a launch of its own costs some 4 us)
     if (x && tile_cost(kTile64, *x, false) > tile_cost(best_tile(*x, false), *x, false) + 4.0f) {
@@ -667,11 +678,19 @@ hipError_t launch_adapters_dx_grads(const AdapterProduct* x, const AdapterGrads&
         x = nullptr;
     }
     switch (plane_columns(g.r)) {
-        case 16: return launch_dx_grads<1>(x, g, s);
-        case 32: return launch_dx_grads<2>(x, g, s);
-        case 64: return launch_dx_grads<4>(x, g, s);
-        default: return launch_dx_grads<8>(x, g, s);
+        case 16: return launch_dx_grads<T64x64, 1>(x, g, 0, s);
+        case 32: return launch_dx_grads<T64x64, 2>(x, g, 0, s);
+        case 64: return launch_dx_grads<T64x64, 4>(x, g, 0, s);
+        default: return launch_dx_grads<T64x64, 8>(x, g, 0, s);
     }
+}
+
+bool adapters_dx_beside_grads(const AdapterProduct& x, const AdapterGrads& g) {
+    const float grads = 2.0f * (float)g.M * (float)((g.dA ? g.m : 0) + (g.dB ? g.n : 0)) / 4e6f;
+    return g.r <= 32 && tile_cost(kTile128x192, x, false) - tile_cost(best_tile(x, false), x, false) < 0.5f * grads;
+}
+hipError_t launch_adapters_dx_grad_pieces(const AdapterProduct& x, const AdapterGrads& g, int piece, hipStream_t s) {
+    return g.r <= 16 ? launch_dx_grads<T128x192, 1>(&x, g, piece, s) : launch_dx_grads<T128x192, 2>(&x, g, piece, s);
 }
 
 }  // namespace abt

@@ -171,9 +171,10 @@ int lr_adapters_bwd(const void* dY, const void* X, const float* T, const void* W
         g.dY = (const uint16_t*)dY; g.T_planes = p.T_planes; g.dA = dA; g.X = (const uint16_t*)X; g.dT_planes = p.dT_planes; g.dB = dB;
         g.order = prep.order; g.offsets = prep.offsets; g.partials = (float*)(ws + at.partials);
         g.M = M; g.m = (int)m; g.n = (int)n; g.r = (int)r; g.count = (int)count; g.accumulate = accumulate;
-        if (grads && M <= kAdapterFewGradRows) return launch_adapters_dx_grads(dX ? &x : nullptr, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
-        if (dX && launch_adapters_y(x, false, s) != hipSuccess) return ABT_EHIP;
-        if (grads && launch_adapters_grads(g, s) != hipSuccess) return ABT_EHIP;
+        if (grads && M <= kAdapterFewGradRows) return launch_adapters_few_dx_grads(dX ? &x : nullptr, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
+        const bool beside = dX && grads && adapters_dx_beside_grads(x, g);
+        if (dX && !beside && launch_adapters_y(x, false, s) != hipSuccess) return ABT_EHIP;
+        if (grads && launch_adapters_grads(g, beside ? &x : nullptr, s) != hipSuccess) return ABT_EHIP;
         return ABT_OK;
     });
 }

@@ -22,15 +22,15 @@ struct Grad {
     static constexpr int RP = 16 * VB, VROW = 3 * RP * 2;            // bytes of a row's planes
     static constexpr int upart = kPiece * 256, vpart = kPiece * VROW < 8192 ? 8192 : kPiece * VROW, slab = upart + vpart;
     static constexpr int NU = upart / 4096, NV = vpart / 4096, NL = NU + NV;       // load instructions per wave and slab
-    static constexpr int NS = VB == 8 ? 2 : VB == 4 ? 3 : 4;
-    static constexpr int list = 4096 * 4;                            // a piece's part of `order`
+    static constexpr int NS = VB == 1 || VB == 4 ? 3 : 2;           // up to VB = 2 two work-groups share a compute unit
+    static constexpr int list = 1024 * 4;                            // a piece's part of `order`
     static constexpr int lds = NS * slab + list;
     static_assert(lds <= 160 * 1024, "");
     // 16-byte chunks of a row change places so that the sixteen rows of a transposing load fall on all banks (32 bytes of each)
     static __device__ __forceinline__ int uswz(int row) { return (row & 7) << 1; }
     static __device__ __forceinline__ int vswz(int row) { return VB == 1 ? 0 : VB == 2 ? ((row >> 2) & 1) << 1 : VB == 4 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; }
 };
-constexpr int kMaxPiece = 4096;
+constexpr int kMaxPiece = 1024;
 
 struct Side { const uint16_t* U; const uint16_t* V; float* part; float* out; int cols, blocks; };
 

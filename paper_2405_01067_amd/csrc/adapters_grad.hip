@@ -2,6 +2,8 @@
 // dY or X and one piece, and leaves the sums of each adapter in it as a partial of its own (piece p and adapter a meet in slot p + a:
 // along the list either grows by one, so no two meetings share a slot).  A second launch adds an adapter's partials in order.
 // No atomics: the same call gives the same bits.
+#include <climits>
+
 #include "adapters_grad.h"
 
 namespace abt {
@@ -10,7 +12,8 @@ namespace {
 template <int VB>
 __global__ __launch_bounds__(256) void adapters_grad_kernel(const AdapterGrads g, const Side a, const Side b, int piece) {
     extern __shared__ __align__(1024) unsigned char lds[];
-    grad_block<VB>(g, a, b, blockIdx.x, piece, blockIdx.y, lds);
+    const int blocks = a.blocks + b.blocks;
+    grad_block<VB>(g, a, b, (int)blockIdx.x % blocks, piece, (int)blockIdx.x / blocks, lds);
 }
 
 // out[a] (+)= the partials of its pieces, in order; zeros for an adapter without rows
@@ -38,7 +41,7 @@ hipError_t launch_grads(const AdapterGrads& p, const Side& a, const Side& b, int
     static std::atomic<bool> attr_set{false};
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(&adapters_grad_kernel<VB>), L::lds, attr_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((adapters_grad_kernel<VB>), dim3((unsigned)(a.blocks + b.blocks), (unsigned)ceil_div(p.M, piece)), dim3(256), L::lds, s, p, a, b, piece);
+    hipLaunchKernelGGL((adapters_grad_kernel<VB>), dim3((unsigned)((a.blocks + b.blocks) * ceil_div(p.M, piece))), dim3(256), L::lds, s, p, a, b, piece);
     return hipGetLastError();
 }
 
@@ -54,15 +57,17 @@ size_t adapters_grad_partial_bytes(int64_t M, int m, int n, int r, int count) {
     return (size_t)(ceil_div(M, adapters_grad_piece(M, m, n)) + count) * (size_t)(m + n) * (size_t)r * 4;
 }
 
-hipError_t launch_adapters_grads(const AdapterGrads& p, hipStream_t s) {
+hipError_t launch_adapters_grads(const AdapterGrads& p, const AdapterProduct* x, hipStream_t s) {
     const int piece = adapters_grad_piece(p.M, p.m, p.n);
     const int64_t pieces = ceil_div(p.M, piece);
-    if (pieces > 65535 || p.count > 65535) return hipErrorInvalidValue;
+    if (p.count > 65535) return hipErrorInvalidValue;
     Side a, b;
     grad_sides(p, pieces + p.count, a, b);
     if (a.blocks + b.blocks == 0) return hipSuccess;
+    if ((a.blocks + b.blocks) * pieces > INT_MAX) return hipErrorInvalidValue;
     hipError_t e;
-    switch (plane_columns(p.r)) {
+    if (x) e = launch_adapters_dx_grad_pieces(*x, p, piece, s);
+    else switch (plane_columns(p.r)) {
         case 16: e = launch_grads<1>(p, a, b, piece, s); break;
         case 32: e = launch_grads<2>(p, a, b, piece, s); break;
         case 64: e = launch_grads<4>(p, a, b, piece, s); break;
