@@ -634,10 +634,11 @@ __global__ __launch_bounds__(256, 2) void adapters_t_kernel(const AdapterProduct
 
 // dT, and beside it what only later launches need
 template <class L>
-__global__ __launch_bounds__(256, 2) void adapters_dt_kernel(const AdapterProduct g, const AdapterPrep p, const PrepBlocks n) {
+__global__ __launch_bounds__(256, 2) void adapters_dt_kernel(const AdapterProduct g, const AdapterPrep p, const PrepBlocks n, int tiles) {
     extern __shared__ __align__(1024) unsigned char lds[];
-    if ((int)blockIdx.x < n.all) prepare(p, n, blockIdx.x, lds);
-    else t_tile<L, true>(g, (int)blockIdx.x - n.all, lds);
+    const int i = blockIdx.x, t = i - n.list;             // lists, tiles of dT, transposes
+    if (t >= 0 && t < tiles) t_tile<L, true>(g, t, lds);
+    else prepare(p, n, t < 0 ? i : i - tiles, lds);
 }
 
 template <class L>
@@ -657,7 +658,7 @@ hipError_t launch_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream
     const PrepBlocks n = prep_blocks(prep);
     const int64_t tiles = ceil_div(p.M, 32), blocks = tiles + n.all;
     if (blocks > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((adapters_dt_kernel<L>), dim3((unsigned)blocks), dim3(256), L::lds, s, p, prep, n);
+    hipLaunchKernelGGL((adapters_dt_kernel<L>), dim3((unsigned)blocks), dim3(256), L::lds, s, p, prep, n, (int)tiles);
     return hipGetLastError();
 }
 
