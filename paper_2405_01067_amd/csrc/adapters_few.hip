@@ -1,6 +1,6 @@
 // The layer with adapters for a few rows, as single tokens of many requests are: T_i = B_a x_i, then Y_i = W x_i + A_a T_i.
 // Little is reused, so the operands go from memory to registers.  Two launches:
-//   first    T beside the dense product.  T: a work-group per row and sixteen of its rank's rows of B, two rows a wave.  The dense product: 64 columns, up to
+//   first    T beside the dense product.  T: a work-group per row and eight of its rank's rows of B, one a wave.  The dense product: 64 columns, up to
 //            64 rows and a part of the contraction, which eight waves share out, 128 bytes of every row at a time; with 16 columns and the whole
 //            contraction per work-group the rows of X, read by every work-group, were several times the bytes of W.
 //   second   adds the parts in order, and the adapters: 16 columns a work-group, eight waves that share out the adapters of the rows.
@@ -32,61 +32,56 @@ __device__ __forceinline__ u32x4 first_of(u32x4 v, int valid) {
     return v;
 }
 
-// T of one row: rows j0, j0 + 1 of its adapter's B by each wave
-__device__ __forceinline__ void t_of_row(const AdapterProduct& g, const uint16_t* X, const uint16_t* B, int n, int64_t row, int j0) {
+// T of one row: row j of its adapter's B by each wave
+__device__ __forceinline__ void t_of_row(const AdapterProduct& g, const uint16_t* X, const uint16_t* B, int n, int64_t row, int j) {
     const int lane = threadIdx.x & 63;
-    if (j0 >= g.r) return;
+    if (j >= g.r) return;
     const int a = __builtin_amdgcn_readfirstlane(gload(g.row_adapter + row));
     const bool have = a >= 0 && a < g.count;
-    float sum[2] = {0.0f, 0.0f};
+    float sum = 0.0f, s = 1.0f;
     int rank = 0;
     if (have) {
         // (rows past the rank are there: they are read beside the rank and not used)
         const int k = g.ranks ? gload(g.ranks + a) : g.r;
+        if (g.scales) s = gload(g.scales + a);
         const uint16_t* const x = X + row * n;
-        const uint16_t* const b = B + ((int64_t)a * g.r + j0) * n;
-        float other[2] = {0.0f, 0.0f};
-        const auto add = [&](u32x4 xv, u32x4 b0, u32x4 b1) {
+        const uint16_t* const b = B + ((int64_t)a * g.r + j) * n;
+        float other = 0.0f;
+        const auto add = [&](u32x4 xv, u32x4 bv) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                sum[0] += lo(xv[i]) * lo(b0[i]);
-                other[0] += hi(xv[i]) * hi(b0[i]);
-                sum[1] += lo(xv[i]) * lo(b1[i]);
-                other[1] += hi(xv[i]) * hi(b1[i]);
+                sum += lo(xv[i]) * lo(bv[i]);
+                other += hi(xv[i]) * hi(bv[i]);
             }
         };
         const auto at = [&](const uint16_t* p, int c) { return gload(reinterpret_cast<const u32x4*>(p + c)); };
         int c = lane * 8;
-        for (; c + 1536 < n; c += 2048) {                 // four pieces on their way at a time
-            u32x4 v[4][3];
+        for (; c + 3584 < n; c += 4096) {                 // eight pieces on their way at a time
+            u32x4 v[8][2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i][0] = at(x, c + 512 * i); v[i][1] = at(b, c + 512 * i); v[i][2] = at(b + n, c + 512 * i); }
+            for (int i = 0; i < 8; ++i) { v[i][0] = at(x, c + 512 * i); v[i][1] = at(b, c + 512 * i); }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) add(v[i][0], v[i][1], v[i][2]);
+            for (int i = 0; i < 8; ++i) add(v[i][0], v[i][1]);
         }
-        for (; c < n; c += 512) add(at(x, c), at(b, c), at(b + n, c));
-        sum[0] += other[0];
-        sum[1] += other[1];
-#pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            sum[0] += __shfl_xor(sum[0], d);
-            sum[1] += __shfl_xor(sum[1], d);
+        for (; c + 512 < n; c += 1024) {
+            const u32x4 x0 = at(x, c), b0 = at(b, c), x1 = at(x, c + 512), b1 = at(b, c + 512);
+            add(x0, b0);
+            add(x1, b1);
         }
+        if (c < n) add(at(x, c), at(b, c));
+        sum += other;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
         rank = k > g.r ? g.r : k;
-        if (j0 >= rank) sum[0] = 0.0f;
-        if (j0 + 1 >= rank) sum[1] = 0.0f;
+        if (j >= rank) sum = 0.0f;
     }
     if (lane) return;
-    const float s = have && g.scales ? gload(g.scales + a) : 1.0f;
-    if (g.T) {
-        gstore(g.T + row * g.r + j0, sum[0]);
-        gstore(g.T + row * g.r + j0 + 1, sum[1]);
-    }
+    if (g.T) gstore(g.T + row * g.r + j, sum);
     // what is past the rank is zero whatever the scale
-    if (g.Tb) gstore(reinterpret_cast<uint32_t*>(g.Tb + row * g.r + j0), pack2_bf16(j0 < rank ? s * sum[0] : 0.0f, j0 + 1 < rank ? s * sum[1] : 0.0f));
+    if (g.Tb) gstore(g.Tb + row * g.r + j, (uint16_t)(pack2_bf16(j < rank ? s * sum : 0.0f, 0.0f) & 0xffffu));
 }
 
-struct FewParts { int col_blocks, row_groups, splits, units; float* sums; const uint16_t* X; const uint16_t* B; };   // X as the adapters see it
+struct FewParts { int col_blocks, blocks16, row_groups, splits, units; float* sums; const uint16_t* X; const uint16_t* B; };   // X as the adapters see it
 
 // RB blocks of 16 rows
 template <int RB, bool F8>
@@ -98,8 +93,8 @@ __global__ __launch_bounds__(512) void few_first_kernel(const AdapterProduct g, 
     int w = blockIdx.x;
     if (w >= nbase) {
         w -= nbase;
-        const int per = (g.r + 15) / 16;
-        t_of_row(g, f.X, f.B, g.kmain, w / per, (w % per) * 16 + 2 * wave);
+        const int per = g.r / 8;
+        t_of_row(g, f.X, f.B, g.kmain, w / per, (w % per) * 8 + wave);
         return;
     }
     const int cb = w % f.col_blocks;
@@ -153,11 +148,12 @@ __global__ __launch_bounds__(512) void few_first_kernel(const AdapterProduct g, 
 #pragma unroll
         for (int t = 0; t < RB * CB; ++t) at(wave, t) = acc[t / CB][t % CB] + at(wave, t);
     __syncthreads();
-    float* const out = f.sums + (int64_t)split * g.M * g.Q;
+    // parts lie as [split][16 columns][row]: whole lines for whoever stores or adds them
+    float* const out = f.sums + (int64_t)split * f.blocks16 * g.M * 16;
     for (int t = wave; t < RB * CB; t += 8) {
         const f32x4 v = (at(0, t) + at(1, t)) + (at(2, t) + at(3, t));
         const int row = 16 * (t / CB) + li, c = 16 * (t % CB) + 4 * lq;      // lane: row li of the block, four columns
-        if (row < rows && c < cols) gstore(reinterpret_cast<f32x4*>(out + (int64_t)(row0 + row) * g.Q + col0 + c), v);
+        if (row < rows && c < cols) gstore(reinterpret_cast<f32x4*>(out + ((int64_t)(cb * CB + t % CB) * g.M + row0 + row) * 16 + 4 * lq), v);
     }
 }
 
@@ -175,9 +171,16 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
     f32x4 v = {0, 0, 0, 0};
     float xs = 1.0f, ws[4] = {1.0f, 1.0f, 1.0f, 1.0f};
     if (out) {
-        const float* const from = f.sums + (int64_t)(row0 + row) * g.Q + col0 + c0;
-        const int64_t step = g.M * g.Q;
-        for (int s = 0; s < f.splits; ++s) v += gload(reinterpret_cast<const f32x4*>(from + s * step));
+        const float* const from = f.sums + ((int64_t)blockIdx.x * g.M + row0 + row) * 16 + c0;
+        const int64_t step = (int64_t)f.blocks16 * g.M * 16;
+        for (int s = 0; s < f.splits; s += 4) {           // four on their way at a time
+            f32x4 part[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[i] = gload(reinterpret_cast<const f32x4*>(from + (s + i < f.splits ? s + i : s) * step));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s + i < f.splits) v += part[i];
+        }
         if constexpr (F8) {
             xs = gload(g.x_scale + row0 + row);
 #pragma unroll
@@ -246,6 +249,7 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
 FewParts few_parts(int64_t M, int Q, int n, bool fp8) {
     FewParts f{};
     f.col_blocks = (Q + 63) / 64;
+    f.blocks16 = (Q + 15) / 16;
     f.row_groups = (int)((M + 63) / 64);
     const int units = (n * (fp8 ? 1 : 2) + 127) / 128;
     // one work-group per compute unit, but for each of its eight waves at least one unit
@@ -260,7 +264,7 @@ FewParts few_parts(int64_t M, int Q, int n, bool fp8) {
 
 template <bool F8>
 hipError_t few(const AdapterProduct& p, const FewParts& f, hipStream_t s) {
-    const dim3 first((unsigned)(f.col_blocks * f.row_groups * f.splits + p.M * ((p.r + 15) / 16))), second((unsigned)ceil_div(p.Q, 16), (unsigned)f.row_groups);
+    const dim3 first((unsigned)(f.col_blocks * f.row_groups * f.splits + p.M * (p.r / 8))), second((unsigned)ceil_div(p.Q, 16), (unsigned)f.row_groups);
     const auto launch = [&](auto rb) {
         constexpr int RB = decltype(rb)::value;
         hipLaunchKernelGGL((few_first_kernel<RB, F8>), first, dim3(512), 0, s, p, f);
@@ -279,7 +283,7 @@ hipError_t few(const AdapterProduct& p, const FewParts& f, hipStream_t s) {
 
 size_t adapters_few_sums_bytes(int64_t M, int m, int n) {
     const int s8 = few_parts(M, m, n, true).splits, s16 = few_parts(M, m, n, false).splits;
-    return (size_t)(s8 > s16 ? s8 : s16) * (size_t)M * (size_t)m * 4;
+    return (size_t)(s8 > s16 ? s8 : s16) * (size_t)M * align_up((size_t)m, 16) * 4;
 }
 
 hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s) {
