@@ -4,6 +4,7 @@
 //            64 rows and a part of the contraction, which eight waves share out, 128 bytes of every row at a time; with 16 columns and the whole
 //            contraction per work-group the rows of X, read by every work-group, were several times the bytes of W.
 //   second   adds the parts in order, and the adapters: 16 columns a work-group, eight waves that share out the adapters of the rows.
+// A row or two of narrow adapters go in one launch.
 // Bound by the bytes of W and of the adapters in use, and by the latency of two launches where these are few.
 #include <type_traits>
 
@@ -246,6 +247,118 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
     gstore(reinterpret_cast<u32x2*>(g.Y + (int64_t)(row0 + row) * g.Q + col0 + c0), u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])});
 }
 
+// One launch where there is next to nothing to share: up to sixteen rows and 32 values of T in all, which every work-group computes for itself.  16
+// columns a work-group, whose eight waves share out the contraction, the values of T and the adapters.
+constexpr int kOneT = 32, kOnePitch = 136;               // values of T; LDS values per row of T, rank columns and zeros behind them
+template <bool F8>
+__global__ __launch_bounds__(512) void few_one_kernel(const AdapterProduct g, const uint16_t* X, const uint16_t* B) {
+    __shared__ __align__(16) f32x4 sums[8 * 64];
+    __shared__ __align__(16) uint16_t ts[16 * kOnePitch];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 15, lq = lane >> 4;
+    const int M = (int)g.M, n = g.kmain, r = g.r;
+    const int col0 = blockIdx.x * 16, cols = g.Q - col0 < 16 ? g.Q - col0 : 16;
+    const int id0 = gload(g.row_adapter + (lane < M ? lane : 0));
+    for (int i = threadIdx.x; i < 16 * kOnePitch / 8; i += 512) *reinterpret_cast<u32x4*>(ts + 8 * i) = u32x4{0, 0, 0, 0};
+    const int id = lane < M && id0 >= 0 && id0 < g.count ? id0 : -1;
+    const int rank0 = g.ranks && id >= 0 ? gload(g.ranks + id) : r;
+    const float scale0 = g.scales && id >= 0 ? gload(g.scales + id) : 1.0f;
+    // T: values wave, wave + 8, .., value v is column v % r of row v / r
+    float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uint16_t *xp[4], *bp[4];
+    bool have[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int v = wave + 8 * i, row = v / r;
+        const int a = row < M ? __builtin_amdgcn_readlane(id, row < 16 ? row : 0) : -1;
+        have[i] = a >= 0;
+        xp[i] = X + (int64_t)(have[i] ? row : 0) * n;
+        bp[i] = B + ((int64_t)(have[i] ? a : 0) * r + (v - row * r)) * n;
+    }
+#pragma unroll 2
+    for (int c = lane * 8; c < n; c += 512) {
+        u32x4 x[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (have[i]) {
+                x[i] = gload(reinterpret_cast<const u32x4*>(xp[i] + c));
+                b[i] = gload(reinterpret_cast<const u32x4*>(bp[i] + c));
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (have[i])
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    t[i] += lo(x[i][k]) * lo(b[i][k]);
+                    t[i] += hi(x[i][k]) * hi(b[i][k]);
+                }
+    }
+    // the dense product, 128 bytes of every row at a time
+    const int bytes = n * (F8 ? 1 : 2), units = (bytes + 127) / 128;
+    const rsrc_t xres = make_rsrc(g.X, (int64_t)M * bytes), wres = make_rsrc((const char*)g.W + (int64_t)col0 * bytes, (int64_t)cols * bytes);
+    f32x4 acc = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int u = wave; u < units; u += 8) {
+        const int at0 = u * 128 + lq * 16, at1 = at0 + 64;
+        const u32x4 w0 = buf_load16(wres, at0 < bytes ? li * bytes + at0 : kBufNowhere, 0), w1 = buf_load16(wres, at1 < bytes ? li * bytes + at1 : kBufNowhere, 0);
+        const u32x4 x0 = buf_load16(xres, at0 < bytes ? li * bytes + at0 : kBufNowhere, 0), x1 = buf_load16(xres, at1 < bytes ? li * bytes + at1 : kBufNowhere, 0);
+        if constexpr (F8) {
+            acc = mfma16_f8(w0, w1, x0, x1, acc);
+        } else {
+            acc = mfma16(w0, x0, acc);
+            acc = mfma16(w1, x1, acc);
+        }
+    }
+    if constexpr (F8) {
+        const float xs = gload(g.x_scale + (li < M ? li : 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= xs * (4 * lq < cols ? gload(g.w_scale + col0 + 4 * lq + i) : 0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 32; d; d >>= 1) t[i] += __shfl_xor(t[i], d);
+    __syncthreads();                                      // (the zeros are there)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int v = wave + 8 * i, row = v / r, j = v - row * r;
+        if (row >= M) break;
+        const bool in = j < __builtin_amdgcn_readlane(rank0, row) && have[i];
+        const float value = in ? t[i] : 0.0f;
+        if (lane == 0) {
+            if (g.T && blockIdx.x == 0) gstore(g.T + (int64_t)row * r + j, value);
+            if (in) ts[row * kOnePitch + j] = (uint16_t)(pack2_bf16(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale0), row)) * value, 0.0f) & 0xffffu);
+        }
+    }
+    __syncthreads();
+    // the adapters of the rows, every eighth by this wave
+    uint64_t left = __ballot(id >= 0);
+    for (int k = 0; left; ++k) {
+        const int first = __builtin_ctzll(left), a = __builtin_amdgcn_readlane(id, first), rank = __builtin_amdgcn_readlane(rank0, first);
+        const uint64_t same = __ballot(id == a);
+        left &= ~same;
+        if ((k & 7) != wave) continue;
+        const rsrc_t fres = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * r, (int64_t)cols * r * 2);
+        for (int j = 0; j < r; j += 32) {
+            const int c = j + lq * 8;
+            const u32x4 f = first_of(buf_load16(fres, c < r ? (li * r + c) * 2 : kBufNowhere, 0), rank - c);
+            const u32x4 e = (same >> li) & 1 ? *reinterpret_cast<const u32x4*>(ts + li * kOnePitch + c) : u32x4{0, 0, 0, 0};
+            acc = mfma16(f, e, acc);
+        }
+    }
+    sums[wave * 64 + lane] = acc;
+    __syncthreads();
+    if (wave || li >= M || 4 * lq >= cols) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) acc += sums[w * 64 + lane];
+    gstore(reinterpret_cast<u32x2*>(g.Y + (int64_t)li * g.Q + col0 + 4 * lq), u32x2{pack2_bf16(acc[0], acc[1]), pack2_bf16(acc[2], acc[3])});
+}
+// Where the contraction is so short that its parts are not missed.  us, one launch / two, rows of W 768 x 768 5.9 / 7.2 (one row, r = 16) and 6.5 / 7.2 (two), 2304 x
+// 768 6.8 / 7.4 (two); 4096 x 2048 in 8 bits 8.3 / 8.4 (two), 4096 x 4096 15.3 / 13.3 and in 8 bits 11.7 / 9.6 (one).
+bool few_in_one(const AdapterProduct& p, bool fp8) {
+    return p.M <= 16 && p.M * p.r <= kOneT && (int64_t)p.kmain * (fp8 ? 1 : 2) <= 3072;
+}
+
 FewParts few_parts(int64_t M, int Q, int n, bool fp8) {
     FewParts f{};
     f.col_blocks = (Q + 63) / 64;
@@ -288,6 +401,12 @@ size_t adapters_few_sums_bytes(int64_t M, int m, int n) {
 
 hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s) {
     if (p.M > kAdapterFewRows || p.e_pitch != p.r || p.ke != p.r) return hipErrorInvalidValue;
+    if (few_in_one(p, fp8)) {
+        const dim3 grid((unsigned)ceil_div(p.Q, 16));
+        if (fp8) hipLaunchKernelGGL(few_one_kernel<true>, grid, dim3(512), 0, s, p, X, B);
+        else hipLaunchKernelGGL(few_one_kernel<false>, grid, dim3(512), 0, s, p, X, B);
+        return hipGetLastError();
+    }
     FewParts f = few_parts(p.M, p.Q, p.kmain, fp8);
     f.sums = sums; f.X = X; f.B = B;
     return fp8 ? few<true>(p, f, s) : few<false>(p, f, s);
