@@ -192,7 +192,7 @@ int lr_rms_norm_fwd(const void* X, const void* residual, const float* gain, doub
 
 size_t lr_rms_norm_bwd_workspace_bytes(int64_t M, int64_t n, int dt) {
     if (M < 1 || n < 8 || n % 8 || n > ABT_RMS_NORM_MAX_WIDTH || M > INT_MAX || (dt != ABT_F32 && dt != ABT_BF16)) return 0;
-    return align_up((size_t)rms_norm_bwd_blocks(M, (int)n) * (size_t)n * 4, 256);
+    return align_up((size_t)rms_norm_bwd_blocks(M, (int)n, dt == ABT_BF16) * (size_t)n * 4, 256);
 }
 
 int lr_rms_norm_bwd(const void* dY, const void* H, const float* gain, double eps, const void* dH, void* dX, float* dgain,

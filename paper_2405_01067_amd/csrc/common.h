@@ -344,7 +344,7 @@ hipError_t launch_grad_clip(const GradTensor* t, int n, const double* sums, int 
 hipError_t launch_rms_norm_fwd(const void* X, const void* R, const float* gain, float eps, void* H, void* Y, void* Yq, float* scale, int64_t M, int n, bool bf16,
                                hipStream_t s);
 // sums: rms_norm_bwd_blocks * n values, where dgain is wanted; dH, dX, dgain may be NULL
-int rms_norm_bwd_blocks(int64_t M, int n);
+int rms_norm_bwd_blocks(int64_t M, int n, bool bf16);
 hipError_t launch_rms_norm_bwd(const void* dY, const void* H, const float* gain, float eps, const void* dH, void* dX, float* dgain, float* sums, int64_t M, int n,
                                bool bf16, int accumulate, hipStream_t s);
 

@@ -2,7 +2,7 @@
 //     h = x + res,  s = (mean h^2 + eps)^(-1/2),  y = h s g           also q ~ y / scale in 8-bit floats, scale = max |y| / 448
 //     dX = dH + s (dY g - h s^2 mean(dY g h)),  dg = sum over rows of dY h s
 // A row stays in registers from its one read to its last write: one wave per row up to 2048 columns, a work-group of four
-// waves per row beyond.  The backward forms s again from h, which it has in registers anyway, so the forward keeps nothing for it.
+// waves per row beyond (two waves in a range of the backward).  The backward forms s again from h, which it has in registers anyway, so the forward keeps nothing for it.
 // Statistics and gradients of the gain are fp32; y is formed from h before h is rounded.  Bound by memory.
 #include <type_traits>
 
@@ -36,8 +36,9 @@ __device__ __forceinline__ void store8(uint16_t* p, f32x8 v) {
 }
 
 constexpr int kNormThreads = 256;
+constexpr int kNormBlocks = 1 << 23;                       // of a launch, which has fewer than 2^32 threads
 
-// Sum or largest value over the lanes of a row: a wave (WPR = 1) or the four waves of the work-group, in a fixed order.
+// Sum or largest value over the lanes of a row: WPR waves of the work-group, in a fixed order.
 template <int WPR, bool MAX>
 __device__ __forceinline__ float over_row(float v, float* part) {
 #pragma unroll
@@ -49,7 +50,9 @@ __device__ __forceinline__ float over_row(float v, float* part) {
         __syncthreads();                                  // (the values of the call before have been read)
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = MAX ? fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) : (part[0] + part[1]) + (part[2] + part[3]);
+        const float* const p = part + (WPR == 2 ? threadIdx.x >> 7 << 1 : 0);
+        v = MAX ? fmaxf(p[0], p[1]) : p[0] + p[1];
+        if constexpr (WPR == 4) v = MAX ? fmaxf(v, fmaxf(p[2], p[3])) : v + (p[2] + p[3]);
     }
     return v;
 }
@@ -59,9 +62,9 @@ template <class T, int WPR, int V, bool Q8>
 __global__ __launch_bounds__(kNormThreads) void rms_norm_fwd_kernel(const T* X, const T* R, const float* gain, float eps, T* H, T* Y, uint8_t* Yq, float* scale,
                                                                     int64_t M, int n) {
     __shared__ float part[4];
-    const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + (WPR == 1 ? threadIdx.x >> 6 : 0);
+    const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / (64 * WPR);
     if (row >= M) return;                                 // whole waves; whole work-groups where they share a row
-    const int l = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int l = threadIdx.x % (64 * WPR);
     f32x8 h[V], g[V];
     const int64_t base = row * n;
 #pragma unroll
@@ -123,8 +126,9 @@ template <class T, int WPR, int V>
 __global__ __launch_bounds__(kNormThreads) void rms_norm_bwd_kernel(const T* dY, const T* Hin, const float* gain, float eps, const T* dH, T* dX, float* sums,
                                                                     int64_t M, int n) {
     __shared__ float part[4];
-    __shared__ __align__(16) float rows_of[WPR == 1 ? 3 * 512 * V : 4];
-    const int wave = threadIdx.x >> 6, l = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int RPB = 4 / WPR;
+    __shared__ __align__(16) float rows_of[RPB > 1 ? (RPB - 1) * 512 * WPR * V : 4];
+    const int sub = threadIdx.x / (64 * WPR), l = threadIdx.x % (64 * WPR);
     f32x8 dg[V], g[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -132,14 +136,14 @@ __global__ __launch_bounds__(kNormThreads) void rms_norm_bwd_kernel(const T* dY,
         dg[i] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
         g[i] = c < n ? load8(gain + c) : dg[i];
     }
-    constexpr int RPB = 4 / WPR;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + (WPR == 1 ? wave : 0); row < M; row += (int64_t)gridDim.x * RPB) {
-        const int64_t base = row * n;
+    for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < M; row0 += (int64_t)gridDim.x * RPB) {
+        const int64_t base = (row0 + sub) * n;
+        const int cols = row0 + sub < M ? n : 0;          // all rows of the work-group meet at the barriers, also one that is not there
         f32x8 h[V], u[V], r[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = (l + 64 * WPR * i) * 8;
-            if (c < n) {
+            if (c < cols) {
                 h[i] = load8(Hin + base + c);
                 u[i] = load8(dY + base + c);
                 if (dH) r[i] = load8(dH + base + c);
@@ -147,7 +151,7 @@ __global__ __launch_bounds__(kNormThreads) void rms_norm_bwd_kernel(const T* dY,
                 h[i] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
                 u[i] = h[i];
             }
-            if (!(c < n && dH)) r[i] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+            if (!(c < cols && dH)) r[i] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
         }
         float hh = 0.0f, uh = 0.0f;
 #pragma unroll
@@ -170,27 +174,27 @@ __global__ __launch_bounds__(kNormThreads) void rms_norm_bwd_kernel(const T* dY,
                 o[j] = r[i][j] + s * (u[i][j] * g[i][j] - k * h[i][j]);
                 dg[i][j] += u[i][j] * (h[i][j] * s);
             }
-            if (c < n && dX) store8(dX + base + c, o);
+            if (c < cols && dX) store8(dX + base + c, o);
         }
     }
     if (!sums) return;
-    if constexpr (WPR == 1) {                             // the four waves' sums, in order
+    if constexpr (RPB > 1) {                              // the sums of the work-group's rows, in order
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (wave)
+            if (sub)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    *reinterpret_cast<f32x4*>(rows_of + ((wave - 1) * V + i) * 512 + j * 256 + l * 4) =
+                    *reinterpret_cast<f32x4*>(rows_of + (((sub - 1) * V + i) * 2 + j) * 256 * WPR + l * 4) =
                         f32x4{dg[i][4 * j], dg[i][4 * j + 1], dg[i][4 * j + 2], dg[i][4 * j + 3]};
         __syncthreads();
-        if (wave) return;
+        if (sub) return;
 #pragma unroll
-        for (int w = 0; w < 3; ++w)
+        for (int w = 0; w < RPB - 1; ++w)
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const f32x4 v = *reinterpret_cast<const f32x4*>(rows_of + (w * V + i) * 512 + j * 256 + l * 4);
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(rows_of + ((w * V + i) * 2 + j) * 256 * WPR + l * 4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) dg[i][4 * j + e] += v[e];
                 }
@@ -226,10 +230,11 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* sums, in
     gstore(out + c, accumulate ? gload(out + c) + v : v);
 }
 
-// f(waves per row, pieces per lane) as constants
+// f(waves per row, pieces per lane) as constants; pairs: two waves per row where n is more than 2048 and at most 4096
 template <class F>
-hipError_t by_width(int n, F&& f) {
+hipError_t by_width(int n, bool pairs, F&& f) {
     const auto c = [](auto v) { return v; };
+    if (pairs) return n <= 3072 ? f(std::integral_constant<int, 2>{}, c(std::integral_constant<int, 3>{})) : f(std::integral_constant<int, 2>{}, c(std::integral_constant<int, 4>{}));
     if (n <= 2048) {
         switch ((n + 511) / 512) {
             case 1: return f(std::integral_constant<int, 1>{}, c(std::integral_constant<int, 1>{}));
@@ -249,22 +254,32 @@ hipError_t by_width(int n, F&& f) {
 
 template <class T>
 hipError_t fwd(const void* X, const void* R, const float* gain, float eps, void* H, void* Y, void* Yq, float* scale, int64_t M, int n, hipStream_t s) {
-    return by_width(n, [&](auto wpr, auto v) {
+    return by_width(n, false, [&](auto wpr, auto v) {
         constexpr int W = decltype(wpr)::value, V = decltype(v)::value;
-        const dim3 grid((unsigned)ceil_div(M, 4 / W));
-        if (Yq) hipLaunchKernelGGL((rms_norm_fwd_kernel<T, W, V, true>), grid, dim3(kNormThreads), 0, s, (const T*)X, (const T*)R, gain, eps, (T*)H, (T*)Y,
-                                   (uint8_t*)Yq, scale, M, n);
-        else hipLaunchKernelGGL((rms_norm_fwd_kernel<T, W, V, false>), grid, dim3(kNormThreads), 0, s, (const T*)X, (const T*)R, gain, eps, (T*)H, (T*)Y,
-                                nullptr, nullptr, M, n);
-        return hipGetLastError();
+        const auto from = [&](auto* p, int64_t at) { return p ? p + at : p; };
+        for (int64_t row = 0; row < M; row += (int64_t)kNormBlocks * (4 / W)) {
+            const int64_t rows = M - row < (int64_t)kNormBlocks * (4 / W) ? M - row : (int64_t)kNormBlocks * (4 / W), at = row * n;
+            const dim3 grid((unsigned)ceil_div(rows, 4 / W));
+            if (Yq) hipLaunchKernelGGL((rms_norm_fwd_kernel<T, W, V, true>), grid, dim3(kNormThreads), 0, s, from((const T*)X, at), from((const T*)R, at), gain, eps,
+                                       from((T*)H, at), from((T*)Y, at), (uint8_t*)Yq + at, scale + row, rows, n);
+            else hipLaunchKernelGGL((rms_norm_fwd_kernel<T, W, V, false>), grid, dim3(kNormThreads), 0, s, from((const T*)X, at), from((const T*)R, at), gain, eps,
+                                    from((T*)H, at), from((T*)Y, at), nullptr, nullptr, rows, n);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     });
 }
 
 }  // namespace
 
-// One row per wave or work-group up to two work-groups per compute unit, beyond several
-int rms_norm_bwd_blocks(int64_t M, int n) {
-    const int64_t b = n <= 2048 ? ceil_div(M, 4) : M;
+// Two waves per row in the backward of many rows of bf16: fewer rounds of the 512 work-groups.  us, two / four waves: 600 x 2304 9.1 / 10.5, 4096 x 2304 19.2 / 22.2,
+// 12608 x 2304 43.3 / 51.9, 8190 x 4096 39.0 / 43.0; but 48 x 4096 7.4 / 6.5, fp32 2100 x 3000 21.9 / 20.9 and 8190 x 4096 82.7 / 76.2, and the
+// forward, whose grid is not bounded, 8190 x 4096 44.2 / 40.5.
+static bool row_pairs(int64_t M, int n, bool bf16) { return bf16 && M > 512 && n > 2048 && n <= 4096; }
+// One row per wave, pair or work-group up to two work-groups per compute unit, beyond several
+int rms_norm_bwd_blocks(int64_t M, int n, bool bf16) {
+    const int64_t b = ceil_div(M, n <= 2048 ? 4 : row_pairs(M, n, bf16) ? 2 : 1);
     return (int)(b < 512 ? b : 512);
 }
 
@@ -275,13 +290,13 @@ hipError_t launch_rms_norm_fwd(const void* X, const void* R, const float* gain, 
 
 hipError_t launch_rms_norm_bwd(const void* dY, const void* H, const float* gain, float eps, const void* dH, void* dX, float* dgain, float* sums, int64_t M, int n,
                                bool bf16, int accumulate, hipStream_t s) {
-    const int blocks = rms_norm_bwd_blocks(M, n);
+    const int blocks = rms_norm_bwd_blocks(M, n, bf16);
     float* const to = dgain ? sums : nullptr;
-    const hipError_t e = by_width(n, [&](auto wpr, auto v) {
+    const hipError_t e = by_width(n, row_pairs(M, n, bf16), [&](auto wpr, auto v) {
         constexpr int W = decltype(wpr)::value, V = decltype(v)::value;
-        if (bf16) hipLaunchKernelGGL((rms_norm_bwd_kernel<uint16_t, W, V>), dim3((unsigned)blocks), dim3(kNormThreads), 0, s, (const uint16_t*)dY,
+        if (bf16 || W == 2) hipLaunchKernelGGL((rms_norm_bwd_kernel<uint16_t, W, V>), dim3((unsigned)blocks), dim3(kNormThreads), 0, s, (const uint16_t*)dY,
                                      (const uint16_t*)H, gain, eps, (const uint16_t*)dH, (uint16_t*)dX, to, M, n);
-        else hipLaunchKernelGGL((rms_norm_bwd_kernel<float, W, V>), dim3((unsigned)blocks), dim3(kNormThreads), 0, s, (const float*)dY, (const float*)H, gain,
+        else if constexpr (W != 2) hipLaunchKernelGGL((rms_norm_bwd_kernel<float, W, V>), dim3((unsigned)blocks), dim3(kNormThreads), 0, s, (const float*)dY, (const float*)H, gain,
                                 eps, (const float*)dH, (float*)dX, to, M, n);
         return hipGetLastError();
     });
