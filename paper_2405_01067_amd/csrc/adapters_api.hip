@@ -11,12 +11,12 @@ using namespace abt;
 
 namespace {
 
-constexpr int64_t kMaxWidth = 1 << 20;
+constexpr int64_t kMaxWidth = 1 << 20, kMaxRows = 1 << 28;     // (launches have fewer than 2^32 threads)
 
 // columns: what m and n are multiples of
 int check_adapters(const abt_adapters* ad, const int32_t* row_adapter, int64_t M, int64_t m, int64_t n, int columns) {
     if (!ad || !ad->A || !ad->B || !row_adapter) return ABT_EINVAL;
-    if (M < 1 || M > INT_MAX || m < 1 || n < 1 || m > kMaxWidth || n > kMaxWidth || m % 8 || n % columns) return ABT_ESHAPE;
+    if (M < 1 || M > kMaxRows || m < 1 || n < 1 || m > kMaxWidth || n > kMaxWidth || m % 8 || n % columns) return ABT_ESHAPE;
     if (ad->count < 1 || ad->count > 65535 || ad->r < 8 || ad->r > ABT_ADAPTERS_MAX_RANK || ad->r % 8) return ABT_ESHAPE;
     if (!aligned(ad->A, 16) || !aligned(ad->B, 16) || !aligned(ad->ranks, 4) || !aligned(ad->scales, 4) || !aligned(row_adapter, 4)) return ABT_EALIGN;
     return ABT_OK;
@@ -98,7 +98,7 @@ int check_grad_tensors(const abt_grad_tensor* tensors, int n, bool with_out, std
 extern "C" {
 
 size_t lr_adapters_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n, int64_t r, int64_t count) {
-    if (M < 1 || M > INT_MAX || m < 1 || m > kMaxWidth || m % 8 || n < 1 || n > kMaxWidth || n % 8 || r < 8 || r > ABT_ADAPTERS_MAX_RANK || r % 8 || count < 1 || count > 65535)
+    if (M < 1 || M > kMaxRows || m < 1 || m > kMaxWidth || m % 8 || n < 1 || n > kMaxWidth || n % 8 || r < 8 || r > ABT_ADAPTERS_MAX_RANK || r % 8 || count < 1 || count > 65535)
         return 0;
     return t_bytes(M, r) + (M <= kAdapterFewRows ? align_up(adapters_few_sums_bytes(M, (int)m, (int)n), 256) : 0);
 }
