@@ -392,23 +392,28 @@ hipError_t launch_dx_grads(const AdapterProduct* x, const AdapterGrads& g, int p
 }
 
 // ------------------------------------------------------------------------------------------ T
-// 32 rows a work-group; its four waves share out the four steps of a slab and add their sums at the end, in order.  CB blocks of 32 columns hold
-// 32 CB / r adapters; rows of more adapters than that take another pass over their x.
-// PLANES: the backward's dT_i = A_a^T dY_i.  A lies with the contraction first, [m, r]: slabs of 64 rows of the adapters' A, one behind the other as they lie
+// 32 rows a work-group.  A slab is two parts of 64 columns; the four waves share out the four steps of a part and add their sums at the end, in order.  CB blocks of
+// 32 columns hold 32 CB / r adapters; rows of more adapters than that take another pass over their x.
+// PLANES: the backward's dT_i = A_a^T dY_i.  A lies with the contraction first, [m, r]: parts of 64 rows of the adapters' A, one behind the other as they lie
 // in memory, read with the transposing load.
+// Bound by memory where there are many rows and one adapter or two in 32 of them, otherwise by latency: 5 us for the first load, the sums and the launch, then
+// 0.14 us (r = 16 or 32) to 0.22 us (112) a part of 64 columns while only one work-group shares the compute unit.  One part per slab, each read followed by its
+// product, took 0.19 to 0.27 us.  us, T / dT: 12608 rows of 768 in runs of 64, r = 32: 12.2 / 14.0 (one part: 13.3 / 16.4), r = 128: 33.6 / 47.6 (36.4 /
+// 59.2); 1379 x 768, r = 32, runs of 7: 12.7 / 16.0 (14.2 / 19.0); 8190 x 4096, r = 32, one adapter: 21.6 / 20.9, 3.1 TB/s (21.9 / 23.8).
 template <int CB_, int NS_>
 struct Low {
-    static constexpr int CB = CB_, NS = NS_, TN = 32 * CB;
-    static constexpr int xpart = 4096, slab = xpart + TN * 128, NF = CB, NL = 1 + NF;
+    static constexpr int CB = CB_, KS = 2, NS = NS_, TN = 32 * CB;          // KS: parts of 128 bytes a row
+    static constexpr int xpart = 4096, part = xpart + TN * 128, slab = KS * part, NF = KS * CB, NL = KS + NF;
     static constexpr int sums = 3 * CB * 4096;
     static constexpr int ring = NS * slab > sums ? NS * slab : sums;
     static constexpr int lds = ring + 32 * 4 * 4;         // and the adapters, their ranks and scales, the rows' places among them
+    static constexpr int per_cu = 2 * lds <= 160 * 1024 ? 2 : 1;
     static_assert((NS - 2) * NL < 64 && lds <= 160 * 1024, "");
 };
 
 template <class L, bool PLANES>
 __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsigned char* lds) {
-    constexpr int CB = L::CB, NS = L::NS;
+    constexpr int CB = L::CB, KS = L::KS, NS = L::NS;
     int* const list = reinterpret_cast<int*>(lds + L::ring);
     int* const ranks = list + 32;
     int* const place = ranks + 32;
@@ -421,16 +426,17 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
 
     const int slots = L::TN / r;
     const int lrow = lane >> 3;
-    const int ns = (n * 2 + 127) / 128;
+    const int ns = (n * 2 + 128 * KS - 1) / (128 * KS);
     const int xrow = 8 * wave + lrow, xchunk = ((lane & 7) ^ ((xrow >> 1) & 7)) * 16;
     const rsrc_t xres = make_rsrc(g.E + row0 * g.e_pitch, (int64_t)rows * g.e_pitch * 2);
     int xslot = 0, xissued = 0;
     auto issue_x = [&]() {
         unsigned char* const dst = lds + xslot + wave * 1024;
         xslot = xslot == (NS - 1) * L::slab ? 0 : xslot + L::slab;
-        const int x = xissued * 128 + xchunk;
+        const int x = xissued * KS * 128 + xchunk;
         ++xissued;
-        load_lds16(xres, dst, x < 2 * n ? xrow * g.e_pitch * 2 + x : kBufNowhere, 0);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) load_lds16(xres, dst + k * L::part, x + k * 128 < 2 * n ? xrow * g.e_pitch * 2 + x + k * 128 : kBufNowhere, 0);
     };
     while (xissued < NS - 1 && xissued < ns) issue_x();   // before anything is known of the adapters
 
@@ -465,20 +471,20 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
     for (int first = 0; first == 0 || first < count; first += slots) {
         const int used = (count - first < slots ? count - first : slots) * r;      // columns of this pass
         // B: load instruction j covers eight columns, of one adapter (r is a multiple of 8): rows 8 (wave + 4 j) .. of the side-by-side B
-        rsrc_t fres[L::NF];
+        rsrc_t fres[CB];
         // A: this lane's 16 bytes of the first slab, and where in its adapter's they lie
-        const uint16_t* apart[L::NF];
-        int at_a[L::NF];
+        const uint16_t* apart[CB];
+        int at_a[CB];
         if constexpr (PLANES) {
 #pragma unroll
-            for (int j = 0; j < L::NF; ++j) {
+            for (int j = 0; j < CB; ++j) {
                 const int pos = 64 * (wave + 4 * j) + lane, p = pos / (8 * r);
                 at_a[j] = (pos - p * 8 * r) * 8;
                 apart[j] = p < slots && first + p < count ? g.F + (int64_t)list[first + p] * n * r + at_a[j] : nullptr;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < L::NF; ++j) {
+            for (int j = 0; j < CB; ++j) {
                 const int c = 8 * (wave + 4 * j), p = first + c / r, k = c % r;
                 const bool have = c / r < slots && p < count;
                 const int a = have ? __builtin_amdgcn_readfirstlane(list[p]) : 0;
@@ -489,16 +495,18 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
         auto issue_f = [&]() {
             unsigned char* const dst = lds + fslot + L::xpart + wave * 1024;
             fslot = fslot == (NS - 1) * L::slab ? 0 : fslot + L::slab;
-            if constexpr (PLANES) {
 #pragma unroll
-                for (int j = 0; j < L::NF; ++j) {
-                    const int64_t k = (int64_t)64 * r * fissued;
-                    load_lds16_at(apart[j] && k + at_a[j] < (int64_t)n * r ? (const void*)(apart[j] + k) : (const void*)zero_line, dst + j * 4096);
+            for (int k = 0; k < KS; ++k) {
+                if constexpr (PLANES) {
+                    const int64_t off = (int64_t)64 * r * (fissued * KS + k);
+#pragma unroll
+                    for (int j = 0; j < CB; ++j)
+                        load_lds16_at(apart[j] && off + at_a[j] < (int64_t)n * r ? (const void*)(apart[j] + off) : (const void*)zero_line, dst + k * L::part + j * 4096);
+                } else {
+                    const int x = (fissued * KS + k) * 128 + xchunk;      // (the same chunk of eight rows further on)
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) load_lds16(fres[j], dst + k * L::part + j * 4096, x < 2 * n ? lrow * n * 2 + x : kBufNowhere, 0);
                 }
-            } else {
-                const int x = fissued * 128 + xchunk;     // (the same chunk of eight rows further on)
-#pragma unroll
-                for (int j = 0; j < L::NF; ++j) load_lds16(fres[j], dst + j * 4096, x < 2 * n ? lrow * n * 2 + x : kBufNowhere, 0);
             }
             ++fissued;
         };
@@ -522,19 +530,26 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
             if (xissued < ns) { issue_x(); issue_f(); }
             const unsigned char* const x = lds + slot;
             slot = slot == (NS - 1) * L::slab ? 0 : slot + L::slab;
-            const u32x4 xo = *reinterpret_cast<const u32x4*>(x + xread);
-            u32x4 fo[CB];
+            // all reads before the first product: a read's way is as long as a product
+            u32x4 xo[KS], fo[KS][CB];
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                xo[k] = *reinterpret_cast<const u32x4*>(x + k * L::part + xread);
+                if constexpr (!PLANES)
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) fo[k][b] = *reinterpret_cast<const u32x4*>(x + k * L::part + fread + b * 4096);
+            }
             if constexpr (PLANES) {
                 const uint32_t base = lds_address(x);
 #pragma unroll
                 for (int b = 0; b < CB; b += 2)
-                    read_tr2(base + kread[b], base + kread[b] + 8 * r, base + kread[b + 1], base + kread[b + 1] + 8 * r, fo[b], fo[b + 1]);
-            } else {
-#pragma unroll
-                for (int b = 0; b < CB; ++b) fo[b] = *reinterpret_cast<const u32x4*>(x + fread + b * 4096);
+                    read_tr4<L::part>(base + kread[b], base + kread[b] + 8 * r, base + kread[b + 1], base + kread[b + 1] + 8 * r, fo[0][b], fo[0][b + 1], fo[1][b], fo[1][b + 1]);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int b = 0; b < CB; ++b) acc[b] = mfma_bf16(fo[b], xo, acc[b]);
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int b = 0; b < CB; ++b) acc[b] = mfma_bf16(fo[k][b], xo[k], acc[b]);
         }
         // the waves' sums: blocks of 32 columns in turn, b by wave b % 4
         if (first == 0 && (int)threadIdx.x < count) {
@@ -635,9 +650,9 @@ __global__ __launch_bounds__(256, 2) void adapters_t_kernel(const AdapterProduct
     t_tile<L, false>(g, blockIdx.x, lds);
 }
 
-// dT, and beside it what only later launches need
+// dT, and beside it what only later launches need.  (More than 256 registers only where one work-group fills the compute unit: T gains nothing by them.)
 template <class L>
-__global__ __launch_bounds__(256, 2) void adapters_dt_kernel(const AdapterProduct g, const AdapterPrep p, const PrepBlocks n, int tiles) {
+__global__ __launch_bounds__(256, L::per_cu) void adapters_dt_kernel(const AdapterProduct g, const AdapterPrep p, const PrepBlocks n, int tiles) {
     extern __shared__ __align__(1024) unsigned char lds[];
     const int i = blockIdx.x, t = i - n.list;             // lists, tiles of dT, transposes
     if (t >= 0 && t < tiles) t_tile<L, true>(g, t, lds);
@@ -668,9 +683,9 @@ hipError_t launch_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream
 }  // namespace
 
 hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s) { return fp8 ? launch_y<true>(p, s) : launch_y<false>(p, s); }
-hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return p.r <= 32 ? launch_t<Low<2, 6>>(p, s) : launch_t<Low<4, 4>>(p, s); }
+hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return p.r <= 32 ? launch_t<Low<2, 3>>(p, s) : launch_t<Low<4, 3>>(p, s); }
 hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream_t s) {
-    return p.r <= 32 ? launch_dt<Low<2, 6>>(p, prep, s) : launch_dt<Low<4, 4>>(p, prep, s);
+    return p.r <= 32 ? launch_dt<Low<2, 3>>(p, prep, s) : launch_dt<Low<4, 3>>(p, prep, s);
 }
 
 hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {

@@ -39,19 +39,23 @@ __device__ __forceinline__ void read_tr2(uint32_t at0, uint32_t at1, u32x4& v0, 
     v0 = u32x4{a[0], a[1], b[0], b[1]};
     v1 = u32x4{c[0], c[1], d[0], d[1]};
 }
-// the same with halves at addresses of their own
-__device__ __forceinline__ void read_tr2(uint32_t at0, uint32_t back0, uint32_t at1, uint32_t back1, u32x4& v0, u32x4& v1) {
-    u32x2 a, b, c, d;
-    asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %2, %6\n\tds_read_b64_tr_b16 %3, %7\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d) : "v"(at0), "v"(back0), "v"(at1), "v"(back1));
+// the same with halves at addresses of their own, and all of it once more OFF bytes further on
+template <int OFF>
+__device__ __forceinline__ void read_tr4(uint32_t at0, uint32_t back0, uint32_t at1, uint32_t back1, u32x4& v0, u32x4& v1, u32x4& w0, u32x4& w1) {
+    u32x2 a, b, c, d, e, f, g, h;
+    asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11\n\t"
+                 "ds_read_b64_tr_b16 %4, %8 offset:%12\n\tds_read_b64_tr_b16 %5, %9 offset:%12\n\tds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(f), "=&v"(g), "=&v"(h) : "v"(at0), "v"(back0), "v"(at1), "v"(back1), "n"(OFF));
     v0 = u32x4{a[0], a[1], b[0], b[1]};
     v1 = u32x4{c[0], c[1], d[0], d[1]};
+    w0 = u32x4{e[0], e[1], f[0], f[1]};
+    w1 = u32x4{g[0], g[1], h[0], h[1]};
 }
 // lane l's 16 bytes at its own address go to LDS address dst + 16 l
 __device__ __forceinline__ void load_lds16_at(const void* src, unsigned char* dst) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src, (__attribute__((address_space(3))) uint32_t*)(void*)dst, 16, 0, 0);
 }
-
 
 inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<bool>& done) {
     if (done.load(std::memory_order_acquire)) return hipSuccess;
