@@ -28,7 +28,10 @@ hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s);
 hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s);         // X absent, Q = r <= 128
 
 // Few rows: T (p.T, p.Tb, either may be NULL but for Tb = p.E) from X [M, n] and B, and Y, together.  sums: adapters_few_sums_bytes.
-constexpr int kAdapterFewRows = 128;
+// The limit is where rows that lie together by adapter no longer gain; rows in any order gain far beyond it (every tile of Y and of T takes a pass per
+// adapter or two), but the host does not see the order.  us, few rows' kernels / tiles, 192 rows together, 192 in any order, 256 together: 768 x 768, r = 16 11.1 / 13.1,
+// 11.7 / 15.1, 11.5 / 13.7; 2304 x 768, r = 64 16.9 / 16.8, 20.8 / 36.8, 20.5 / 15.9; 4096 x 4096, r = 16 42.8 / 39.8, -, 44.4 / 40.0; r = 64, 24 adapters -, 54 / 208, -.
+constexpr int kAdapterFewRows = 192;
 size_t adapters_few_sums_bytes(int64_t M, int m, int n);
 hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s);
 
@@ -57,7 +60,8 @@ int adapters_grad_piece(int64_t M, int m, int n);      // rows of a piece
 size_t adapters_grad_partial_bytes(int64_t M, int m, int n, int r, int count);
 // With x, dX beside them in the same launch
 hipError_t launch_adapters_grads(const AdapterGrads& p, const AdapterProduct* x, hipStream_t s);
-// Few rows: no partials, and dX (or NULL) in the same launch
+// Few rows: no partials, and dX (or NULL) in the same launch.  At most what a work-group's list of rows holds; up to there it is faster, us, this / pieces: 768 x 768, r = 8
+// 17.8 / 25.8 (394 rows), 20.0 / 27.3 (1024); 2304 x 768, r = 16 33.8 / 44.1, 34.9 / 44.5; 1024 x 1024, r = 64 27.1 / 39.8, 45.0 / 49.8.
 constexpr int kAdapterFewGradRows = 1024;
 hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGrads& p, hipStream_t s);
 // Many rows and a narrow rank: is dX faster beside the gradients than before them?  And that launch.

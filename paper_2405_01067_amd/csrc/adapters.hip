@@ -367,6 +367,7 @@ hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
 
 // dX and the factor gradients in one launch, the tiles of dX first: of few rows neither fills the chip; of many one is bound by the matrix unit and the
 // other by memory, and a work-group of each fits a compute unit beside the other.
+// 12608 x 2304 x 768, r = 16: 60 us for both (dX alone 51, the gradients 24.5); 394 x 768 x 768, r = 8: 7.9.
 template <class L, int VB>
 __global__ __launch_bounds__(256, 2) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b, int piece) {
     extern __shared__ __align__(1024) unsigned char lds[];
@@ -683,6 +684,9 @@ hipError_t launch_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream
 }  // namespace
 
 hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s) { return fp8 ? launch_y<true>(p, s) : launch_y<false>(p, s); }
+// 64 columns for r <= 32: half the bytes of the adapters' side where 32 rows have one adapter or two.  us, T with one part a step, 64 / 128 columns: 12608 x 768, r = 32, runs of 64
+// 13.0 / 16.2; 1379 x 768, runs of 200 6.9 / 8.4, of 7 14.0 / 13.7; 8190 x 4096, runs of 9 51.8 / 43.2.  For r > 64, 256 columns: 12608 x 768, r = 128
+// 46.6 / 35.7 with 128.
 hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return p.r <= 32 ? launch_t<Low<2, 3>>(p, s) : launch_t<Low<4, 3>>(p, s); }
 hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream_t s) {
     return p.r <= 32 ? launch_dt<Low<2, 3>>(p, prep, s) : launch_dt<Low<4, 3>>(p, prep, s);
@@ -704,9 +708,12 @@ hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGr
     }
 }
 
+// Beside the gradients dX has one tile only, which may not be its best; the gradients' time (their bytes at 4 TB/s) is half hidden and a launch, 3.6 us, saved.
+// (From r = 33 on the gradients fill a compute unit alone.)  us, beside / apart: 768 x 768, r = 8 1500 rows 29.8 / 31.9, 12608 52.7 / 60.2; 2304 x 768, r = 16 1500
+// 52.2 / 47.6 (apart), 4096 54.9 / 57.3, 12608 83.1 / 95.9; 768 x 2304, r = 32 1500 38.4 / 46.7, 12608 95.7 / 107.7; 2304 x 2304, r = 16 4096 73.0 / 80.9.
 bool adapters_dx_beside_grads(const AdapterProduct& x, const AdapterGrads& g) {
     const float grads = 2.0f * (float)g.M * (float)((g.dA ? g.m : 0) + (g.dB ? g.n : 0)) / 4e6f;
-    return g.r <= 32 && tile_cost(kTile128x192, x, false) - tile_cost(best_tile(x, false), x, false) < 0.5f * grads;
+    return g.r <= 32 && tile_cost(kTile128x192, x, false) - tile_cost(best_tile(x, false), x, false) < 0.5f * grads + 3.6f;
 }
 hipError_t launch_adapters_dx_grad_pieces(const AdapterProduct& x, const AdapterGrads& g, int piece, hipStream_t s) {
     return g.r <= 16 ? launch_dx_grads<T128x192, 1>(&x, g, piece, s) : launch_dx_grads<T128x192, 2>(&x, g, piece, s);

@@ -79,6 +79,18 @@ def test_few_rows(M, m, n, r, K):
         within(Y, o["Y"], b["Y"], "Y")
 
 
+# Three groups of 64 rows, to where tiles take over.
+@pytest.mark.parametrize("M,m,n,r,K,rows", [(130, 40, 264, 16, 3, "any"), (160, 136, 520, 64, 30, "any"), (191, 72, 1032, 128, 5, "any"), (192, 200, 264, 8, 192, "any"), (192, 72, 2056, 24, 3, "sorted"),
+                                            (193, 72, 264, 16, 5, "any")])
+def test_rows_of_a_few_groups(M, m, n, r, K, rows):
+    c = make(M, m, n, r, K, rows, True, seed=M + m + r)
+    d = gpu(c)
+    o, b = reference(c)
+    Y, T = abt.lr_adapters_fwd(d["X"], d["W"], d["A"], d["B"], d["row_adapter"], d["ranks"], d["scales"])
+    within(T, o["T"], b["T"], "T")
+    within(Y, o["Y"], b["Y"], "Y")
+
+
 # Gradients with dX in the same launch, before it, and beside pieces of many rows; ranks padded to 16, 32, 64 and 128; 1024 rows and one more.
 @pytest.mark.parametrize("M,m,n,r,K,rows", [
     (1000, 776, 2056, 8, 4, "runs"), (1000, 776, 2056, 24, 4, "any"), (1000, 776, 2056, 40, 4, "runs"), (1000, 776, 2056, 72, 4, "runs"),
