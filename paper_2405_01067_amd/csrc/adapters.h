@@ -26,12 +26,17 @@ inline __host__ __device__ int plane_columns(int r) { return r <= 16 ? 16 : r <=
 
 hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s);
 hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s);         // X absent, Q = r <= 128
+// T row by row: up to 1024 rows and this many values of T.  us, the forward by rows / by tiles of 32 rows, in runs of 100 and any order: 768 x 768, r = 16, 394 rows
+// 12.5 / 13.7, 13.4 / 15.3; 2304 x 768, r = 64, 256 rows 16.1 / 16.9, 22.3 / 36.7, 394 rows 18.6 / 17.3, 24.6 / 36.9, 1024 rows 39.1 / 28.6, 51.5 / 48.9; 4096 x 4096,
+// r = 128, 256 rows 44.8 / 47.7, 512 rows 64.8 / 53.0.
+constexpr int64_t kAdapterRowsOfT = 24576;
+hipError_t launch_adapters_t_rows(const AdapterProduct& p, hipStream_t s);
 
 // Few rows: T (p.T, p.Tb, either may be NULL but for Tb = p.E) from X [M, n] and B, and Y, together.  sums: adapters_few_sums_bytes.
-// The limit is where rows that lie together by adapter no longer gain; rows in any order gain far beyond it (every tile of Y and of T takes a pass per
-// adapter or two), but the host does not see the order.  us, few rows' kernels / tiles, 192 rows together, 192 in any order, 256 together: 768 x 768, r = 16 11.1 / 13.1,
-// 11.7 / 15.1, 11.5 / 13.7; 2304 x 768, r = 64 16.9 / 16.8, 20.8 / 36.8, 20.5 / 15.9; 4096 x 4096, r = 16 42.8 / 39.8, -, 44.4 / 40.0; r = 64, 24 adapters -, 54 / 208, -.
-constexpr int kAdapterFewRows = 192;
+// The limit is where rows that lie together by adapter no longer gain (rows in any order gain longer, but the host does not see the order).  us, these kernels / T row by
+// row and tiles, in runs of 100, 128 and 192 rows: 768 x 768, r = 16 10.9 / 10.7, 11.2 / 11.4; 2304 x 768, r = 64 13.9 / 13.9, 16.6 / 14.7; 4096 x 4096, r = 16
+// 26.2 / 29.9, 43.3 / 30.3, in 8 bits 20.1 / 18.2, 29.2 / 19.4; in any order, 128 rows: 4096 x 4096, r = 64 36.5 / 51.5.
+constexpr int kAdapterFewRows = 128;
 size_t adapters_few_sums_bytes(int64_t M, int m, int n);
 hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s);
 

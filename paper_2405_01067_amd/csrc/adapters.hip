@@ -412,6 +412,31 @@ struct Low {
     static_assert((NS - 2) * NL < 64 && lds <= 160 * 1024, "");
 };
 
+// Columns k .. k + 7 of a row.  Three bf16 values that add up to the fp32 one (each takes eight bits of what the ones before left): the factor gradients
+// are fp32 sums of exact products, as they would be of fp32 operands.
+__device__ __forceinline__ void store_planes(uint16_t* to, int64_t row, int k, int r, const float (&u)[8]) {
+    const int rp = plane_columns(r);
+    u32x4 w[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x = u[2 * i], y = u[2 * i + 1];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const uint32_t t = pack2_bf16(x, y);
+            w[q][i] = t;
+            x -= __builtin_bit_cast(float, t << 16);
+            y -= __builtin_bit_cast(float, t & 0xffff0000u);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        uint16_t* const d = to + (row * 3 + q) * rp;
+        gstore(reinterpret_cast<u32x4*>(d + k), w[q]);
+        if (k + 8 == r)                                   // the columns that the gradients' blocks have beyond r
+            for (int z = r; z < rp; z += 8) gstore(reinterpret_cast<u32x4*>(d + z), u32x4{0, 0, 0, 0});
+    }
+}
+
 template <class L, bool PLANES>
 __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsigned char* lds) {
     constexpr int CB = L::CB, KS = L::KS, NS = L::NS;
@@ -604,39 +629,15 @@ __device__ __forceinline__ void t_tile(const AdapterProduct& g, int tile, unsign
                         gstore(reinterpret_cast<u32x4*>(g.Tb + row * r + k), w);
                     }
                 } else {
-                    // Three bf16 values that add up to the fp32 one (each takes eight bits of what the ones before left): the factor gradients are
-                    // fp32 sums of exact products, as they would be of fp32 operands.
-                    const int rp = plane_columns(r);
-                    auto planes = [&](uint16_t* to, const float (&u)[8]) {
-                        u32x4 w[3];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float x = u[2 * i], y = u[2 * i + 1];
-#pragma unroll
-                            for (int q = 0; q < 3; ++q) {
-                                const uint32_t t = pack2_bf16(x, y);
-                                w[q][i] = t;
-                                x -= __builtin_bit_cast(float, t << 16);
-                                y -= __builtin_bit_cast(float, t & 0xffff0000u);
-                            }
-                        }
-#pragma unroll
-                        for (int q = 0; q < 3; ++q) {
-                            uint16_t* const d = to + (row * 3 + q) * rp;
-                            gstore(reinterpret_cast<u32x4*>(d + k), w[q]);
-                            if (k + 8 == r)               // the columns that the gradients' blocks have beyond r
-                                for (int z = r; z < rp; z += 8) gstore(reinterpret_cast<u32x4*>(d + z), u32x4{0, 0, 0, 0});
-                        }
-                    };
                     float u[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) u[i] = k + i < mine ? scale * v[i] : 0.0f;
-                    planes(g.dT_planes, u);
+                    store_planes(g.dT_planes, row, k, r, u);
                     if (g.T_planes) {
                         const f32x4 t0 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k)), t1 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k + 4));
 #pragma unroll
                         for (int i = 0; i < 8; ++i) u[i] = k + i < mine ? scale * (i < 4 ? t0[i & 3] : t1[i & 3]) : 0.0f;
-                        planes(g.T_planes, u);
+                        store_planes(g.T_planes, row, k, r, u);
                     }
                 }
             }
@@ -658,6 +659,81 @@ __global__ __launch_bounds__(256, L::per_cu) void adapters_dt_kernel(const Adapt
     const int i = blockIdx.x, t = i - n.list;             // lists, tiles of dT, transposes
     if (t >= 0 && t < tiles) t_tile<L, true>(g, t, lds);
     else prepare(p, n, t < 0 ? i : i - tiles, lds);
+}
+
+// dT of few rows, in whatever order: a work-group for a row and 32 columns of its A, whose threads share out A's rows, eight columns each.
+// Bound by latency, then by reads of A from L2 (2 M m r bytes).  us, row by row / tiles of 32 rows, in runs of 100 and any order: 394 rows of 768, r = 8 6.2 / 9.2, 6.1 / 10.0;
+// 394 of 4096, r = 32 15.0 / 20.3, 14.8 / 52.4; 1024 of 2304, r = 16 11.0 / 14.6, 12.4 / 27.0; 1024 of 4096, r = 128 81.5 / 86.6, 79.4 / 173; but 2048 of 1024, r = 128
+// 44.3 / 31.3, 45.0 / 60.4.
+constexpr int kDtRowLds = 256 * 32 + 256 * 4;
+__device__ __forceinline__ void dt_of_row(const AdapterProduct& g, int64_t row, int k0, unsigned char* lds) {
+    float* const parts = reinterpret_cast<float*>(lds);
+    float* const sums = parts + 256 * 8;
+    const int t = threadIdx.x, r = g.r, m = g.ke, cols = r - k0 < 32 ? r - k0 : 32, groups = cols / 8;
+    const int cg = t % groups, each = 256 / groups, first = t / groups;       // (of three groups one thread is left over)
+    const int a = __builtin_amdgcn_readfirstlane(gload(g.row_adapter + row));
+    const bool have = a >= 0 && a < g.count;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    if (have && first < each) {
+        const uint16_t* const y = g.E + row * g.e_pitch;
+        const uint16_t* const A = g.F + (int64_t)a * m * r + k0 + 8 * cg;
+        for (int j = first; j < m; j += 8 * each) {       // eight loads on their way at a time
+            u32x4 v[8];
+            uint32_t d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = j + i * each < m ? j + i * each : j;
+                v[i] = gload(reinterpret_cast<const u32x4*>(A + (int64_t)at * r));
+                d[i] = gload(y + at);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (j + i * each >= m) continue;
+                const float x = __builtin_bit_cast(float, d[i] << 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t w = v[i][e];
+                    sum[2 * e] += x * __builtin_bit_cast(float, w << 16);
+                    sum[2 * e + 1] += x * __builtin_bit_cast(float, w & 0xffff0000u);
+                }
+            }
+        }
+    }
+    *reinterpret_cast<f32x4*>(parts + 8 * t) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+    *reinterpret_cast<f32x4*>(parts + 8 * t + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+    __syncthreads();
+    const int c = t % cols, many = 256 / cols, p = t / cols;      // a column's parts in `many` sums, then those
+    float v = 0.0f;
+    if (p < many)
+        for (int q = p; q < each; q += many) v += parts[8 * (q * groups + c / 8) + c % 8];
+    sums[t] = v;
+    __syncthreads();
+    if (t < cols) {
+        v = 0.0f;
+        for (int q = 0; q < many; ++q) v += sums[q * cols + t];
+        parts[t] = v;
+    }
+    __syncthreads();
+    if (t >= groups) return;
+    const int k = k0 + 8 * t, mine = have ? rank_of(g, a) : 0;
+    const float scale = have && g.scales ? gload(g.scales + a) : 1.0f;
+    float u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = k + i < mine ? scale * parts[8 * t + i] : 0.0f;
+    store_planes(g.dT_planes, row, k, r, u);
+    if (!g.T_planes) return;
+    const f32x4 t0 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k)), t1 = gload(reinterpret_cast<const f32x4*>(g.T_in + row * r + k + 4));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = k + i < mine ? scale * (i < 4 ? t0[i & 3] : t1[i & 3]) : 0.0f;
+    store_planes(g.T_planes, row, k, r, u);
+}
+__global__ __launch_bounds__(256) void adapters_dt_rows_kernel(const AdapterProduct g, const AdapterPrep p, const PrepBlocks n, int rows) {
+    __shared__ __align__(16) unsigned char lds[kDtRowLds > kPrepLds ? kDtRowLds : kPrepLds];
+    const int i = blockIdx.x, t = i - n.list, per = (g.r + 31) / 32;          // lists, rows, transposes
+    if (t >= 0 && t < rows) dt_of_row(g, t / per, t % per * 32, lds);
+    else prepare(p, n, t < 0 ? i : i - rows, lds);
 }
 
 template <class L>
@@ -687,8 +763,17 @@ hipError_t launch_adapters_y(const AdapterProduct& p, bool fp8, hipStream_t s) {
 // 64 columns for r <= 32: half the bytes of the adapters' side where 32 rows have one adapter or two.  us, T with one part a step, 64 / 128 columns: 12608 x 768, r = 32, runs of 64
 // 13.0 / 16.2; 1379 x 768, runs of 200 6.9 / 8.4, of 7 14.0 / 13.7; 8190 x 4096, runs of 9 51.8 / 43.2.  For r > 64, 256 columns: 12608 x 768, r = 128
 // 46.6 / 35.7 with 128.
-hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) { return p.r <= 32 ? launch_t<Low<2, 3>>(p, s) : launch_t<Low<4, 3>>(p, s); }
+hipError_t launch_adapters_t(const AdapterProduct& p, hipStream_t s) {
+    if (p.M <= 1024 && p.M * p.r <= kAdapterRowsOfT) return launch_adapters_t_rows(p, s);
+    return p.r <= 32 ? launch_t<Low<2, 3>>(p, s) : launch_t<Low<4, 3>>(p, s);
+}
 hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, hipStream_t s) {
+    if (p.M <= kAdapterFewGradRows) {
+        const PrepBlocks n = prep_blocks(prep);
+        const int rows = (int)(p.M * ceil_div(p.r, 32));
+        hipLaunchKernelGGL(adapters_dt_rows_kernel, dim3((unsigned)(rows + n.all)), dim3(256), 0, s, p, prep, n, rows);
+        return hipGetLastError();
+    }
     return p.r <= 32 ? launch_dt<Low<2, 3>>(p, prep, s) : launch_dt<Low<4, 3>>(p, prep, s);
 }
 

@@ -86,6 +86,12 @@ __device__ __forceinline__ void t_of_row(const AdapterProduct& g, const uint16_t
     if (g.Tb) gstore(g.Tb + row * g.r + j, (uint16_t)(pack2_bf16(j < rank ? s * sum : 0.0f, 0.0f) & 0xffffu));
 }
 
+// T alone, for tiles of Y after it
+__global__ __launch_bounds__(512) void adapters_t_rows_kernel(const AdapterProduct g) {
+    const int per = g.r / 8, w = blockIdx.x;
+    t_of_row(g, g.E, g.F, g.ke, w / per, (w % per) * 8 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+}
+
 struct FewParts { int col_blocks, blocks16, row_groups, splits, units; float* sums; const uint16_t* X; const uint16_t* B; };   // X as the adapters see it
 
 // RB blocks of 16 rows
@@ -401,6 +407,11 @@ hipError_t few(const AdapterProduct& p, const FewParts& f, hipStream_t s) {
 size_t adapters_few_sums_bytes(int64_t M, int m, int n) {
     const int s8 = few_parts(M, m, n, true).splits, s16 = few_parts(M, m, n, false).splits;
     return (size_t)(s8 > s16 ? s8 : s16) * (size_t)M * align_up((size_t)m, 16) * 4;
+}
+
+hipError_t launch_adapters_t_rows(const AdapterProduct& p, hipStream_t s) {
+    hipLaunchKernelGGL(adapters_t_rows_kernel, dim3((unsigned)(p.M * (p.r / 8))), dim3(512), 0, s, p);
+    return hipGetLastError();
 }
 
 hipError_t launch_adapters_few(const AdapterProduct& p, const uint16_t* X, const uint16_t* B, float* sums, bool fp8, hipStream_t s) {

@@ -79,9 +79,10 @@ def test_few_rows(M, m, n, r, K):
         within(Y, o["Y"], b["Y"], "Y")
 
 
-# Three groups of 64 rows, to where tiles take over.
+# Between the few rows' kernels and those of many: T row by row up to 24576 values and 1024 rows, by tiles beyond.
 @pytest.mark.parametrize("M,m,n,r,K,rows", [(130, 40, 264, 16, 3, "any"), (160, 136, 520, 64, 30, "any"), (191, 72, 1032, 128, 5, "any"), (192, 200, 264, 8, 192, "any"), (192, 72, 2056, 24, 3, "sorted"),
-                                            (193, 72, 264, 16, 5, "any")])
+                                            (193, 72, 264, 16, 5, "any"), (1024, 40, 264, 24, 3, "any"), (1025, 40, 264, 24, 3, "any"), (1024, 40, 264, 32, 30, "any"),
+                                            (512, 40, 4104, 48, 6, "runs"), (513, 40, 4104, 48, 6, "runs")])
 def test_rows_of_a_few_groups(M, m, n, r, K, rows):
     c = make(M, m, n, r, K, rows, True, seed=M + m + r)
     d = gpu(c)
