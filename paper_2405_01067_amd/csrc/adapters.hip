@@ -779,8 +779,11 @@ hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, 
 
 hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
     if (g.M > kAdapterFewGradRows) return hipErrorInvalidValue;
-    // (a launch of its own costs some 4 us)
-    if (x && tile_cost(kTile64, *x, false) > tile_cost(best_tile(*x, false), *x, false) + 4.0f) {
+    // dX has the smallest tile here, and from r = 33 on one work-group fills a compute unit: it goes alone where its best tile saves 16 us, or from 400 tiles on.  us,
+    // together / apart: 2304 x 768, r = 16, 1024 rows 31.7 / 37.4; 2304 x 2304, r = 16, 911 rows 50.0 / 53.3 (its best tile: 11 us less); 1024 x 1024, r = 64, 1024 rows (256
+    // tiles) 45.6 / 46.4; 768 x 2304, r = 48, 700 rows (396) 34.8 / 38.6, 911 (540) 46.1 / 43.6; 88 x 3272, r = 120, 512 rows (416) 46.6 / 44.2, 1024 (832) 77.4 / 63.6.
+    if (x && (g.r > 32 ? ceil_div(x->M, T64x64::TM) * ceil_div(x->Q, T64x64::TN) > 400
+                       : tile_cost(kTile64, *x, false) > tile_cost(best_tile(*x, false), *x, false) + 16.0f)) {
         const hipError_t e = launch_adapters_y(*x, false, s);
         if (e != hipSuccess) return e;
         x = nullptr;
