@@ -31,8 +31,17 @@ __global__ __launch_bounds__(256) void adapters_sum_kernel(const AdapterGrads g,
     float* const out = (first ? g.dA : g.dB) + a * size + i;
     const int begin = gload(g.offsets + a), end = gload(g.offsets + a + 1);
     f32x4 v = {0, 0, 0, 0};
-    if (end > begin)
-        for (int p = begin / piece; p <= (end - 1) / piece; ++p) v += gload(reinterpret_cast<const f32x4*>(part + (int64_t)(p + a) * size));
+    if (end > begin) {
+        const int last = (end - 1) / piece;
+        for (int p = begin / piece; p <= last; p += 8) {  // eight loads on their way at a time
+            f32x4 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = gload(reinterpret_cast<const f32x4*>(part + (int64_t)((p + i < last ? p + i : last) + a) * size));
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (p + i <= last) v += x[i];
+        }
+    }
     if (g.accumulate) v += gload(reinterpret_cast<const f32x4*>(out));
     gstore(reinterpret_cast<f32x4*>(out), v);
 }
