@@ -2,7 +2,7 @@
 //     Y_i = W x_i + A_a T_i          T_i = B_a x_i          a = adapter of row i, T scaled where it is an operand
 // Y: a tile of the dense product, then in the same accumulators the adapters that occur among its rows, one after the other, with the T of other
 // adapters' rows as zeros.  Rows that lie together by adapter cost a tile one or two short passes; rows in any other order more of them.
-// T: 32 rows against the B of all adapters among them, side by side as columns of one product; every row keeps those of its own.
+// T: 32 rows against the B of all adapters among them, side by side as columns of one product; every row keeps those of its own.  (Of up to 1024 rows row by row.)
 //
 // A slab is 128 bytes of every row: 64 columns in bf16, 128 in 8 bits.  It comes straight to LDS, NS slots in a ring, one barrier per
 // slab.  Both types read LDS alike: two 16-byte pieces are two bf16 operands of 32x32x16 or one 8-bit operand of 32x32x64, whose columns are taken in
@@ -367,7 +367,7 @@ hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
 
 // dX and the factor gradients in one launch, the tiles of dX first: of few rows neither fills the chip; of many one is bound by the matrix unit and the
 // other by memory, and a work-group of each fits a compute unit beside the other.
-// 12608 x 2304 x 768, r = 16: 60 us for both (dX alone 51, the gradients 24.5); 394 x 768 x 768, r = 8: 7.9.
+// 12608 x 2304 x 768, r = 16: 59 us for both (dX alone 51, the gradients 24.5); 394 x 768 x 768, r = 8: 8.2.
 template <class L, int VB>
 __global__ __launch_bounds__(256, 2) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b, int piece) {
     extern __shared__ __align__(1024) unsigned char lds[];
