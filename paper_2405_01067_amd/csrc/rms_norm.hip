@@ -165,7 +165,8 @@ __global__ __launch_bounds__(kNormThreads) void rms_norm_bwd_kernel(const T* dY,
             }
         hh = over_row<WPR, false>(hh, part);
         uh = over_row<WPR, false>(uh, part);
-        const float s = 1.0f / sqrtf(hh / (float)n + eps);
+        // (a row that is not there has h = 0: without eps its factor would be infinite, and its part in dg NaN)
+        const float s = cols ? 1.0f / sqrtf(hh / (float)n + eps) : 0.0f;
         const float k = s * s * (uh / (float)n);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
