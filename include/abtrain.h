@@ -378,6 +378,7 @@ size_t lr_conv_bwd_workspace_bytes(const abt_conv_geom* geom, int64_t m, int64_t
  * A frozen dense layer with low-rank adapters: `count` pairs of factors (Eq. 3's A and B, as a group phase or ab_factorize leaves
  * them) beside one weight W [m, n] that is not trained.  Every row belongs to an adapter of its own choice:
  *     T_i = B_a x_i          Y_i = W x_i + scale_a A_a T_i          a = row_adapter[i]
+ * An adapter that holds infinities or NaN has a part in the results of its own rows only.
  * row_adapter [M]: int32; an id outside [0, count), -1 by custom, is no adapter: Y_i = W x_i, T_i = 0.  The ids may come in any
  * order; rows that lie together by adapter are the fast case (a tile of the result makes one short pass per adapter among its
  * rows).  All tables are read by the kernels, so a captured graph can be replayed with other ids, ranks and scales.

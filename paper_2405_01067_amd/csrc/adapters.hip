@@ -260,7 +260,9 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
         mma(o[1]);
     }
 
-    // what is left of the adapters
+    // What is left of the adapters.  Infinities and NaN in them are left out here, where the rows of other adapters are summed up too.  Looking for them
+    // costs 0 to 1 % of a launch where rows lie in runs, 1 to 4 % in any order (12608 x 2304 x 768, r = 16: 0.6 and 2 us).
+    bool poisoned = false;
     while (piece.a != INT_MAX) {
         const Piece now = piece;
         Ops m = ahead;
@@ -273,6 +275,14 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
             if (valid < 8)
 #pragma unroll
                 for (int b = 0; b < CB; ++b) m.f[b] = first_of(m.f[b], valid);
+        }
+        float bad = 0.0f;
+#pragma unroll
+        for (int b = 0; b < CB; ++b) bad += zero_times(m.f[b]);
+        if (__builtin_expect(any_not_finite(bad), 0)) {
+            poisoned = true;
+#pragma unroll
+            for (int b = 0; b < CB; ++b) m.f[b] = finite_of(m.f[b]);
         }
         mma(m);
     }
@@ -292,6 +302,40 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
                 *reinterpret_cast<u32x4*>(d + 16 * h) = v;
             }
         }
+    // and come into the rows of their own adapter, in this wave's part of the tile
+    if (__builtin_expect(poisoned, 0))
+        for (piece = adapter(after(-1)); piece.a != INT_MAX; piece = adapter(after(piece.a)))
+            for (; piece.k < piece.rank; piece.k += 16) {
+                fetch(piece);
+                const int valid = piece.rank - piece.k - 8 * lh;
+                float bad = 0.0f;
+#pragma unroll
+                for (int b = 0; b < CB; ++b) {
+                    if (valid < 8) ahead.f[b] = first_of(ahead.f[b], valid);
+                    bad += zero_times(ahead.f[b]);
+                    ahead.f[b] ^= finite_of(ahead.f[b]);
+                }
+                if (!any_not_finite(bad)) continue;
+#pragma unroll
+                for (int a = 0; a < RB; ++a)
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) {
+                        f32x16 sum;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
+                        sum = mfma_bf16(ahead.f[b], ahead.x[a], sum);
+                        u32x4* const d = reinterpret_cast<u32x4*>(lds + ((wr * RB + a) * 32 + lj) * L::opitch + ((wc * CB + b) * 32 + 16 * lh) * 2);
+                        if (mine[a] != piece.a) continue;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            u32x4 y = d[h];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                y[i] = pack2_bf16(__builtin_bit_cast(float, y[i] << 16) + sum[8 * h + 2 * i], __builtin_bit_cast(float, y[i] & 0xffff0000u) + sum[8 * h + 2 * i + 1]);
+                            d[h] = y;
+                        }
+                    }
+            }
     lds_barrier();
     constexpr int CPR = L::TN / 8;
     const rsrc_t yres = make_rsrc(g.Y + row0 * g.Q + col0, ((int64_t)(rows - 1) * g.Q + cols) * 2);

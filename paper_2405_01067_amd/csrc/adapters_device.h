@@ -4,6 +4,7 @@
 #include <atomic>
 
 #include "adapters.h"
+#include "adapters_operands.h"
 
 namespace abt {
 namespace {

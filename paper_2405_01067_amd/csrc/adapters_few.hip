@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "adapters.h"
+#include "adapters_operands.h"
 
 namespace abt {
 namespace {
@@ -206,6 +207,7 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
     const int rank0 = g.ranks && id >= 0 ? gload(g.ranks + id) : g.r;
     const rsrc_t eres = make_rsrc(g.E + (int64_t)row0 * g.r, (int64_t)rows * g.r * 2);
     uint64_t left = __ballot(id >= 0);
+    float bad = 0.0f;
     for (int k = 0; left;) {
         uint64_t of[4] = {0, 0, 0, 0};             // its rows
         rsrc_t fres[4];
@@ -238,6 +240,7 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
                 if (!of[q]) break;
                 const int rank = __builtin_amdgcn_readlane(rank0, who[q]);
                 if (rank - j < 32) f[q] = first_of(f[q], rank - c);            // (T is zero there)
+                bad += zero_times(f[q]);
 #pragma unroll
                 for (int b = 0; b < RB; ++b) acc[b] = mfma16(f[q], t[q][b], acc[b]);
             }
@@ -246,6 +249,31 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
     // lane: row 16 b + li, columns 4 lq .. + 3
 #pragma unroll
     for (int b = 0; b < RB; ++b) sums[(wave * RB + b) * 64 + lane] = acc[b];
+    // Where an adapter is not finite: all of it again, each into its own rows alone.
+    if (any_not_finite(bad)) {
+#pragma unroll
+        for (int b = 0; b < RB; ++b) sums[(wave * RB + b) * 64 + lane] = f32x4{0, 0, 0, 0};
+        left = __ballot(id >= 0);
+        for (int k = 0; left; ++k) {
+            const int first = __builtin_ctzll(left), a = __builtin_amdgcn_readlane(id, first), rank = __builtin_amdgcn_readlane(rank0, first);
+            const uint64_t same = __ballot(id == a);
+            left &= ~same;
+            if ((k & 7) != wave) continue;
+            const rsrc_t fres = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * g.r, (int64_t)cols * g.r * 2);
+            for (int j = 0; j < g.r; j += 32) {
+                const int c = j + lq * 8;
+                const u32x4 f = first_of(buf_load16(fres, c < g.r ? (li * g.r + c) * 2 : kBufNowhere, 0), rank - c);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    const bool own = (same >> (16 * b + li)) & 1;
+                    const u32x4 t = buf_load16(eres, c < g.r && own ? ((16 * b + li) * g.r + c) * 2 : kBufNowhere, 0);
+                    f32x4& to = sums[(wave * RB + b) * 64 + lane];
+                    const f32x4 sum = mfma16(f, t, to);
+                    if (own) to = sum;
+                }
+            }
+        }
+    }
     __syncthreads();
     if (!out) return;
 #pragma unroll
@@ -353,7 +381,8 @@ __global__ __launch_bounds__(512) void few_one_kernel(const AdapterProduct g, co
             const int c = j + lq * 8;
             const u32x4 f = first_of(buf_load16(fres, c < r ? (li * r + c) * 2 : kBufNowhere, 0), rank - c);
             const u32x4 e = (same >> li) & 1 ? *reinterpret_cast<const u32x4*>(ts + li * kOnePitch + c) : u32x4{0, 0, 0, 0};
-            acc = mfma16(f, e, acc);
+            const f32x4 sum = mfma16(f, e, acc);
+            acc = (same >> li) & 1 ? sum : acc;           // (zero times an infinity is NaN in the other rows)
         }
     }
     sums[wave * 64 + lane] = acc;
