@@ -449,7 +449,7 @@ size_t lr_rms_norm_bwd_workspace_bytes(int64_t M, int64_t n, int dt);
 /* -------------------------------------------------------------------------------------
  * Clipping by the global norm N = sqrt(sum of g^2 over all tensors), between the backward and ab_adamw_step:
  *     g' = c g,   c = max_norm / N where N > max_norm, else 1
- * Squares are summed in fp64 in a fixed order.  Where N is not finite nothing is scaled or stepped: the caller sees it in norm_out.
+ * Squares are summed in fp64 in a fixed order.  Where N, as the fp32 value of norm_out, is not finite nothing is scaled or stepped.
  * `tensors` is a HOST array read before the call returns; per tensor grad (DEVICE, fp32 or bf16 by dt), out (DEVICE, the same type, NULL: in
  * place), count (0 .. 2^40).  All pointers 16-byte aligned; outputs must not overlap but with their own grad, whole.
  * norm_out: one fp32 in device memory receiving N (before clipping); may be NULL but for ab_grad_norm.

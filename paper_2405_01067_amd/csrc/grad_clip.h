@@ -22,7 +22,8 @@ __device__ __forceinline__ double norm_of(const double* sums, int nsums) {
     return sqrt(part[0] + part[1] + part[2] + part[3]);
 }
 
-__device__ __forceinline__ bool norm_finite(double N) { return N <= 1.7976931348623157e308; }      // false for NaN too
+// As it is reported, in fp32: the caller has to see what happened.  (False for NaN too.)
+__device__ __forceinline__ bool norm_finite(double N) { return (float)N <= 3.4028234663852886e38f; }
 // A norm that is not finite scales nothing.
 __device__ __forceinline__ float clip_factor(double N, double max_norm) { return N > max_norm && norm_finite(N) ? (float)(max_norm / N) : 1.0f; }
 
