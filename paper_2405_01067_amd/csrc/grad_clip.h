@@ -24,7 +24,15 @@ __device__ __forceinline__ double norm_of(const double* sums, int nsums) {
 
 // As it is reported, in fp32: the caller has to see what happened.  (False for NaN too.)
 __device__ __forceinline__ bool norm_finite(double N) { return (float)N <= 3.4028234663852886e38f; }
+// The factor as a product: where fp32 would hold it with fewer bits (below 2^-126), `second` is a power of two, otherwise 1.
+struct ClipFactor {
+    float first, second;
+    __device__ __forceinline__ float operator()(float g) const { return first * g * second; }
+};
 // A norm that is not finite scales nothing.
-__device__ __forceinline__ float clip_factor(double N, double max_norm) { return N > max_norm && norm_finite(N) ? (float)(max_norm / N) : 1.0f; }
+__device__ __forceinline__ ClipFactor clip_factor(double N, double max_norm) {
+    const double c = N > max_norm && norm_finite(N) ? max_norm / N : 1.0;
+    return c < 0x1p-126 ? ClipFactor{(float)(c * 0x1p126), 0x1p-126f} : ClipFactor{(float)c, 1.0f};
+}
 
 }  // namespace abt

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const GradTable a, const
             if (e + 8 <= here) v[i] = gload(reinterpret_cast<const u32x4*>(g + e));
         }
         const double N = norm_of(sums, nsums);
-        const float c = clip_factor(N, max_norm);
+        const ClipFactor c = clip_factor(N, max_norm);
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)N;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -118,10 +118,10 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const GradTable a, const
             if (e + 8 <= here) {
                 u32x4 w;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = pack2_bf16(c * bf16_value(v[i][j] & 0xffffu), c * __builtin_bit_cast(float, v[i][j] & 0xffff0000u));
+                for (int j = 0; j < 4; ++j) w[j] = pack2_bf16(c(bf16_value(v[i][j] & 0xffffu)), c(__builtin_bit_cast(float, v[i][j] & 0xffff0000u)));
                 gstore(reinterpret_cast<u32x4*>(o + e), w);
             } else {
-                for (int j = e; j < here; ++j) gstore(o + j, (uint16_t)(pack2_bf16(c * bf16_value(gload(g + j)), 0.0f) & 0xffffu));
+                for (int j = e; j < here; ++j) gstore(o + j, (uint16_t)(pack2_bf16(c(bf16_value(gload(g + j))), 0.0f) & 0xffffu));
             }
         }
     } else {
@@ -134,15 +134,15 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const GradTable a, const
             if (e + 4 <= here) v[i] = gload(reinterpret_cast<const f32x4*>(g + e));
         }
         const double N = norm_of(sums, nsums);
-        const float c = clip_factor(N, max_norm);
+        const ClipFactor c = clip_factor(N, max_norm);
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)N;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int e = (i * kThreads + (int)threadIdx.x) * 4;
             if (e + 4 <= here) {
-                gstore(reinterpret_cast<f32x4*>(o + e), f32x4{c * v[i][0], c * v[i][1], c * v[i][2], c * v[i][3]});
+                gstore(reinterpret_cast<f32x4*>(o + e), f32x4{c(v[i][0]), c(v[i][1]), c(v[i][2]), c(v[i][3])});
             } else {
-                for (int j = e; j < here; ++j) gstore(o + j, c * gload(g + j));
+                for (int j = e; j < here; ++j) gstore(o + j, c(gload(g + j)));
             }
         }
     }

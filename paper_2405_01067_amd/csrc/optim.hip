@@ -39,14 +39,14 @@ __device__ __forceinline__ AdamwOut adamw_element(float theta, float g, float m,
 // CLIP: the gradients count c times, with c from the sums of their squares (grad_clip.hip); where their norm is not finite nothing is written but the norm.
 template <bool CLIP>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTable a, const AdamwClip clip) {
-    float c = 1.0f;
+    ClipFactor c{1.0f, 1.0f};
     if constexpr (CLIP) {
         const double N = norm_of(clip.sums, clip.nsums);
         if (clip.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *clip.norm_out = (float)N;
         if (!norm_finite(N)) return;
         c = clip_factor(N, clip.max_norm);
     }
-    const auto clipped = [c](float g) { return CLIP ? c * g : g; };
+    const auto clipped = [c](float g) { return CLIP ? c(g) : g; };
     // blockIdx.x -> tensor: the table is short and wave-uniform, a linear scan is enough
     int ti = 0;
     while (ti + 1 < a.n && (int)blockIdx.x >= a.first_block[ti + 1]) ++ti;

@@ -29,3 +29,27 @@ def test_a_norm_that_is_reported_as_infinite_changes_nothing(dtype):
         assert float(abt.ab_adamw_step_clipped(table, max_norm=1.0, step=1, lr=0.1)) == float("inf")
         for t in table:
             assert all(bool((t[k] == 1).all()) for k in ("param", "exp_avg", "exp_avg_sq", "param_bf16"))
+
+
+# c = max_norm / N down to 1e-44, where an fp32 value has three bits.  The factor and the product round to fp32 (2^-24 each), bf16 once more, and values
+# below the normal range to a multiple of 2^-149.
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size,max_norm", [(1e36, 1.0), (3e36, 1.0), (1e36, 1e-3), (1e36, 1e-6), (1e30, 1e-9), (1e20, 1e-20)])
+def test_factors_below_the_range_of_fp32(size, max_norm, dtype):
+    gen = torch.Generator().manual_seed(2)
+    host = [(torch.randn((c,), generator=gen) * size).to(dtype) for c in (4099, 70)]
+    N = float(sum((t.double() ** 2).sum() for t in host)) ** 0.5
+    grads = [t.cuda() for t in host]
+    out = [torch.zeros_like(t) for t in grads]
+    norm = abt.ab_clip_grads(abt.GradPlan(grads, out=out), max_norm)
+    assert abs(float(norm) - N) <= 1.001 * 2.0 ** -24 * N
+    u = 2.0 ** -23 if dtype == torch.float32 else 2.0 ** -8 + 2.0 ** -22
+    least = 2.0 ** -149 if dtype == torch.float32 else 2.0 ** -133
+    for h, o in zip(host, out):
+        want = h.double() * (max_norm / N)
+        assert bool(((o.double().cpu() - want).abs() <= 1.0001 * u * want.abs() + least).all())
+    if dtype == torch.float32:
+        one, two = step_table(grads), step_table(out)
+        abt.ab_adamw_step_clipped(one, max_norm=max_norm, step=3, lr=0.1)
+        abt.ab_adamw_step(two, step=3, lr=0.1)
+        assert all(torch.equal(x[k], y[k]) for x, y in zip(one, two) for k in ("param", "exp_avg", "exp_avg_sq", "param_bf16"))
