@@ -44,8 +44,22 @@ class AdapterStack:
         for params, grads, copies in ((self.A, self.dA, self.Ab), (self.B, self.dB, self.Bb), (self.gains, self.dgains, [None] * len(self.gains))):
             table += [dict(param=p, grad=g, exp_avg=torch.zeros_like(p), exp_avg_sq=torch.zeros_like(p), param_bf16=c) for p, g, c in zip(params, grads, copies)]
         self.plan = abt.AdamwPlan(table)
-        self.steps = 0
+        self._steps, self._asked = 0, None                   # steps known to have been taken, and the one behind them that may have been
         self.W8 = None
+
+    @property
+    def steps(self) -> int:
+        """The steps that changed the stack (one that goes on from elsewhere sets it).  Waits for the norm of the last one."""
+        if self._asked is not None:
+            norm, done = self._asked
+            done.synchronize()
+            self._steps += bool(self.torch.isfinite(norm))
+            self._asked = None
+        return self._steps
+
+    @steps.setter
+    def steps(self, taken: int):
+        self._steps, self._asked = int(taken), None
 
     def forward(self, X, row_adapter, keep: bool = False):
         """The output [M, d] (bf16); with keep, also what `backward` needs."""
@@ -71,11 +85,16 @@ class AdapterStack:
 
     def train_step(self, X, row_adapter, loss_grad, lr: float, max_norm: float = 1.0, **hyper):
         """One step of every factor and gain: loss_grad(out) -> the gradient at the output (bf16).  Returns the gradients' global norm
-        before clipping (a 0-d fp32 GPU tensor); a step whose norm is not finite changes nothing."""
+        before clipping (a 0-d fp32 GPU tensor); a step whose norm is not finite changes nothing, and is not counted in the bias corrections
+        of those after it.  So the host waits for the norm of the step before, once this one's gradients are enqueued."""
         out, kept = self.forward(X, row_adapter, keep=True)
         self.backward(loss_grad(out), kept, row_adapter)
-        self.steps += 1
-        return abt.ab_adamw_step_clipped(self.plan, max_norm=max_norm, step=self.steps, lr=lr, **hyper)
+        norm = abt.ab_adamw_step_clipped(self.plan, max_norm=max_norm, step=self.steps + 1, lr=lr, **hyper)
+        on_host = self.torch.empty((), dtype=norm.dtype, pin_memory=True)
+        on_host.copy_(norm, non_blocking=True)
+        self._asked = (on_host, self.torch.cuda.Event())
+        self._asked[1].record()
+        return norm
 
     def freeze(self):
         """The dense weights once more in 8 bits (e4m3) with a scale per output, for `serve`."""
