@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "abtrain.h"
+#include "grad_table.h"
 
 namespace abt {
 
@@ -331,8 +332,6 @@ struct AdamwClip { const double* sums; float* norm_out; double max_norm; int nsu
 hipError_t launch_adamw(const AdamwTensor* tensors, int n, const AdamwHyper& h, hipStream_t s, const AdamwClip* clip = nullptr);
 
 // ------------------------------------------------------------------ global norm of the gradients
-constexpr int kGradMaxTensors = 128;      // per launch
-struct GradTensor { const void* grad; void* out; int64_t count; bool bf16; };   // count up to 2^40
 int grad_sums_capacity(int n);            // values that launch_grad_sums may write for n tensors
 hipError_t launch_grad_sums(const GradTensor* t, int n, double* sums, int* nsums, hipStream_t s);
 hipError_t launch_grad_norm(const double* sums, int nsums, float* norm_out, hipStream_t s);

@@ -5,6 +5,8 @@
 // c g without writing c g.  Squares are added in fp64: no overflow or underflow of a square, and the rate of fp64 is far
 // above that of the loads.  Every sum has a fixed order.  Both passes are bound by memory where there is much of it: 36 tensors of 19 M elements 25.7 us (77 MB, 3.0 TB/s, what the
 // step before left in the last-level cache included); 6 tensors of 100 thousand elements 4.3 us either pass, a load, the sum and a launch.
+#include <climits>
+
 #include "grad_clip.h"
 
 namespace abt {
@@ -14,16 +16,6 @@ constexpr int kSumThreads = 1024;
 constexpr int kSumChunk = 16 * 1024;           // elements that a work-group takes at a time
 constexpr int kThreads = 256;
 constexpr int kChunk = kThreads * 16;
-
-struct GradTable {
-    const void* grad[kGradMaxTensors];
-    void* out[kGradMaxTensors];
-    int64_t count[kGradMaxTensors];
-    int first[kGradMaxTensors + 1];            // chunks [first[i], first[i + 1]) are those of tensor i
-    uint64_t bf16[kGradMaxTensors / 64];       // types
-    int n;
-};
-static_assert(sizeof(GradTable) <= 3840 && kGradMaxTensors % 64 == 0, "kernel arguments");
 
 // The tensor that a chunk belongs to: the last one with first <= chunk (tensors without elements are not in the table).
 __device__ __forceinline__ int tensor_of(const int* first, int n, int chunk) {
@@ -148,38 +140,16 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const GradTable a, const
     }
 }
 
-struct Tables {                                // the next table of tensors with elements, in chunks of `chunk`
-    const GradTensor* t;
-    int n, at = 0;
-    bool next(GradTable& a, int chunk, int& chunks) {
-        a = GradTable{};
-        chunks = 0;
-        while (at < n && a.n < kGradMaxTensors) {
-            const GradTensor& x = t[at];
-            const int64_t nb = ceil_div(x.count, chunk);
-            if (nb > (1 << 30) - chunks) break;                    // (a tensor has at most 2^40 elements)
-            ++at;
-            if (nb == 0) continue;
-            a.grad[a.n] = x.grad; a.out[a.n] = x.out; a.count[a.n] = x.count; a.first[a.n] = chunks;
-            if (x.bf16) a.bf16[a.n >> 6] |= 1ull << (a.n & 63);
-            chunks += (int)nb;
-            ++a.n;
-        }
-        a.first[a.n] = chunks;
-        return a.n > 0;
-    }
-};
-
 }  // namespace
 
 int grad_sums_capacity(int n) { return 256 * (n < 1 ? 1 : (int)ceil_div(n, kGradMaxTensors) + 1); }
 
 hipError_t launch_grad_sums(const GradTensor* t, int n, double* sums, int* nsums, hipStream_t s) {
-    Tables tables{t, n};
+    GradTables tables(t, n);
     GradTable a;
     int chunks, used = 0;
     const int room = grad_sums_capacity(n);
-    while (tables.next(a, kSumChunk, chunks)) {
+    while (tables.next(a, kSumChunk, INT_MAX - 256, chunks)) {
         const int blocks = chunks < 256 ? chunks : 256;
         if (used + blocks > room) return hipErrorInvalidValue;
         hipLaunchKernelGGL(sum_squares_kernel, dim3((unsigned)blocks), dim3(kSumThreads), 0, s, a, chunks, sums + used);
@@ -197,11 +167,11 @@ hipError_t launch_grad_norm(const double* sums, int nsums, float* norm_out, hipS
 }
 
 hipError_t launch_grad_clip(const GradTensor* t, int n, const double* sums, int nsums, double max_norm, float* norm_out, hipStream_t s) {
-    Tables tables{t, n};
+    GradTables tables(t, n);
     GradTable a;
     int chunks;
     bool any = false;
-    while (tables.next(a, kChunk, chunks)) {
+    while (tables.next(a, kChunk, kGradMaxBlocks, chunks)) {
         hipLaunchKernelGGL(clip_kernel, dim3((unsigned)chunks), dim3(kThreads), 0, s, a, sums, nsums, max_norm, any ? nullptr : norm_out);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
