@@ -15,24 +15,6 @@
 namespace abt {
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-
-// Products of 8-bit floats are added eight at a time, each cut at 2^-13 of the largest of the eight (also by the other 8-bit forms; bf16 keeps fp32): up to 1.7e-5 of
-// the sum of the sizes was measured, next to 6 % in either operand's rounding.  Its results may only be used where all lanes go: the compiler
-// moves this instruction, unlike that for bf16, into a branch that holds all its uses, where only that branch's lanes would get operands.
-__device__ __forceinline__ f32x16 mfma_f8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x16 c) {
-    const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-    const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);       // scales of 2^0
-}
-
-// the first `valid` (less than eight, may be negative) of eight bf16 values, zeros behind them
-__device__ __forceinline__ u32x4 first_of(u32x4 v, int valid) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] &= valid >= 2 * i + 2 ? 0xffffffffu : valid == 2 * i + 1 ? 0xffffu : 0u;
-    return v;
-}
-
 // The smallest of the lanes' values, INT_MAX where none is left
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
@@ -48,19 +30,19 @@ __device__ __forceinline__ int rank_of(const AdapterProduct& g, int a) {
 }
 
 // ------------------------------------------------------------------------------------------ Y
-// WM x WN waves, each RB x CB blocks of 32 x 32.  X's parts of slabs are requested LX slabs ahead, W's LW ahead (they come from L2): at most LX.
-template <int TM_, int TN_, int WM_, int WN_, int LX_, int LW_>
+// WM x WN waves, each RB x CB blocks of 32 x 32.  Slabs are requested AHEAD of their turn.
+template <int TM_, int TN_, int WM_, int WN_, int AHEAD_>
 struct Tile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, LX = LX_, LW = LW_, NW = WM * WN;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, AHEAD = AHEAD_, NW = WM * WN;
     static constexpr int RB = TM / (32 * WM), CB = TN / (32 * WN);
-    static constexpr int xpart = TM * 128, wpart = TN * 128, wbase = (LX + 1) * xpart, ring = wbase + (LW + 1) * wpart;
+    static constexpr int xpart = TM * 128, wpart = TN * 128, wbase = (AHEAD + 1) * xpart, ring = wbase + (AHEAD + 1) * wpart;
     static constexpr int NX = TM / 8 / NW, NF = TN / 8 / NW, NL = NX + NF;       // load instructions per wave and slab: eight rows each
     static constexpr int opitch = TN * 2 + 16;
     static constexpr int out = TM * opitch;
     static constexpr int lds = out > ring ? out : ring;
-    static constexpr int behind = (LX - 1) * NX + (LW - 1) * NF + (LX > LW ? NX : 0);       // loads issued after the last one of a slab
+    static constexpr int behind = (AHEAD - 1) * NL;       // loads issued after the last one of a slab
     static_assert(NX * 8 * NW == TM && NF * 8 * NW == TN && RB * 32 * WM == TM && CB * 32 * WN == TN, "");
-    static_assert(NW % 2 == 0 && LW >= 1 && (LX == LW || LX == LW + 1) && behind < 64 && lds <= 160 * 1024, "");
+    static_assert(NW % 2 == 0 && AHEAD >= 1 && behind < 64 && lds <= 160 * 1024, "");
 };
 
 struct Order { int row_tiles, col_tiles; };
@@ -100,23 +82,24 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
     auto offset = [&](int s) { return s * 128 + chunk < bytes ? lrow * bytes + s * 128 + chunk : kBufNowhere; };
     auto issue_x = [&](int s) {
         unsigned char* const dst = lds + xslot + wave * 1024;
-        xslot = xslot == L::LX * L::xpart ? 0 : xslot + L::xpart;
+        xslot = xslot == L::AHEAD * L::xpart ? 0 : xslot + L::xpart;
         const int off = offset(s), step = off == kBufNowhere ? 0 : 8 * NW * bytes;
 #pragma unroll
         for (int j = 0; j < L::NX; ++j) load_lds16(xres, dst + j * (NW * 1024), off + j * step, 0);
     };
     auto issue_w = [&](int s) {
         unsigned char* const dst = lds + wslot + wave * 1024;
-        wslot = wslot == L::wbase + L::LW * L::wpart ? L::wbase : wslot + L::wpart;
+        wslot = wslot == L::wbase + L::AHEAD * L::wpart ? L::wbase : wslot + L::wpart;
         const int off = offset(s), step = off == kBufNowhere ? 0 : 8 * NW * bytes;
 #pragma unroll
         for (int j = 0; j < L::NF; ++j) load_lds16(wres, dst + j * (NW * 1024), off + j * step, 0);
     };
 #pragma unroll
-    for (int s = 0; s < L::LX; ++s) {                     // in the order of the loop below
-        if (s >= L::LX - L::LW && s - L::LX + L::LW < nmain) issue_w(s - L::LX + L::LW);
-        if (s < nmain) issue_x(s);
-    }
+    for (int s = 0; s < L::AHEAD; ++s)                    // in the order of the loop below
+        if (s < nmain) {
+            issue_w(s);
+            issue_x(s);
+        }
 
     // the adapters of this lane's rows
     int mine[RB];
@@ -187,17 +170,19 @@ __device__ __forceinline__ void y_tile(const AdapterProduct& g, const Order& ord
     Piece piece = adapter(after(-1)), coming = piece.a == INT_MAX ? piece : adapter(after(piece.a));
     // Slab s has landed: loads come back in the order of issue.
     auto slab = [&](int s) {
-        if (s + L::LX > nmain) wait_newest<0>();
+        if (s + L::AHEAD > nmain) wait_newest<0>();
         else wait_newest<L::behind>();
         lds_barrier();
         // into the slots whose reads ended before this barrier
-        if (s + L::LW < nmain) issue_w(s + L::LW);
-        if (s + L::LX < nmain) issue_x(s + L::LX);
+        if (s + L::AHEAD < nmain) {
+            issue_w(s + L::AHEAD);
+            issue_x(s + L::AHEAD);
+        }
         if (s + 1 == nmain && piece.a != INT_MAX) fetch(piece);
     };
     auto next = [&]() {
-        xat = xat == L::LX * L::xpart ? 0 : xat + L::xpart;
-        wat = wat == L::wbase + L::LW * L::wpart ? L::wbase : wat + L::wpart;
+        xat = xat == L::AHEAD * L::xpart ? 0 : xat + L::xpart;
+        wat = wat == L::wbase + L::AHEAD * L::wpart ? L::wbase : wat + L::wpart;
     };
     Ops o[2];
     if constexpr (F8) {
@@ -364,12 +349,12 @@ hipError_t launch_tile(const AdapterProduct& p, hipStream_t s) {
 }
 
 // The tiles.  Two or three work-groups of the smaller ones share a compute unit, and while one starts or stores the others compute.
-using T256x256 = Tile<256, 256, 2, 4, 1, 1>;
-using T192x256 = Tile<192, 256, 2, 4, 1, 1>;
-using T128x192 = Tile<128, 192, 2, 2, 1, 1>;
-using T128x128 = Tile<128, 128, 2, 2, 1, 1>;
-using T64x128 = Tile<64, 128, 2, 2, 1, 1>;
-using T64x64 = Tile<64, 64, 2, 2, 2, 2>;
+using T256x256 = Tile<256, 256, 2, 4, 1>;
+using T192x256 = Tile<192, 256, 2, 4, 1>;
+using T128x192 = Tile<128, 192, 2, 2, 1>;
+using T128x128 = Tile<128, 128, 2, 2, 1>;
+using T64x128 = Tile<64, 128, 2, 2, 1>;
+using T64x64 = Tile<64, 64, 2, 2, 2>;
 
 // What a tile costs, us: a slab and the rest of a tile where the compute unit is shared by as many as fit, and where it has the unit to itself.  Fitted to
 // launches of all six at 54 shapes in both types (140 to 12608 rows, 768 to 4096 columns and contractions; r = 16, runs of 197 rows): the rule takes

@@ -15,28 +15,8 @@
 namespace abt {
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-
-__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-// Products of 8-bit floats are added eight at a time, each cut at 2^-13 of the largest of the eight (also by the other 8-bit forms; bf16 keeps fp32): up to 1.7e-5 of
-// the sum of the sizes was measured, next to 6 % in either operand's rounding.  Its results may only be used where all lanes go: the compiler
-// moves this instruction, unlike that for bf16, into a branch that holds all its uses, where only that branch's lanes would get operands.
-__device__ __forceinline__ f32x4 mfma16_f8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4 c) {
-    const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-    const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);      // scales of 2^0
-}
 __device__ __forceinline__ float lo(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
 __device__ __forceinline__ float hi(uint32_t v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
-
-// the first `valid` of eight bf16 values, zeros behind them (all of them from eight on, none below one)
-__device__ __forceinline__ u32x4 first_of(u32x4 v, int valid) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] &= valid >= 2 * i + 2 ? 0xffffffffu : valid == 2 * i + 1 ? 0xffffu : 0u;
-    return v;
-}
 
 // T of one row: row j of its adapter's B by each wave
 __device__ __forceinline__ void t_of_row(const AdapterProduct& g, const uint16_t* X, const uint16_t* B, int n, int64_t row, int j) {
@@ -285,19 +265,19 @@ __global__ __launch_bounds__(512) void few_second_kernel(const AdapterProduct g,
     gstore(reinterpret_cast<u32x2*>(g.Y + (int64_t)(row0 + row) * g.Q + col0 + c0), u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])});
 }
 
-// One launch where there is next to nothing to share: up to sixteen rows and 32 values of T in all, which every work-group computes for itself.  16
+// One launch where there is next to nothing to share: up to 32 values of T in all (at r = 8 four rows), which every work-group computes for itself.  16
 // columns a work-group, whose eight waves share out the contraction, the values of T and the adapters.
-constexpr int kOneT = 32, kOnePitch = 136;               // values of T; LDS values per row of T, rank columns and zeros behind them
+constexpr int kOneT = 32, kOneRows = kOneT / 8, kOnePitch = kOneT + 8;      // values of T; rows; LDS values per row of T, rank columns and zeros behind them
 template <bool F8>
 __global__ __launch_bounds__(512) void few_one_kernel(const AdapterProduct g, const uint16_t* X, const uint16_t* B) {
     __shared__ __align__(16) f32x4 sums[8 * 64];
-    __shared__ __align__(16) uint16_t ts[16 * kOnePitch];
+    __shared__ __align__(16) uint16_t ts[kOneRows * kOnePitch];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 15, lq = lane >> 4;
     const int M = (int)g.M, n = g.kmain, r = g.r;
     const int col0 = blockIdx.x * 16, cols = g.Q - col0 < 16 ? g.Q - col0 : 16;
     const int id0 = gload(g.row_adapter + (lane < M ? lane : 0));
-    for (int i = threadIdx.x; i < 16 * kOnePitch / 8; i += 512) *reinterpret_cast<u32x4*>(ts + 8 * i) = u32x4{0, 0, 0, 0};
+    if (threadIdx.x < kOneRows * kOnePitch / 8) *reinterpret_cast<u32x4*>(ts + 8 * threadIdx.x) = u32x4{0, 0, 0, 0};
     const int id = lane < M && id0 >= 0 && id0 < g.count ? id0 : -1;
     const int rank0 = g.ranks && id >= 0 ? gload(g.ranks + id) : r;
     const float scale0 = g.scales && id >= 0 ? gload(g.scales + id) : 1.0f;
@@ -308,7 +288,7 @@ __global__ __launch_bounds__(512) void few_one_kernel(const AdapterProduct g, co
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int v = wave + 8 * i, row = v / r;
-        const int a = row < M ? __builtin_amdgcn_readlane(id, row < 16 ? row : 0) : -1;
+        const int a = row < M ? __builtin_amdgcn_readlane(id, row) : -1;
         have[i] = a >= 0;
         xp[i] = X + (int64_t)(have[i] ? row : 0) * n;
         bp[i] = B + ((int64_t)(have[i] ? a : 0) * r + (v - row * r)) * n;
@@ -377,13 +357,11 @@ __global__ __launch_bounds__(512) void few_one_kernel(const AdapterProduct g, co
         left &= ~same;
         if ((k & 7) != wave) continue;
         const rsrc_t fres = make_rsrc(g.F + ((int64_t)a * g.Q + col0) * r, (int64_t)cols * r * 2);
-        for (int j = 0; j < r; j += 32) {
-            const int c = j + lq * 8;
-            const u32x4 f = first_of(buf_load16(fres, c < r ? (li * r + c) * 2 : kBufNowhere, 0), rank - c);
-            const u32x4 e = (same >> li) & 1 ? *reinterpret_cast<const u32x4*>(ts + li * kOnePitch + c) : u32x4{0, 0, 0, 0};
-            const f32x4 sum = mfma16(f, e, acc);
-            acc = (same >> li) & 1 ? sum : acc;           // (zero times an infinity is NaN in the other rows)
-        }
+        const int c = lq * 8;
+        const u32x4 f = first_of(buf_load16(fres, c < r ? (li * r + c) * 2 : kBufNowhere, 0), rank - c);
+        const u32x4 e = (same >> li) & 1 ? *reinterpret_cast<const u32x4*>(ts + li * kOnePitch + c) : u32x4{0, 0, 0, 0};
+        const f32x4 sum = mfma16(f, e, acc);
+        acc = (same >> li) & 1 ? sum : acc;               // (zero times an infinity is NaN in the other rows)
     }
     sums[wave * 64 + lane] = acc;
     __syncthreads();
@@ -395,7 +373,7 @@ __global__ __launch_bounds__(512) void few_one_kernel(const AdapterProduct g, co
 // Where the contraction is so short that its parts are not missed.  us, one launch / two, rows of W 768 x 768 5.9 / 7.2 (one row, r = 16) and 6.5 / 7.2 (two), 2304 x
 // 768 6.8 / 7.4 (two); 4096 x 2048 in 8 bits 8.3 / 8.4 (two), 4096 x 4096 15.3 / 13.3 and in 8 bits 11.7 / 9.6 (one).
 bool few_in_one(const AdapterProduct& p, bool fp8) {
-    return p.M <= 16 && p.M * p.r <= kOneT && (int64_t)p.kmain * (fp8 ? 1 : 2) <= 3072;
+    return p.M * p.r <= kOneT && (int64_t)p.kmain * (fp8 ? 1 : 2) <= 3072;
 }
 
 FewParts few_parts(int64_t M, int Q, int n, bool fp8) {

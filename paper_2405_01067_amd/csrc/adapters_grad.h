@@ -13,9 +13,6 @@ namespace {
 
 constexpr int kPiece = 64;                                // rows of a slab; pieces are whole slabs
 
-__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
 // VB blocks of 16 rank columns
 template <int VB>
 struct Grad {
@@ -125,7 +122,6 @@ __device__ __forceinline__ void grad_piece(const AdapterGrads& g, const Side& si
             for (int s = 0; s < ns; ++s) {
                 const int behind = issued - s - 1;
                 if (behind >= L::NS - 2) wait_newest<(L::NS - 2) * L::NL>();
-                else if (L::NS > 3 && behind == L::NS - 3) wait_newest<(L::NS > 3 ? L::NS - 3 : 0) * L::NL>();
                 else wait_newest<0>();
                 lds_barrier();
                 if (issued < ns) { issue(issued, issued % L::NS); ++issued; }
