@@ -357,20 +357,25 @@ using T64x128 = Tile<64, 128, 2, 2, 1>;
 using T64x64 = Tile<64, 64, 2, 2, 2>;
 
 // What a tile costs, us: a slab and the rest of a tile where the compute unit is shared by as many as fit, and where it has the unit to itself.  Fitted to
-// launches of all six at 54 shapes in both types (140 to 12608 rows, 768 to 4096 columns and contractions; r = 16, runs of 197 rows): the rule takes
-// the fastest or one 8 % slower at all but one of them, 0.8 % on average.  The ends of the range, us:
+// launches of all six at 54 shapes (140 to 12608 rows, 768 to 4096 columns and contractions; r = 16, runs of 197 rows) and looked at at 49 others: what the rule takes
+// is slower than the fastest by 1.0 and 1.3 % on average in bf16 (16 % at worst: 300 x 4096 x 1024), 0.1 and 0.6 % in 8 bits (11 % at worst: 900 x 3000 x 1200).  It puts
+// tiles in an order and is no time of a launch: 42 for the largest tile at 12608 x 2304 x 768, 127 for the smallest.  The ends of the range, us:
 //                      256x256   192x256   128x192   128x128   64x128    64x64
-//   140 x 768 x 768       20.4      16.6      12.4       9.7      8.0      7.5
-//   1379 x 2304 x 768     22.6      18.5      14.1      11.6     11.6     16.9
-//   12608 x 768 x 2304    53.8      45.5      47.5      61.3     56.3     74.0
-//   12608 x 2304 x 768    51.6      59.8      53.4      58.0     68.3     89.5
-//   8190 x 4096 x 4096   208.9     252.0     252.6     237.3    317.2    418.0        1320 TFLOP/s; 8 bits 110 us, 2490
+//   140 x 768 x 768       19.9      16.3      13.2      10.3      8.3      7.5
+//   1379 x 2304 x 768     22.8      18.7      15.7      13.0     12.7     17.6
+//   12608 x 768 x 2304    61.4      52.2      54.4      64.0     61.5     87.9
+//   12608 x 2304 x 768    56.1      62.2      54.4      58.4     68.6     99.6
+//   8190 x 4096 x 4096   223.5     242.9     262.0     248.1    316.4    419.7        1230 TFLOP/s
+//     in 8 bits          130.9     145.3     203.1     135.5    169.1    217.6        2100 TFLOP/s
 struct TileCost { int tm, tn, per_cu; float slab, rest, alone_slab, alone_rest; };
-constexpr TileCost kTiles[] = {{256, 256, 1, 1.27f, 5.86f, 1.27f, 5.86f}, {192, 256, 1, 0.94f, 6.01f, 0.94f, 6.01f}, {128, 192, 2, 0.55f, 2.79f, 0.61f, 5.85f},
-                               {128, 128, 2, 0.46f, 2.66f, 0.56f, 5.33f}, {64, 128, 3, 0.27f, 1.36f, 0.56f, 2.22f},  {64, 64, 3, 0.27f, 1.30f, 0.33f, 2.65f}};
+constexpr TileCost kTiles[2][6] = {                       // bf16; 8 bits, where 128 x 192 has registers for one work-group per compute unit only
+    {{256, 256, 1, 1.27f, 5.86f, 1.27f, 5.86f}, {192, 256, 1, 0.94f, 6.01f, 0.94f, 6.01f}, {128, 192, 2, 0.55f, 2.79f, 0.61f, 5.85f},
+     {128, 128, 2, 0.46f, 2.66f, 0.56f, 5.33f}, {64, 128, 3, 0.27f, 1.36f, 0.56f, 2.22f},  {64, 64, 3, 0.27f, 1.30f, 0.33f, 2.65f}},
+    {{256, 256, 1, 1.38f, 7.61f, 1.38f, 7.61f}, {192, 256, 1, 1.18f, 6.65f, 1.18f, 6.65f}, {128, 192, 1, 0.88f, 7.95f, 0.88f, 7.95f},
+     {128, 128, 2, 0.39f, 3.66f, 0.54f, 5.92f}, {64, 128, 3, 0.26f, 2.66f, 0.46f, 4.61f},  {64, 64, 3, 0.165f, 1.64f, 0.33f, 4.48f}}};
 constexpr int kTile128x192 = 2, kTile64 = 5;
 float tile_cost(int i, const AdapterProduct& p, bool fp8) {
-    const TileCost& t = kTiles[i];
+    const TileCost& t = kTiles[fp8][i];
     const int64_t tiles = ceil_div(p.M, t.tm) * ceil_div(p.Q, t.tn);
     const float slabs = (float)ceil_div((int64_t)p.kmain * (fp8 ? 1 : 2), 128);
     const float shared = (float)ceil_div(tiles, 256) * (slabs * t.slab + t.rest), alone = (float)ceil_div(tiles, 256 * t.per_cu) * (slabs * t.alone_slab + t.alone_rest);
@@ -808,9 +813,10 @@ hipError_t launch_adapters_dt(const AdapterProduct& p, const AdapterPrep& prep, 
 
 hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGrads& g, hipStream_t s) {
     if (g.M > kAdapterFewGradRows) return hipErrorInvalidValue;
-    // dX has the smallest tile here, and from r = 33 on one work-group fills a compute unit: it goes alone where its best tile saves 16 us, or from 400 tiles on.  us,
-    // together / apart: 2304 x 768, r = 16, 1024 rows 31.7 / 37.4; 2304 x 2304, r = 16, 911 rows 50.0 / 53.3 (its best tile: 11 us less); 1024 x 1024, r = 64, 1024 rows (256
-    // tiles) 45.6 / 46.4; 768 x 2304, r = 48, 700 rows (396) 34.8 / 38.6, 911 (540) 46.1 / 43.6; 88 x 3272, r = 120, 512 rows (416) 46.6 / 44.2, 1024 (832) 77.4 / 63.6.
+    // dX has the smallest tile here, and from r = 33 on one work-group fills a compute unit: it goes alone where its best tile costs 16 less, or from 400 tiles on.  us,
+    // together / apart, r = 16 (what the best tile costs less): 1024 x 2304 x 768 28.4 / 35.9 (0), 911 x 2304 x 2304 45.5 / 46.9 (11), 1024 x 1024 x 4096 38.6 / 37.1 (11), 700 x 4096 x
+    // 4096 79.0 / 75.5 (18), 1024 x 4096 x 4096 91.8 / 83.0 (36), 1024 x 2048 x 8192 96.8 / 76.2 (45); r = 64 (tiles): 512 x 768 x 2304 30.9 / 34.6 (288), 700 x 768 x 2304 34.3 / 36.8
+    // (396), 911 x 768 x 2304 42.8 / 42.3 (540), 512 x 4096 x 4096 101 / 86 (512), 1024 x 4096 x 4096 167 / 123 (1024); but 300 x 4096 x 4096 81.1 / 72.6 (320).
     if (x && (g.r > 32 ? ceil_div(x->M, T64x64::TM) * ceil_div(x->Q, T64x64::TN) > 400
                        : tile_cost(kTile64, *x, false) > tile_cost(best_tile(*x, false), *x, false) + 16.0f)) {
         const hipError_t e = launch_adapters_y(*x, false, s);
@@ -826,8 +832,9 @@ hipError_t launch_adapters_few_dx_grads(const AdapterProduct* x, const AdapterGr
 }
 
 // Beside the gradients dX has one tile only, which may not be its best; the gradients' time (their bytes at 4 TB/s) is half hidden and a launch, 3.6 us, saved.
-// (From r = 33 on the gradients fill a compute unit alone.)  us, beside / apart: 768 x 768, r = 8 1500 rows 29.8 / 31.9, 12608 52.7 / 60.2; 2304 x 768, r = 16 1500
-// 52.2 / 47.6 (apart), 4096 54.9 / 57.3, 12608 83.1 / 95.9; 768 x 2304, r = 32 1500 38.4 / 46.7, 12608 95.7 / 107.7; 2304 x 2304, r = 16 4096 73.0 / 80.9.
+// (From r = 33 on the gradients fill a compute unit alone.)  us, beside / apart, r = 16, where the rule says beside: 1500 x 768 x 2304 30.4 / 34.9, 3000 x 2304 x 2304
+// 66.0 / 65.8, 4096 x 2304 x 768 51.2 / 55.1, 12608 x 768 x 768 43.4 / 50.5, 12608 x 2304 x 768 77.6 / 89.0; apart: 1500 x 2304 x 768 50.4 / 45.5, 1500 x 4096 x 1024 74.4 / 60.8, 8190 x 4096 x 4096
+// 316 / 305; but 1500 x 768 x 768 26.1 / 28.9 and 6000 x 1536 x 1024 49.4 / 55.9 (of 34 shapes near the limit 14 are 2 to 13 % faster beside).
 bool adapters_dx_beside_grads(const AdapterProduct& x, const AdapterGrads& g) {
     const float grads = 2.0f * (float)g.M * (float)((g.dA ? g.m : 0) + (g.dB ? g.n : 0)) / 4e6f;
     return g.r <= 32 && tile_cost(kTile128x192, x, false) - tile_cost(best_tile(x, false), x, false) < 0.5f * grads + 3.6f;
