@@ -437,7 +437,7 @@ size_t lr_adapters_bwd_workspace_bytes(int64_t M, int64_t m, int64_t n, int64_t 
  * none): dX = dH + s (dY gain - H s^2 mean_j(dY gain H)) of type dt, the gradient of X and of the residual, and dgain [n] = sum_i dY H s
  * (fp32; accumulate != 0 adds).  Either may be NULL; the workspace is only needed for dgain.  dX may be dH, dY or H itself.  Fixed summation order.
  * Statistics in fp32.  M >= 1, n a multiple of 8, at most ABT_RMS_NORM_MAX_WIDTH; eps >= 0 and finite (with eps = 0, or one that is 0 in fp32, a row of zeros is
- * 0 / 0: NaN, in dgain too).  Nothing blocks the host; can be captured.
+ * 0 / 0: NaN, in dgain too; a mean square beyond fp32, of values from 1.8e19 on, makes s = 0).  Nothing blocks the host; can be captured.
  * ------------------------------------------------------------------------------------- */
 #define ABT_RMS_NORM_MAX_WIDTH 16384
 int lr_rms_norm_fwd(const void* X, const void* residual, const float* gain, double eps, void* H, void* Y,

@@ -401,7 +401,7 @@ hipError_t launch_y(const AdapterProduct& p, hipStream_t s) {
 
 // dX and the factor gradients in one launch, the tiles of dX first: of few rows neither fills the chip; of many one is bound by the matrix unit and the
 // other by memory, and a work-group of each fits a compute unit beside the other.
-// 12608 x 2304 x 768, r = 16: 59 us for both (dX alone 51, the gradients 24.5); 394 x 768 x 768, r = 8: 8.2.
+// 12608 x 2304 x 768, r = 16: 61 us for both (dX alone 51, the gradients 24.5); 394 x 768 x 768, r = 8: 7.9.
 template <class L, int VB>
 __global__ __launch_bounds__(256, 2) void adapters_dx_grad_kernel(const AdapterProduct x, const Order order, const AdapterGrads g, const Side a, const Side b, int piece) {
     extern __shared__ __align__(1024) unsigned char lds[];

@@ -6,7 +6,7 @@
 //   second   adds the parts in order, and the adapters: 16 columns a work-group, eight waves that share out the adapters of the rows.
 // A row or two of narrow adapters go in one launch.
 // Bound by the bytes of W and of the adapters in use, and by the latency of two launches where these are few: 48 rows of 4096 x 4096 in 8 bits with 24 adapters of r = 16
-// 8.9 and 6.0 us (23 MB, 1.6 TB/s; a copy's rate would be 4.9 us); one row of 768 x 768, r = 8, 5.9 us (1.2 MB).
+// 10.0 and 5.8 us (23 MB, 1.5 TB/s; a copy's rate would be 4.9 us); one row of 768 x 768, r = 8, 5.9 us (1.2 MB).
 #include <type_traits>
 
 #include "adapters.h"

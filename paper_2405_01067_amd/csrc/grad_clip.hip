@@ -3,8 +3,8 @@
 // Two passes over the gradients, as c is known only after the first: one launch sums squares (256 work-groups at most, so that
 // whoever needs N afterwards adds up one value per thread), the next takes the sums, forms c and scales, or runs the AdamW step on
 // c g without writing c g.  Squares are added in fp64: no overflow or underflow of a square, and the rate of fp64 is far
-// above that of the loads.  Every sum has a fixed order.  Both passes are bound by memory where there is much of it: 36 tensors of 19 M elements 25.7 us (77 MB, 3.0 TB/s, what the
-// step before left in the last-level cache included); 6 tensors of 100 thousand elements 4.3 us either pass, a load, the sum and a launch.
+// above that of the loads.  Every sum has a fixed order.  Both passes are bound by memory where there is much of it: 36 tensors of 19 M elements 25.2 us (76 MB, 3.0 TB/s, what the
+// step before left in the last-level cache included); 6 tensors of 100 thousand elements 4.3 and 4.5 us, a load, the sum and a launch.
 #include <climits>
 
 #include "grad_clip.h"

@@ -4,8 +4,8 @@
 // A row stays in registers from its one read to its last write: one wave per row up to 2048 columns, a work-group of four
 // waves per row beyond (two waves in a range of the backward).  The backward forms s again from h, which it has in registers anyway, so the forward keeps nothing for it.
 // Statistics and gradients of the gain are fp32; y is formed from h before h is rounded.  Bound by memory: 50432 x 768
-// in bf16 with the residual 61 us (310 MB, 5.1 TB/s; part of it from the last-level cache); backward of 12608 x 768 17.9 us and 3.9 for the gain's sums (77 MB, 4.3 TB/s); 48 x 4096 with 8
-// bits 4.1 us, latency of the load, two sums over the work-group and the stores.
+// in bf16 with the residual 61 us (310 MB, 5.1 TB/s; part of it from the last-level cache); backward of 12608 x 768 17.9 us and 4.0 for the gain's sums (77 MB, 4.3 TB/s); 48 x 4096 with 8
+// bits 4.2 us, latency of the load, two sums over the work-group and the stores.
 #include <type_traits>
 
 #include "common.h"
