@@ -78,3 +78,24 @@ def test_backward(M, m, n, r, K, rows):
     row = torch.zeros_like(dB, dtype=torch.bool)
     row[a, 0] = True
     only(dB, clean[2], row, "dB")
+
+
+@pytest.mark.parametrize("M,m,n,r,K,rows", SIZES)
+def test_all_but_one(M, m, n, r, K, rows):
+    """Every adapter but the first is nothing but NaN and infinities, up to ranks that end inside a piece and past them: the first one's rows and those of
+    none are what they were, the others have no finite value but where their rank is 0."""
+    d, (ids, _, scales), _, _ = case(M, m, n, r, K, rows)
+    ranks = torch.tensor([r if a == 0 else (r, 5, 0, r - 3)[a % 4] for a in range(K)], dtype=torch.int32, device="cuda")
+    of = (ids, ranks, scales)
+    broken = (ids > 0) & (ranks[ids.clamp(min=0).long()] > 0)
+    A, B = d["A"].clone(), d["B"].clone()
+    A[1::2], A[2::2], B[1::2], B[2::2] = float("nan"), float("inf"), float("-inf"), float("nan")
+    Y, T = abt.lr_adapters_fwd(d["X"], d["W"], d["A"], d["B"], *of)
+    got, T1 = abt.lr_adapters_fwd(d["X"], d["W"], A, d["B"], *of)
+    assert torch.equal(T, T1)
+    only(got, Y, broken[:, None].expand_as(Y), "Y, A broken")
+    only(abt.lr_adapters_fwd(d["X"], d["W"], A, B, *of)[0], Y, broken[:, None].expand_as(Y), "Y, both broken")
+    clean = abt.lr_adapters_bwd(d["dY"], d["X"], T, d["W"], d["A"], d["B"], *of)
+    dX, dA, dB = abt.lr_adapters_bwd(d["dY"], d["X"], T, d["W"], A, B, *of)
+    only(dX, clean[0], broken[:, None].expand_as(dX), "dX")
+    assert torch.equal(dA, clean[1]) and torch.equal(dB[0], clean[2][0])
