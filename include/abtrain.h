@@ -18,7 +18,7 @@
  *     caller; the library never allocates, frees or retains caller memory.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  lr_linear_fwd,
  *     lr_linear_bwd, lr_linear_bwd_static, lr_linear_fwd_grouped, lr_linear_bwd_grouped, lr_conv_fwd, lr_conv_bwd,
- *     ab_adamw_step, ab_reconstruct, lr_adapters_*, lr_rms_norm_*, ab_grad_norm, ab_clip_grads and ab_adamw_step_clipped
+ *     ab_adamw_step, ab_reconstruct, lr_adapters_*, lr_rms_norm_*, lr_dense_*, lr_dropout, ab_grad_norm, ab_clip_grads and ab_adamw_step_clipped
  *     enqueue work on it and return without synchronising the host.  Calls that DO block the host:
  *       ab_merge, ab_merge_batched, ab_factorize, ab_factorize_batched: once after uploading
  *         their layer tables (tables of up to 7680 bytes, which one or two layers may have, travel in
@@ -472,6 +472,56 @@ int ab_adamw_step_clipped(const abt_adamw_tensor* tensors, int n, int64_t step,
                           double weight_decay, double max_norm, float* norm_out,
                           void* workspace, size_t workspace_bytes, void* stream);
 size_t ab_grad_norm_workspace_bytes(int n);
+
+/* -------------------------------------------------------------------------------------
+ * The trained dense layer of the full-rank phases (warm-up, rebound), with what stands at a layer's end in its epilogue:
+ *     Z = X W^T + bias          Y = residual + drop(act(Z))
+ * X [M, n], W [m, n], residual, Y, Z_save [M, m] bf16, bias [m] fp32; bias, residual, dropout may be NULL, and so may Z_save, which receives Z rounded to
+ * bf16 (what lr_dense_bwd needs where there is an activation).  Y comes from Z before it is rounded; the only rounding is Y's own.
+ * A factored layer has the same end with two calls, T = lr_dense_fwd(X, B) and Y = lr_dense_fwd(T, A, bias, ..).
+ *   act: ABT_ACT_RELU max(z, 0), ABT_ACT_GELU z Phi(z), ABT_ACT_GELU_TANH its form with tanh, ABT_ACT_SILU z / (1 + exp(-z)), in fp32.  NaN stays NaN; at
+ *   infinities the last three are what the formulas give in floating point, which may be NaN.
+ *   dropout: see abt_dropout; element (i, j) of Y is element i m + j of its mask.
+ * lr_dense_bwd, from dY [M, m] bf16 and the forward's X, W, Z (bf16, NULL without an activation), act and dropout:
+ *     dZ = act'(Z) drop(dY),   dX = dZ W (bf16),   dW = dZ^T X [m, n],   dbias = sum of the rows of dZ [m]   (fp32; accumulate != 0 adds into dW and dbias)
+ *   The residual's gradient is dY.  dX, dW, dbias: any may be NULL; W may then be NULL without dX, X without dW.  act'(0) = 0 for ABT_ACT_RELU.
+ *   dZ is rounded to bf16 once for dX (not without an activation or with ABT_ACT_RELU: then it is exact), and enters dW as two bf16 values, 16 bits or more.
+ *   Fixed summation order: two calls on the same inputs give bit-identical results.
+ * M from 1 to 2^28; m and n multiples of 8, at most 2^20.  bf16 only.  The outputs must not overlap the inputs (but Y may be the residual) or each other.
+ * Nothing blocks the host; all calls can be captured.
+ * Errors: ABT_EINVAL, ABT_EDTYPE (dt other than ABT_BF16), ABT_ESHAPE, ABT_EALIGN, ABT_EWORKSPACE, ABT_EHIP.
+ * ------------------------------------------------------------------------------------- */
+typedef enum {
+    ABT_ACT_NONE = 0,
+    ABT_ACT_RELU = 1,
+    ABT_ACT_GELU = 2,
+    ABT_ACT_GELU_TANH = 3,
+    ABT_ACT_SILU = 4
+} abt_activation;
+
+/* Dropout whose mask is computed where it is needed and never stored: drop(x) = x q / (q - t) for the elements that are kept, 0 for the others (also where x is
+ * not finite), with q = 2^16 and t = p q rounded to a whole number: an element is kept if its 16 random bits are t or more.  The bits of elements 8 b .. 8 b + 7 are
+ * the four words of Philox4x32-10 in order, low half first, for the counter (b, state[1] + site), two 64-bit numbers, low word first, and the key state[0].
+ * state: two 64-bit numbers in DEVICE memory, read by the kernels: a captured graph can be replayed with another seed or offset.  A forward and its backward need
+ * the same state and site; layers that share a state take sites of their own, and a training step adds more than the largest site to state[1].
+ * p in [0, 1]: 0 keeps everything, 1 drops everything. */
+typedef struct {
+    const uint64_t* state;        /* DEVICE: seed, offset; 8-byte aligned */
+    uint64_t site;
+    double p;
+} abt_dropout;
+
+int lr_dense_fwd(const void* X, const void* W, const float* bias, const void* residual, void* Y, void* Z_save,
+                 int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, void* stream);
+int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, void* dX, float* dW, float* dbias,
+                 int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, int accumulate,
+                 void* workspace, size_t workspace_bytes, void* stream);
+size_t lr_dense_bwd_workspace_bytes(int64_t M, int64_t m, int64_t n);
+
+/* Dropout by itself: Y = residual + drop(X) over `count` elements of type dt, of which element i is element i of the mask; the residual may be NULL.  Its backward
+ * is the same call: dX = lr_dropout(dY) without a residual, whose gradient is dY.  Y may be X or the residual itself.  count from 0 to 2^45.
+ * Errors: ABT_EINVAL (no state, p outside [0, 1]), ABT_EDTYPE, ABT_ESHAPE, ABT_EALIGN, ABT_EHIP. */
+int lr_dropout(const void* X, const void* residual, void* Y, int64_t count, const abt_dropout* dropout, int dt, void* stream);
 
 /* Work-group height of the bf16 chain kernel (T = X B^T, Y = T A^T and the dT / dX half of the
  * backward): 0 = chosen from the batch size (default), 64 or 128 = forced where the rank allows it.

@@ -32,6 +32,7 @@ EXPORTS = (
     "lr_adapters_fwd", "lr_adapters_fwd_q8", "lr_adapters_fwd_workspace_bytes", "lr_adapters_bwd", "lr_adapters_bwd_workspace_bytes",
     "lr_rms_norm_fwd", "lr_rms_norm_bwd", "lr_rms_norm_bwd_workspace_bytes",
     "ab_grad_norm", "ab_clip_grads", "ab_adamw_step_clipped", "ab_grad_norm_workspace_bytes",
+    "lr_dense_fwd", "lr_dense_bwd", "lr_dense_bwd_workspace_bytes", "lr_dropout",
 )
 
 
@@ -75,6 +76,12 @@ class GradTensor(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dt", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class DropoutArgs(ctypes.Structure):
+    """abt_dropout"""
+    _fields_ = [("state", ctypes.c_void_p), ("site", ctypes.c_uint64), ("p", ctypes.c_double)]
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}   # abt_activation
 MAX_GROUPS = 8   # ABT_MAX_GROUPS
 ADAPTERS_MAX_RANK = 128   # ABT_ADAPTERS_MAX_RANK
 
@@ -196,6 +203,15 @@ def load():
     lib.lr_rms_norm_bwd.argtypes = [vp, vp, vp, cd, vp, vp, vp, i64, i64, ci, ci, vp, sz, vp]
     lib.lr_rms_norm_bwd_workspace_bytes.restype = sz
     lib.lr_rms_norm_bwd_workspace_bytes.argtypes = [i64, i64, ci]
+    pdr = ctypes.POINTER(DropoutArgs)
+    lib.lr_dense_fwd.restype = ci
+    lib.lr_dense_fwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, pdr, ci, vp]
+    lib.lr_dense_bwd.restype = ci
+    lib.lr_dense_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, pdr, ci, ci, vp, sz, vp]
+    lib.lr_dense_bwd_workspace_bytes.restype = sz
+    lib.lr_dense_bwd_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.lr_dropout.restype = ci
+    lib.lr_dropout.argtypes = [vp, vp, vp, i64, pdr, ci, vp]
     lib.ab_grad_norm.restype = ci
     lib.ab_grad_norm.argtypes = [pgt, ci, vp, vp, sz, vp]
     lib.ab_clip_grads.restype = ci
@@ -1010,6 +1026,131 @@ def lr_rms_norm_bwd(dY, H, gain, eps: float = 1e-6, dH=None, need_dX: bool = Tru
                                _ptr(dgain if need_dgain else None), M, n, dt, int(bool(accumulate)), _ptr(ws),
                                ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "lr_rms_norm_bwd")
     return (dX if need_dX else None), (dgain if need_dgain else None)
+
+
+class Dropout:
+    """abt_dropout: elements are dropped with probability p (in steps of 2^-16), the same ones wherever state and site are the same.  state: a GPU tensor of
+    two int64, seed and offset, read when the kernels run: a training step adds more than its largest site to state[1] (on the GPU, so that a captured
+    step can be replayed with other masks).  site: which of the masks of a step, from 0."""
+
+    def __init__(self, p: float, state, site: int = 0):
+        torch = _torch()
+        if not 0.0 <= float(p) <= 1.0:
+            raise AbtError("p must be from 0 to 1")
+        if state.dtype != torch.int64 or state.shape != (2,) or not state.is_cuda or not state.is_contiguous():
+            raise AbtError("state must be a contiguous GPU tensor of two int64: seed, offset")
+        if not 0 <= int(site) < 1 << 63:
+            raise AbtError("site must be from 0 to 2^63 - 1")
+        self.p, self.state, self.site = float(p), state, int(site)
+        self.args = DropoutArgs(state.data_ptr(), self.site, self.p)
+
+
+def _dropout(dropout, device):
+    if dropout is None:
+        return None
+    if not isinstance(dropout, Dropout):
+        raise AbtError("dropout must be a Dropout")
+    if dropout.state.device != device:
+        raise AbtError("dropout's state must be on the operands' device")
+    return ctypes.byref(dropout.args)
+
+
+def _activation(act):
+    if act not in ACTIVATIONS:
+        raise AbtError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _on_this_device(first, others):
+    """The launch goes to the current device: every operand has to be there."""
+    index = _torch().cuda.current_device()
+    for t in (first, *others):
+        if t is not None and t.device.index != index:
+            raise AbtError(f"tensors must be on the current device (cuda:{index}), not on {t.device}")
+
+
+def lr_dense_fwd(X, W, bias=None, act: str = "none", dropout=None, residual=None, save_Z: bool = False, Y=None, Z=None):
+    """Y = residual + drop(act(Z)), Z = X W^T + bias, for X [M, n], W [m, n], residual [M, m] (bf16, GPU) and bias [m] fp32; act is none, relu, gelu,
+    gelu_tanh or silu, dropout a Dropout.  Returns (Y, Z) [M, m] bf16, Z for lr_dense_bwd (None without save_Z).  Y may be the residual."""
+    torch = _torch()
+    bf16 = torch.bfloat16
+    if X.dim() != 2 or W.dim() != 2:
+        raise AbtError("X must be [M, n], W [m, n]")
+    M, n = X.shape
+    m = W.shape[0]
+    _plain_matrix(X, "X", (M, n), bf16), _plain_matrix(W, "W", (m, n), bf16)
+    if bias is not None:
+        _plain_matrix(bias, "bias", (m,), torch.float32)
+    if residual is not None:
+        _plain_matrix(residual, "residual", (M, m), bf16)
+    if Y is None:
+        Y = X.new_empty((M, m))
+    else:
+        _plain_matrix(Y, "Y", (M, m), bf16)
+    if not save_Z:
+        Z = None
+    elif Z is None:
+        Z = X.new_empty((M, m))
+    else:
+        _plain_matrix(Z, "Z", (M, m), bf16)
+    _on_this_device(X, (W, bias, residual, Y, Z))
+    _check(load().lr_dense_fwd(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(), _ptr(Z), M, m, n, _activation(act),
+                               _dropout(dropout, X.device), ABT_BF16, _stream()), "lr_dense_fwd")
+    return Y, Z
+
+
+def lr_dense_bwd(dY, X, W, Z=None, act: str = "none", dropout=None, need_dX: bool = True, need_dW: bool = True, need_dbias: bool = True,
+                 dX=None, dW=None, dbias=None, accumulate: bool = False, workspace=None):
+    """Gradients of lr_dense_fwd from dY [M, m] and its X, W, Z (None without an activation), act and dropout: dX [M, n] bf16, dW [m, n] and dbias [m]
+    fp32.  Returns (dX, dW, dbias); skipped ones are None.  The residual's gradient is dY."""
+    torch = _torch()
+    lib = load()
+    bf16, f32 = torch.bfloat16, torch.float32
+    if X.dim() != 2 or W.dim() != 2:
+        raise AbtError("X must be [M, n], W [m, n]")
+    M, n = X.shape
+    m = W.shape[0]
+    _plain_matrix(dY, "dY", (M, m), bf16), _plain_matrix(X, "X", (M, n), bf16), _plain_matrix(W, "W", (m, n), bf16)
+    code = _activation(act)
+    if code and Z is None:
+        raise AbtError("an activation's gradient needs Z, which lr_dense_fwd returns with save_Z")
+    if Z is not None:
+        _plain_matrix(Z, "Z", (M, m), bf16)
+    out = []
+    for t, nm, need, shape, dtype in ((dX, "dX", need_dX, (M, n), bf16), (dW, "dW", need_dW, (m, n), f32), (dbias, "dbias", need_dbias, (m,), f32)):
+        if not need:
+            t = None
+        elif t is not None:
+            _plain_matrix(t, nm, shape, dtype)
+        elif accumulate and nm != "dX":
+            raise AbtError(f"accumulate needs existing {nm}")
+        else:
+            t = torch.empty(shape, dtype=dtype, device=X.device)
+        out.append(t)
+    dX, dW, dbias = out
+    ws = _workspace(lib.lr_dense_bwd_workspace_bytes(M, m, n), X.device, workspace)
+    _on_this_device(X, (dY, W, Z, dX, dW, dbias, ws))
+    _check(lib.lr_dense_bwd(dY.data_ptr(), X.data_ptr(), W.data_ptr(), _ptr(Z), _ptr(dX), _ptr(dW), _ptr(dbias), M, m, n, code, _dropout(dropout, X.device),
+                            ABT_BF16, int(bool(accumulate)), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "lr_dense_bwd")
+    return dX, dW, dbias
+
+
+def lr_dropout(X, dropout, residual=None, Y=None):
+    """Y = residual + drop(X) for a contiguous X (bf16 or fp32, GPU) of any shape and a residual of the same; the gradient of X is lr_dropout(dY, dropout).
+    Y may be X or the residual."""
+    if not isinstance(dropout, Dropout):
+        raise AbtError("dropout must be a Dropout")
+    _dev_tensor(X, "X")
+    dt = _dt(X)
+    if residual is not None:
+        _plain_matrix(residual, "residual", X.shape, X.dtype)
+    if Y is None:
+        Y = _torch().empty_like(X)
+    else:
+        _plain_matrix(Y, "Y", X.shape, X.dtype)
+    _on_this_device(X, (residual, Y))
+    _check(load().lr_dropout(X.data_ptr(), _ptr(residual), Y.data_ptr(), X.numel(), _dropout(dropout, X.device), dt, _stream()), "lr_dropout")
+    return Y
 
 
 def ab_reconstruct(A, B, W=None):

@@ -1,0 +1,70 @@
+// Activations and their slopes in fp32, two evaluations of the transcendental unit each.
+#pragma once
+
+#include <type_traits>
+
+#include "common.h"
+
+namespace abt {
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// The normal distribution below -|z|, and its density times sqrt(2 pi).  erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), to 1.5e-7 of 1 and a
+// few 1e-6 of itself (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).
+__device__ __forceinline__ float normal_tail(float z, float& density) {
+    const float t = rcp_fast(1.0f + 0.23164189f * __builtin_fabsf(z));             // p / sqrt(2)
+    density = exp2_fast(z * z * -0.72134752f);                                     // log2(e) / 2
+    return ((((1.061405429f * t - 1.453152027f) * t + 1.421413741f) * t - 0.284496736f) * t + 0.254829592f) * t * density * 0.5f;
+}
+// 1 / (1 + exp(-2 c (z + 0.044715 z^3))), c = sqrt(2 / pi): the sigmoid by which gelu_tanh multiplies (the tanh form is the same number)
+__device__ __forceinline__ float tanh_gate(float z) {
+    return rcp_fast(1.0f + exp2_fast(z * (-2.30220819f - 0.10294324f * z * z)));   // -2 c log2(e), and 0.044715 times it
+}
+__device__ __forceinline__ float sigmoid(float z) { return rcp_fast(1.0f + exp2_fast(z * -1.44269504f)); }
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if constexpr (ACT == ABT_ACT_RELU) return z < 0.0f ? 0.0f : z;                 // (NaN stays)
+    if constexpr (ACT == ABT_ACT_GELU) {
+        float density;
+        const float tail = normal_tail(z, density);
+        return z * (z > 0.0f ? 1.0f - tail : tail);
+    }
+    if constexpr (ACT == ABT_ACT_GELU_TANH) return z * tanh_gate(z);
+    if constexpr (ACT == ABT_ACT_SILU) return z * sigmoid(z);
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+    if constexpr (ACT == ABT_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+    if constexpr (ACT == ABT_ACT_GELU) {
+        float density;
+        const float tail = normal_tail(z, density);
+        return (z > 0.0f ? 1.0f - tail : tail) + z * density * 0.39894228f;
+    }
+    if constexpr (ACT == ABT_ACT_GELU_TANH) {
+        z = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;                           // the gate is 0 or 1 long before; z^2 stays finite
+        const float s = tanh_gate(z);
+        return s + z * s * (1.0f - s) * (1.59576912f + 0.21406445f * z * z);      // 2 c, and 3 * 0.044715 times it
+    }
+    if constexpr (ACT == ABT_ACT_SILU) {
+        const float s = sigmoid(z);
+        return s + z * s * (1.0f - s);
+    }
+    return 1.0f;
+}
+
+// f(std::integral_constant<int, ACT>) for the activation of a launch, which is the same for all its threads: one branch around what f does
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F&& f) {
+    switch (act) {
+        case ABT_ACT_RELU: f(std::integral_constant<int, ABT_ACT_RELU>{}); break;
+        case ABT_ACT_GELU: f(std::integral_constant<int, ABT_ACT_GELU>{}); break;
+        case ABT_ACT_GELU_TANH: f(std::integral_constant<int, ABT_ACT_GELU_TANH>{}); break;
+        case ABT_ACT_SILU: f(std::integral_constant<int, ABT_ACT_SILU>{}); break;
+        default: f(std::integral_constant<int, ABT_ACT_NONE>{});
+    }
+}
+
+}  // namespace abt

@@ -1,0 +1,52 @@
+// The dense layer with bias, activation, dropout and residual (dense_tile.hip, dense_few.hip, dense_grad.hip): what dense_api.hip calls.
+#pragma once
+
+#include "dropout.h"
+
+namespace abt {
+
+// Y = residual + drop(act(Z)), Z = alpha X W^T + bias
+struct DenseProduct {
+    const uint16_t* X; const uint16_t* W;  // [M, K], [Q, K]; K a multiple of 8
+    uint16_t* Y;                           // [M, Q]; Q a multiple of 8
+    const float* bias;                     // [Q], NULL: none
+    const uint16_t* residual;              // [M, Q], NULL: none
+    uint16_t* Z;                           // [M, Q], NULL: not kept
+    int64_t M;
+    int Q, K, act;
+    float alpha;
+    Drop drop;
+};
+hipError_t launch_dense_tiles(const DenseProduct& p, hipStream_t s);
+bool dense_few_wanted(int64_t M, int Q, int K);
+hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);
+inline hipError_t launch_dense(const DenseProduct& p, hipStream_t s) { return dense_few_wanted(p.M, p.Q, p.K) ? launch_dense_few(p, s) : launch_dense_tiles(p, s); }
+
+// What the gradients are made of: dZ = slope(Z) drop(dY) [M, m].  With a smooth activation it is kept as two bf16 values whose sum has 16 bits or more;
+// otherwise one is exact (dropout's factor is left to the products).  Beside it W^T, and sums of dZ over pieces of the rows.
+struct DenseSlope {
+    const uint16_t* dY; const uint16_t* Z; // Z NULL without an activation
+    uint16_t* high; uint16_t* low;         // high NULL: dY itself is dZ; low NULL: one value
+    float* sums;                           // [pieces, m] of dZ, without the factor where that is left out; NULL: not wanted
+    const uint16_t* W; uint16_t* Wt;       // [m, n] -> [n, m]; NULL: not wanted
+    int64_t M;
+    int m, n, act, rows;                   // rows of a piece
+    int scaled;                            // with dropout's factor
+    Drop drop;
+};
+int dense_piece_rows(int64_t M, int m);
+hipError_t launch_dense_slope(const DenseSlope& p, hipStream_t s);
+
+// dW [m, n] (+)= alpha (high + low)^T X, and dbias [m] (+)= alpha times the sum of `sums`; either may be NULL
+struct DenseGrads {
+    const uint16_t* high; const uint16_t* low; const uint16_t* X;
+    float* dW; float* partials;
+    const float* sums; float* dbias;
+    int64_t M;
+    int m, n, pieces, accumulate;
+    float alpha;
+};
+size_t dense_grad_partial_bytes(int64_t M, int m, int n);
+hipError_t launch_dense_grads(const DenseGrads& p, hipStream_t s);
+
+}  // namespace abt

@@ -1,0 +1,80 @@
+// Dropout by itself: Y = residual + drop(X), eight elements per thread and block of random bits.
+// Bound by memory; the generator (some 270 cycles of a SIMD for 512 elements) runs beside it.
+#include "dropout.h"
+
+namespace abt {
+namespace {
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* p, int64_t i, float (&v)[8]) {
+    if (BF16) {
+        const u32x4 w = gload(reinterpret_cast<const u32x4*>((const uint16_t*)p + i));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = __builtin_bit_cast(float, w[k] << 16);
+            v[2 * k + 1] = __builtin_bit_cast(float, w[k] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 w = gload(reinterpret_cast<const f32x4*>((const float*)p + i + 4 * h));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[4 * h + k] = w[k];
+        }
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ float load1(const void* p, int64_t i) {
+    return BF16 ? __builtin_bit_cast(float, (uint32_t)gload((const uint16_t*)p + i) << 16) : gload((const float*)p + i);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void dropout_kernel(const void* X, const void* R, void* Y, int64_t count, const Drop d) {
+    const int64_t step = (int64_t)gridDim.x * 256;
+    const DropKey key = d.state ? drop_key(d) : DropKey{0, 0, 0, 0};
+    for (int64_t b = (int64_t)blockIdx.x * 256 + threadIdx.x; 8 * b < count; b += step) {
+        const int64_t i = 8 * b;
+        float x[8], r[8];
+        if (i + 8 <= count) {
+            load8<BF16>(X, i, x);
+            if (R) load8<BF16>(R, i, r);
+            if (d.state) drop8(d, key, (uint64_t)b, x);
+            if (R)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] += r[k];
+            if (BF16) {
+                const u32x4 w = {pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7])};
+                gstore(reinterpret_cast<u32x4*>((uint16_t*)Y + i), w);
+            } else {
+                gstore(reinterpret_cast<f32x4*>((float*)Y + i), f32x4{x[0], x[1], x[2], x[3]});
+                gstore(reinterpret_cast<f32x4*>((float*)Y + i + 4), f32x4{x[4], x[5], x[6], x[7]});
+            }
+            continue;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                     // the last elements
+            x[k] = i + k < count ? load1<BF16>(X, i + k) : 0.0f;
+            r[k] = R && i + k < count ? load1<BF16>(R, i + k) : 0.0f;
+        }
+        if (d.state) drop8(d, key, (uint64_t)b, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k < count) {
+                const float v = R ? x[k] + r[k] : x[k];
+                if (BF16) gstore((uint16_t*)Y + i + k, (uint16_t)pack2_bf16(v, 0.0f));
+                else gstore((float*)Y + i + k, v);
+            }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const void* X, const void* residual, void* Y, int64_t count, const Drop& d, bool bf16, hipStream_t s) {
+    const int64_t blocks = ceil_div(count, 2048);
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
+    if (bf16) hipLaunchKernelGGL((dropout_kernel<true>), grid, dim3(256), 0, s, X, residual, Y, count, d);
+    else hipLaunchKernelGGL((dropout_kernel<false>), grid, dim3(256), 0, s, X, residual, Y, count, d);
+    return hipGetLastError();
+}
+
+}  // namespace abt
