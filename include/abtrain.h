@@ -18,7 +18,7 @@
  *     caller; the library never allocates, frees or retains caller memory.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  lr_linear_fwd,
  *     lr_linear_bwd, lr_linear_bwd_static, lr_linear_fwd_grouped, lr_linear_bwd_grouped, lr_conv_fwd, lr_conv_bwd,
- *     ab_adamw_step, ab_reconstruct, lr_adapters_*, lr_rms_norm_*, lr_dense_*, lr_dropout, ab_grad_norm, ab_clip_grads and ab_adamw_step_clipped
+ *     ab_adamw_step, ab_reconstruct, lr_adapters_*, lr_rms_norm_*, lr_dense_*, lr_dropout, lr_group_norm_*, ab_grad_norm, ab_clip_grads and ab_adamw_step_clipped
  *     enqueue work on it and return without synchronising the host.  Calls that DO block the host:
  *       ab_merge, ab_merge_batched, ab_factorize, ab_factorize_batched: once after uploading
  *         their layer tables (tables of up to 7680 bytes, which one or two layers may have, travel in
@@ -522,6 +522,26 @@ size_t lr_dense_bwd_workspace_bytes(int64_t M, int64_t m, int64_t n);
  * is the same call: dX = lr_dropout(dY) without a residual, whose gradient is dY.  Y may be X or the residual itself.  count from 0 to 2^45.
  * Errors: ABT_EINVAL (no state, p outside [0, 1]), ABT_EDTYPE, ABT_ESHAPE, ABT_EALIGN, ABT_EHIP. */
 int lr_dropout(const void* X, const void* residual, void* Y, int64_t count, const abt_dropout* dropout, int dt, void* stream);
+
+/* -------------------------------------------------------------------------------------
+ * Group norm with an activation over channels-last images, the norm behind lr_conv_fwd that does not look at other images (independent groups train on
+ * small batches of their own):
+ *     Y = act(gain (X - mean) rstd + shift),   rstd = 1 / sqrt(var + eps),   mean and var over the pixels and the C / groups channels of a group of one image
+ * X, Y [N, pixels, C] of type dt, gain, shift [C], mean, rstd [N, groups] fp32 (outputs; lr_group_norm_bwd reads them).  act as for lr_dense_fwd.
+ * lr_group_norm_bwd: dX of type dt, dgain and dshift [C] fp32 (accumulate != 0 adds into these two); any may be NULL.  Fixed summation order.
+ * Statistics in fp32, the squares around the mean.  C a multiple of 8 and of groups, at most ABT_GROUP_NORM_MAX_CHANNELS; groups from 1 to C; N and pixels from 1 to 2^28,
+ * N pixels at most 2^36.  eps >= 0 and finite; with eps = 0 a group whose values are all alike is 0 / 0: NaN.  A value that is not finite reaches its
+ * own image and group, and dgain and dshift of its channels.
+ * Y may be X; dX may be dY or X.  Workspace: lr_group_norm_workspace_bytes.  Nothing blocks the host; can be captured.
+ * Errors: ABT_EINVAL, ABT_EDTYPE, ABT_ESHAPE, ABT_EALIGN, ABT_EWORKSPACE, ABT_EHIP.
+ * ------------------------------------------------------------------------------------- */
+#define ABT_GROUP_NORM_MAX_CHANNELS 65536
+int lr_group_norm_fwd(const void* X, const float* gain, const float* shift, double eps, void* Y, float* mean, float* rstd,
+                      int64_t N, int64_t pixels, int64_t C, int64_t groups, int act, int dt, void* workspace, size_t workspace_bytes, void* stream);
+int lr_group_norm_bwd(const void* dY, const void* X, const float* gain, const float* shift, const float* mean, const float* rstd,
+                      void* dX, float* dgain, float* dshift, int64_t N, int64_t pixels, int64_t C, int64_t groups, int act, int dt, int accumulate,
+                      void* workspace, size_t workspace_bytes, void* stream);
+size_t lr_group_norm_workspace_bytes(int64_t N, int64_t pixels, int64_t C, int64_t groups, int dt, int backward);   /* 0 for shapes that are refused */
 
 /* Work-group height of the bf16 chain kernel (T = X B^T, Y = T A^T and the dT / dX half of the
  * backward): 0 = chosen from the batch size (default), 64 or 128 = forced where the rank allows it.

@@ -33,6 +33,7 @@ EXPORTS = (
     "lr_rms_norm_fwd", "lr_rms_norm_bwd", "lr_rms_norm_bwd_workspace_bytes",
     "ab_grad_norm", "ab_clip_grads", "ab_adamw_step_clipped", "ab_grad_norm_workspace_bytes",
     "lr_dense_fwd", "lr_dense_bwd", "lr_dense_bwd_workspace_bytes", "lr_dropout",
+    "lr_group_norm_fwd", "lr_group_norm_bwd", "lr_group_norm_workspace_bytes",
 )
 
 
@@ -212,6 +213,12 @@ def load():
     lib.lr_dense_bwd_workspace_bytes.argtypes = [i64, i64, i64]
     lib.lr_dropout.restype = ci
     lib.lr_dropout.argtypes = [vp, vp, vp, i64, pdr, ci, vp]
+    lib.lr_group_norm_fwd.restype = ci
+    lib.lr_group_norm_fwd.argtypes = [vp, vp, vp, cd, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, sz, vp]
+    lib.lr_group_norm_bwd.restype = ci
+    lib.lr_group_norm_bwd.argtypes = [vp] * 9 + [i64, i64, i64, i64, ci, ci, ci, vp, sz, vp]
+    lib.lr_group_norm_workspace_bytes.restype = sz
+    lib.lr_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci]
     lib.ab_grad_norm.restype = ci
     lib.ab_grad_norm.argtypes = [pgt, ci, vp, vp, sz, vp]
     lib.ab_clip_grads.restype = ci
@@ -1151,6 +1158,81 @@ def lr_dropout(X, dropout, residual=None, Y=None):
     _on_this_device(X, (residual, Y))
     _check(load().lr_dropout(X.data_ptr(), _ptr(residual), Y.data_ptr(), X.numel(), _dropout(dropout, X.device), dt, _stream()), "lr_dropout")
     return Y
+
+
+def _images(X, name="X"):
+    """(N, pixels, C) of a channels-last tensor [N, ..., C]."""
+    _dev_tensor(X, name)
+    if X.dim() < 2:
+        raise AbtError(f"{name} must be [N, ..., C], channels last")
+    N, C = X.shape[0], X.shape[-1]
+    return N, X.numel() // max(N * C, 1), C
+
+
+def lr_group_norm_fwd(X, gain, shift, groups: int, eps: float = 1e-5, act: str = "none", Y=None, mean=None, rstd=None, workspace=None):
+    """Y = act(gain (X - mean) / sqrt(var + eps) + shift) for channels-last images X [N, ..., C] (bf16 or fp32, GPU), mean and var over the pixels and the
+    C / groups channels of a group of one image; gain, shift [C] fp32; act as for lr_dense_fwd.  Returns (Y, mean, rstd), the last two [N, groups] fp32.
+    Y may be X."""
+    torch = _torch()
+    lib = load()
+    f32 = torch.float32
+    N, pixels, C = _images(X)
+    dt = _dt(X)
+    _plain_matrix(gain, "gain", (C,), f32), _plain_matrix(shift, "shift", (C,), f32)
+    need = lib.lr_group_norm_workspace_bytes(N, pixels, C, int(groups), dt, 0)
+    if need == 0:
+        raise AbtError(f"lr_group_norm_fwd: unsupported shape {tuple(X.shape)} with {groups} groups (C a multiple of 8 and of groups)")
+    out = []
+    for t, nm, shape, dtype in ((Y, "Y", X.shape, X.dtype), (mean, "mean", (N, int(groups)), f32), (rstd, "rstd", (N, int(groups)), f32)):
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=X.device)
+        else:
+            _plain_matrix(t, nm, shape, dtype)
+        out.append(t)
+    Y, mean, rstd = out
+    ws = _workspace(need, X.device, workspace)
+    _on_this_device(X, (gain, shift, Y, mean, rstd, ws))
+    _check(lib.lr_group_norm_fwd(X.data_ptr(), gain.data_ptr(), shift.data_ptr(), float(eps), Y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), N, pixels, C, int(groups),
+                                 _activation(act), dt, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "lr_group_norm_fwd")
+    return Y, mean, rstd
+
+
+def lr_group_norm_bwd(dY, X, gain, shift, mean, rstd, act: str = "none", need_dX: bool = True, need_dgain: bool = True, need_dshift: bool = True,
+                      dX=None, dgain=None, dshift=None, accumulate: bool = False, workspace=None):
+    """Gradients of lr_group_norm_fwd from dY and its X, gain, shift, act and returned mean and rstd: dX like X, dgain and dshift [C] fp32 (added into what is there
+    with accumulate).  Returns (dX, dgain, dshift); skipped ones are None.  dX may be dY or X."""
+    torch = _torch()
+    lib = load()
+    f32 = torch.float32
+    N, pixels, C = _images(X)
+    dt = _dt(X)
+    if mean.dim() != 2:
+        raise AbtError("mean must be [N, groups]")
+    groups = mean.shape[1]
+    _plain_matrix(dY, "dY", X.shape, X.dtype)
+    for t, nm, shape in ((gain, "gain", (C,)), (shift, "shift", (C,)), (mean, "mean", (N, groups)), (rstd, "rstd", (N, groups))):
+        _plain_matrix(t, nm, shape, f32)
+    need = lib.lr_group_norm_workspace_bytes(N, pixels, C, groups, dt, 1)
+    if need == 0:
+        raise AbtError(f"lr_group_norm_bwd: unsupported shape {tuple(X.shape)} with {groups} groups (C a multiple of 8 and of groups)")
+    out = []
+    for t, nm, wanted, shape, dtype in ((dX, "dX", need_dX, X.shape, X.dtype), (dgain, "dgain", need_dgain, (C,), f32), (dshift, "dshift", need_dshift, (C,), f32)):
+        if not wanted:
+            t = None
+        elif t is not None:
+            _plain_matrix(t, nm, shape, dtype)
+        elif accumulate and nm != "dX":
+            raise AbtError(f"accumulate needs existing {nm}")
+        else:
+            t = torch.empty(shape, dtype=dtype, device=X.device)
+        out.append(t)
+    dX, dgain, dshift = out
+    ws = _workspace(need, X.device, workspace)
+    _on_this_device(X, (dY, gain, shift, mean, rstd, dX, dgain, dshift, ws))
+    _check(lib.lr_group_norm_bwd(dY.data_ptr(), X.data_ptr(), gain.data_ptr(), shift.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(dX), _ptr(dgain), _ptr(dshift),
+                                 N, pixels, C, groups, _activation(act), dt, int(bool(accumulate)), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()),
+           "lr_group_norm_bwd")
+    return dX, dgain, dshift
 
 
 def ab_reconstruct(A, B, W=None):

@@ -1,28 +1,11 @@
 // Dropout by itself: Y = residual + drop(X), eight elements per thread and block of random bits.
 // Bound by memory; the generator (some 270 cycles of a SIMD for 512 elements) runs beside it.
 #include "dropout.h"
+#include "vec8.h"
 
 namespace abt {
 namespace {
 
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* p, int64_t i, float (&v)[8]) {
-    if (BF16) {
-        const u32x4 w = gload(reinterpret_cast<const u32x4*>((const uint16_t*)p + i));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[2 * k] = __builtin_bit_cast(float, w[k] << 16);
-            v[2 * k + 1] = __builtin_bit_cast(float, w[k] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 w = gload(reinterpret_cast<const f32x4*>((const float*)p + i + 4 * h));
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[4 * h + k] = w[k];
-        }
-    }
-}
 template <bool BF16>
 __device__ __forceinline__ float load1(const void* p, int64_t i) {
     return BF16 ? __builtin_bit_cast(float, (uint32_t)gload((const uint16_t*)p + i) << 16) : gload((const float*)p + i);
@@ -42,13 +25,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const void* X, const void*
             if (R)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) x[k] += r[k];
-            if (BF16) {
-                const u32x4 w = {pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7])};
-                gstore(reinterpret_cast<u32x4*>((uint16_t*)Y + i), w);
-            } else {
-                gstore(reinterpret_cast<f32x4*>((float*)Y + i), f32x4{x[0], x[1], x[2], x[3]});
-                gstore(reinterpret_cast<f32x4*>((float*)Y + i + 4), f32x4{x[4], x[5], x[6], x[7]});
-            }
+            store8<BF16>(Y, i, x);
             continue;
         }
 #pragma unroll

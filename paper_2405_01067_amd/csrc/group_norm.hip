@@ -1,0 +1,564 @@
+// Group norm with an activation over channels-last images:
+//     Y = act(gain (X - mean) rstd + shift),   mean and 1 / rstd^2 - eps over the pixels and the channels of a group of one image
+//     dpre = dY act'(..), u = dpre gain, x^ = (X - mean) rstd:   dX = rstd (u - mean(u) - x^ mean(u x^)),   dgain = sum dpre x^,   dshift = sum dpre
+// Where all pixels of an image fit a work-group's registers over a slab of channels that holds whole groups, a work-group reads them once and does everything (`whole` kernels);
+// otherwise pieces of the pixels leave sums per channel in a first launch and are normalised in a second, which reads again.
+// Threads: eight channels each, TC of them (a power of two) across the slab, the others down the pixels.  Bound by memory.
+#include <climits>
+
+#include "activation.h"
+#include "group_norm.h"
+#include "vec8.h"
+
+namespace abt {
+namespace {
+
+constexpr int kMaxSlab = 512;                             // channels: 64 threads across
+
+// Slabs of the channels, of `width` each (the last may have fewer) and TC = 2^shift threads across; pieces of the pixels
+struct Split { int width, slabs, shift, pieces, rows; };
+
+__device__ __forceinline__ float lanes_sum(float v, int from, int to) {      // over lanes whose numbers differ in the bits from .. to / 2
+    for (int d = from; d < to; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// The sums of each channel of the slab over all threads, in chan[q pitch ..]: lanes with the same channels first, then the waves.  `waves` holds K pitch values
+// for each wave.
+template <int THREADS, int K>
+__device__ __forceinline__ void channel_sums(float (&v)[K][8], int shift, int width, int pitch, float* waves, float* chan) {
+    constexpr int NW = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tc = lane & ((1 << shift) - 1);
+#pragma unroll
+    for (int q = 0; q < K; ++q) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[q][k] = lanes_sum(v[q][k], 1 << shift, 64);
+        if (lane == tc && 8 * tc < width)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) waves[(q * NW + wave) * pitch + 8 * tc + k] = v[q][k];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < width; c += THREADS)
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+            float s = waves[q * NW * pitch + c];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) s += waves[(q * NW + w) * pitch + c];
+            chan[q * pitch + c] = s;
+        }
+    __syncthreads();
+}
+
+// f(group, lane of `lanes`, lanes): the work-group's threads in teams of a power of two of up to 64, a team for a group
+template <int THREADS, class F>
+__device__ __forceinline__ void by_group(int groups, int entries, F&& f) {
+    int lanes = 1;
+    while (lanes < entries && lanes < 64) lanes <<= 1;
+    for (int g = threadIdx.x / lanes; g < groups; g += THREADS / lanes) f(g, (int)threadIdx.x & (lanes - 1), lanes);
+}
+
+// ------------------------------------------------------------------------------------------ everything at once
+// Pixel r of NV: row + r step, where row = thread / TC
+template <bool BF16, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g, const Split sp) {
+    extern __shared__ float lds[];
+    const int pitch = sp.width;
+    float *const waves = lds, *const chan = waves + THREADS / 64 * pitch, *const stat = chan + pitch;
+    const int slab = blockIdx.x % sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
+    const int64_t image = blockIdx.x / sp.slabs;
+    const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
+    const bool there = 8 * tc < width;
+    const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
+    const int cpg = g.C / g.groups, groups = width / cpg;
+    const float n = (float)g.pixels * (float)cpg;
+    Raw8<BF16> x[NV];
+#pragma unroll
+    for (int r = 0; r < NV; ++r)
+        if (there && row + r * step < g.pixels) x[r] = raw8<BF16>(g.X, base + (int64_t)(row + r * step) * g.C);
+    float gain[8], shift[8];
+    if (there) load8<false>(g.gain, c0 + 8 * tc, gain), load8<false>(g.shift, c0 + 8 * tc, shift);
+    float sum[1][8], mean[8], rstd[8];
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {                // the mean, then the squares around it
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[0][k] = 0.0f;
+#pragma unroll
+        for (int r = 0; r < NV; ++r)
+            if (there && row + r * step < g.pixels) {
+                float v[8];
+                values<BF16>(x[r], v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float d = pass ? v[k] - mean[k] : v[k];
+                    sum[0][k] += pass ? d * d : d;
+                }
+            }
+        channel_sums<THREADS, 1>(sum, sp.shift, width, pitch, waves, chan);
+        by_group<THREADS>(groups, cpg, [&](int q, int l, int lanes) {
+            float s = 0.0f;
+            if (q < groups)
+                for (int c = l; c < cpg; c += lanes) s += chan[q * cpg + c];
+            s = lanes_sum(s, 1, lanes);
+            if (l) return;
+            s /= n;
+            if (pass) s = 1.0f / __builtin_sqrtf(s + g.eps);
+            stat[pass * pitch + q] = s;
+            gstore((pass ? g.rstd : g.mean) + image * g.groups + c0 / cpg + q, s);
+        });
+        __syncthreads();
+        if (there)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) (pass ? rstd : mean)[k] = stat[pass * pitch + (8 * tc + k) / cpg];
+    }
+    if (!there) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gain[k] *= rstd[k];
+    with_activation(g.act, [&](auto act) {
+#pragma unroll
+        for (int r = 0; r < NV; ++r)
+            if (row + r * step < g.pixels) {
+                float v[8];
+                values<BF16>(x[r], v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>((v[k] - mean[k]) * gain[k] + shift[k]);
+                store8<BF16>(g.Y, base + (int64_t)(row + r * step) * g.C, v);
+            }
+    });
+}
+
+// sums [2, N, C] of dpre and of dpre x^
+template <bool BF16, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g, const Split sp) {
+    extern __shared__ float lds[];
+    const int pitch = sp.width;
+    float *const waves = lds, *const chan = waves + 2 * (THREADS / 64) * pitch, *const stat = chan + 2 * pitch;
+    const int slab = blockIdx.x % sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
+    const int64_t image = blockIdx.x / sp.slabs;
+    const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
+    const bool there = 8 * tc < width;
+    const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
+    const int cpg = g.C / g.groups, groups = width / cpg;
+    const float n = (float)g.pixels * (float)cpg;
+    Raw8<BF16> x[NV], dy[NV];
+#pragma unroll
+    for (int r = 0; r < NV; ++r)
+        if (there && row + r * step < g.pixels) {
+            x[r] = raw8<BF16>(g.X, base + (int64_t)(row + r * step) * g.C);
+            dy[r] = raw8<BF16>(g.dY, base + (int64_t)(row + r * step) * g.C);
+        }
+    float gain[8], shift[8], mean[8], rstd[8];
+    if (there) {
+        load8<false>(g.gain, c0 + 8 * tc, gain), load8<false>(g.shift, c0 + 8 * tc, shift);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t q = image * g.groups + (c0 + 8 * tc + k) / cpg;
+            mean[k] = gload(g.mean + q), rstd[k] = gload(g.rstd + q);
+        }
+    }
+    float sum[2][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[0][k] = sum[1][k] = 0.0f;
+    with_activation(g.act, [&](auto act) {
+#pragma unroll
+        for (int r = 0; r < NV; ++r)
+            if (there && row + r * step < g.pixels) {
+                float v[8], d[8];
+                values<BF16>(x[r], v), values<BF16>(dy[r], d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = (v[k] - mean[k]) * rstd[k];
+                    if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
+                    sum[0][k] += d[k];
+                    sum[1][k] += d[k] * v[k];
+                }
+            }
+    });
+    channel_sums<THREADS, 2>(sum, sp.shift, width, pitch, waves, chan);
+    if (g.sums)
+        for (int c = threadIdx.x; c < width; c += THREADS)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) gstore(g.sums + (q * g.N + image) * g.C + c0 + c, chan[q * pitch + c]);
+    if (!g.Y) return;
+    by_group<THREADS>(groups, cpg, [&](int q, int l, int lanes) {
+        float s = 0.0f, t = 0.0f;
+        for (int c = l; c < cpg; c += lanes) {
+                const float w = gload(g.gain + c0 + q * cpg + c);
+                s += chan[q * cpg + c] * w;
+                t += chan[pitch + q * cpg + c] * w;
+            }
+        s = lanes_sum(s, 1, lanes), t = lanes_sum(t, 1, lanes);
+        if (l == 0) stat[q] = s / n, stat[pitch + q] = t / n;
+    });
+    __syncthreads();
+    if (!there) return;
+    float first[8], second[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) first[k] = stat[(8 * tc + k) / cpg], second[k] = stat[pitch + (8 * tc + k) / cpg];
+    with_activation(g.act, [&](auto act) {
+#pragma unroll
+        for (int r = 0; r < NV; ++r)
+            if (row + r * step < g.pixels) {
+                float v[8], d[8];
+                values<BF16>(x[r], v), values<BF16>(dy[r], d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = (v[k] - mean[k]) * rstd[k];
+                    if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
+                    v[k] = rstd[k] * (d[k] * gain[k] - first[k] - v[k] * second[k]);
+                }
+                store8<BF16>(g.Y, base + (int64_t)(row + r * step) * g.C, v);
+            }
+    });
+}
+
+// ------------------------------------------------------------------------------------------ in pieces
+struct Piece { int c0, width, piece, tc, first, last, step; int64_t image, base; bool there; };
+__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, int64_t block) {
+    Piece p;
+    const int slab = (int)(block % sp.slabs);
+    block /= sp.slabs;
+    p.piece = (int)(block % sp.pieces);
+    p.image = block / sp.pieces;
+    p.c0 = slab * sp.width;
+    p.width = g.C - p.c0 < sp.width ? g.C - p.c0 : sp.width;
+    p.tc = threadIdx.x & ((1 << sp.shift) - 1);
+    p.there = 8 * p.tc < p.width;
+    p.first = p.piece * sp.rows + (threadIdx.x >> sp.shift);
+    p.last = g.pixels - p.piece * sp.rows < sp.rows ? g.pixels : (p.piece + 1) * sp.rows;
+    p.step = 256 >> sp.shift;
+    p.base = p.image * g.pixels * g.C + p.c0 + 8 * p.tc;
+    return p;
+}
+
+// sums [2, N pieces, C]: the mean of a piece's pixels in a channel, and the squares around it
+template <bool BF16>
+__global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const Split sp) {
+    __shared__ float waves[4 * kMaxSlab], chan[kMaxSlab];
+    const Piece p = piece_of(g, sp, blockIdx.x);
+    const int n = p.last - p.piece * sp.rows;
+    float mean[8], square[8], sum[1][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mean[k] = square[k] = 0.0f;
+    float count = 0.0f;
+    if (p.there)
+        for (int r = p.first; r < p.last; r += p.step) {  // each thread's own mean and squares (Welford)
+            float v[8];
+            load8<BF16>(g.X, p.base + (int64_t)r * g.C, v);
+            count += 1.0f;
+            const float part = 1.0f / count;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float d = v[k] - mean[k];
+                mean[k] += d * part;
+                square[k] += d * (v[k] - mean[k]);
+            }
+        }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[0][k] = mean[k] * count;
+    channel_sums<256, 1>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    float all[8];
+    if (p.there)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) all[k] = chan[8 * p.tc + k] / (float)n;
+    const int64_t at = (p.image * sp.pieces + p.piece) * g.C + p.c0 + 8 * p.tc;
+    const bool writes = p.there && threadIdx.x < (1u << sp.shift);
+    if (writes) store8<false>(g.sums, at, all);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[0][k] = p.there ? square[k] + count * (mean[k] - all[k]) * (mean[k] - all[k]) : 0.0f;
+    __syncthreads();
+    channel_sums<256, 1>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    if (writes) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) all[k] = chan[8 * p.tc + k];
+        store8<false>(g.sums, g.N * sp.pieces * g.C + at, all);
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const Split sp) {
+    __shared__ float stat[2][kMaxSlab];
+    const Piece p = piece_of(g, sp, blockIdx.x);
+    const int cpg = g.C / g.groups, g0 = p.c0 / cpg, groups = (p.c0 + p.width - 1) / cpg - g0 + 1;
+    const float* const means = g.sums + p.image * sp.pieces * g.C;
+    const float* const squares = means + g.N * sp.pieces * g.C;
+    const int entries = cpg * sp.pieces;
+    by_group<256>(groups, entries, [&](int q, int l, int lanes) {
+        const int c = (g0 + q) * cpg;
+        float s = 0.0f, t = 0.0f;
+        const auto of = [&](int e, int& n) {              // an entry's place, and its pixels
+            const int piece = e / cpg;
+            n = g.pixels - piece * sp.rows < sp.rows ? g.pixels - piece * sp.rows : sp.rows;
+            return (int64_t)piece * g.C + c + e % cpg;
+        };
+        int n;
+        for (int e = l; e < entries; e += lanes) {
+                const int64_t at = of(e, n);
+                s += gload(means + at) * (float)n;
+            }
+        const float mean = lanes_sum(s, 1, lanes) / ((float)g.pixels * (float)cpg);
+        for (int e = l; e < entries; e += lanes) {
+                const int64_t at = of(e, n);
+                const float d = gload(means + at) - mean;
+                t += gload(squares + at) + (float)n * d * d;
+            }
+        t = lanes_sum(t, 1, lanes) / ((float)g.pixels * (float)cpg);
+        if (l) return;
+        const float rstd = 1.0f / __builtin_sqrtf(t + g.eps);
+        stat[0][q] = mean, stat[1][q] = rstd;
+        if (p.piece == 0 && c >= p.c0) gstore(g.mean + p.image * g.groups + g0 + q, mean), gstore(g.rstd + p.image * g.groups + g0 + q, rstd);
+    });
+    __syncthreads();
+    if (!p.there) return;
+    float gain[8], shift[8], mean[8];
+    load8<false>(g.gain, p.c0 + 8 * p.tc, gain), load8<false>(g.shift, p.c0 + 8 * p.tc, shift);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int q = (p.c0 + 8 * p.tc + k) / cpg - g0;
+        mean[k] = stat[0][q];
+        gain[k] *= stat[1][q];
+    }
+    with_activation(g.act, [&](auto act) {
+        for (int r = p.first; r < p.last; r += p.step) {
+            const int64_t at = p.base + (int64_t)r * g.C;
+            float v[8];
+            load8<BF16>(g.X, at, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>((v[k] - mean[k]) * gain[k] + shift[k]);
+            store8<BF16>(g.Y, at, v);
+        }
+    });
+}
+
+__device__ __forceinline__ void load_stats(const GroupNorm& g, const Piece& p, int cpg, float (&gain)[8], float (&shift)[8], float (&mean)[8], float (&rstd)[8]) {
+    load8<false>(g.gain, p.c0 + 8 * p.tc, gain), load8<false>(g.shift, p.c0 + 8 * p.tc, shift);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t q = p.image * g.groups + (p.c0 + 8 * p.tc + k) / cpg;
+        mean[k] = gload(g.mean + q), rstd[k] = gload(g.rstd + q);
+    }
+}
+
+// sums [2, N pieces, C] of dpre and of dpre x^
+template <bool BF16>
+__global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, const Split sp) {
+    __shared__ float waves[8 * kMaxSlab], chan[2 * kMaxSlab];
+    const Piece p = piece_of(g, sp, blockIdx.x);
+    const int cpg = g.C / g.groups;
+    float sum[2][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[0][k] = sum[1][k] = 0.0f;
+    if (p.there) {
+        float gain[8], shift[8], mean[8], rstd[8];
+        load_stats(g, p, cpg, gain, shift, mean, rstd);
+        with_activation(g.act, [&](auto act) {
+            for (int r = p.first; r < p.last; r += p.step) {
+                float v[8], d[8];
+                load8<BF16>(g.X, p.base + (int64_t)r * g.C, v), load8<BF16>(g.dY, p.base + (int64_t)r * g.C, d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = (v[k] - mean[k]) * rstd[k];
+                    if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
+                    sum[0][k] += d[k];
+                    sum[1][k] += d[k] * v[k];
+                }
+            }
+        });
+    }
+    channel_sums<256, 2>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    for (int c = threadIdx.x; c < p.width; c += 256)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) gstore(g.sums + ((q * g.N + p.image) * sp.pieces + p.piece) * g.C + p.c0 + c, chan[q * kMaxSlab + c]);
+}
+
+// dshift, dgain of 32 channels from `rows` rows of sums of each
+__device__ __forceinline__ void channel_gradients(const GroupNorm& g, int64_t rows, int block, float (*lds)[32]) {
+    const int c = block * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        float s = 0.0f;
+        if (c < g.C) {
+            const float* const from = g.sums + q * rows * g.C + c;
+            int64_t r = part;
+            for (; r + 56 < rows; r += 64) {              // eight loads on their way at a time
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = gload(from + (r + 8 * k) * g.C);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += v[k];
+            }
+            for (; r < rows; r += 8) s += gload(from + r * g.C);
+        }
+        __syncthreads();
+        lds[part][threadIdx.x & 31] = s;
+        __syncthreads();
+        float* const out = q ? g.dgain : g.dshift;
+        if (part || c >= g.C || !out) continue;
+        for (int k = 1; k < 8; ++k) s += lds[k][threadIdx.x];
+        gstore(out + c, g.accumulate ? gload(out + c) + s : s);
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, const Split sp, int64_t blocks) {
+    __shared__ float stat[2][kMaxSlab];
+    if (blockIdx.x >= blocks) {
+        channel_gradients(g, g.N * sp.pieces, (int)(blockIdx.x - blocks), reinterpret_cast<float (*)[32]>(&stat[0][0]));
+        return;
+    }
+    const Piece p = piece_of(g, sp, blockIdx.x);
+    const int cpg = g.C / g.groups, g0 = p.c0 / cpg, groups = (p.c0 + p.width - 1) / cpg - g0 + 1;
+    const float* const first = g.sums + p.image * sp.pieces * g.C;
+    const float* const second = first + g.N * sp.pieces * g.C;
+    const int entries = cpg * sp.pieces;
+    const float n = (float)g.pixels * (float)cpg;
+    by_group<256>(groups, entries, [&](int q, int l, int lanes) {
+        const int c = (g0 + q) * cpg;
+        float s = 0.0f, t = 0.0f;
+        for (int e = l; e < entries; e += lanes) {
+                const int64_t at = (int64_t)(e / cpg) * g.C + c + e % cpg;
+                const float w = gload(g.gain + c + e % cpg);
+                s += gload(first + at) * w;
+                t += gload(second + at) * w;
+            }
+        s = lanes_sum(s, 1, lanes), t = lanes_sum(t, 1, lanes);
+        if (l == 0) stat[0][q] = s / n, stat[1][q] = t / n;
+    });
+    __syncthreads();
+    if (!p.there) return;
+    float gain[8], shift[8], mean[8], rstd[8], a[8], b[8];
+    load_stats(g, p, cpg, gain, shift, mean, rstd);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int q = (p.c0 + 8 * p.tc + k) / cpg - g0;
+        a[k] = stat[0][q], b[k] = stat[1][q];
+    }
+    with_activation(g.act, [&](auto act) {
+        for (int r = p.first; r < p.last; r += p.step) {
+            const int64_t at = p.base + (int64_t)r * g.C;
+            float v[8], d[8];
+            load8<BF16>(g.X, at, v), load8<BF16>(g.dY, at, d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = (v[k] - mean[k]) * rstd[k];
+                if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
+                v[k] = rstd[k] * (d[k] * gain[k] - a[k] - v[k] * b[k]);
+            }
+            store8<BF16>(g.Y, at, v);
+        }
+    });
+}
+
+__global__ __launch_bounds__(256) void gn_channels_kernel(const GroupNorm g, int64_t rows) {
+    __shared__ float lds[8][32];
+    channel_gradients(g, rows, blockIdx.x, lds);
+}
+
+// ------------------------------------------------------------------------------------------ which
+int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
+
+// How a call is split; threads, vectors: of the `whole` kernels, threads = 0 for the others
+struct Plan { Split sp; int threads, vectors; };
+Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
+    Plan p{};
+    const int cpg = C / groups, unit = cpg / gcd(cpg, 8) * 8, line = bf16 ? 64 : 32;       // whole groups and vectors; 128 bytes
+    if (unit <= kMaxSlab) {
+        int width = (line + unit - 1) / unit * unit;
+        if (width > kMaxSlab) width = unit;
+        if (width > C) width = C;
+        int shift = 0;
+        while ((8 << shift) < width) ++shift;
+        const int most = (bf16 ? 16 : 8) / (backward ? 2 : 1);                             // vectors in a thread's registers
+        for (int threads = 256; threads <= 1024; threads *= 2) {
+            const int vectors = (int)ceil_div(pixels, threads >> shift);
+            if (vectors > most && threads < 1024) continue;
+            if (vectors > most) break;
+            p.sp = Split{width, (int)ceil_div(C, width), shift, 1, pixels};
+            p.threads = threads;
+            p.vectors = vectors;
+            return p;
+        }
+    }
+    int shift = 0;
+    while ((8 << shift) < C && shift < 6) ++shift;
+    const int width = 8 << shift, slabs = (int)ceil_div(C, width), step = 256 >> shift;
+    // some 1024 work-groups, four pixels or more a thread
+    int64_t pieces = ceil_div(1024, N * slabs);
+    if (pieces > ceil_div(pixels, 4 * step)) pieces = ceil_div(pixels, 4 * step);
+    const int rows = (int)ceil_div(pixels, pieces);
+    p.sp = Split{width, slabs, shift, (int)ceil_div(pixels, rows), rows};
+    return p;
+}
+
+template <bool BF16, bool BWD, int THREADS, int NV>
+hipError_t launch_whole(const GroupNorm& g, const Split& sp, hipStream_t s) {
+    const int64_t blocks = g.N * sp.slabs;
+    if (blocks > INT_MAX) return hipErrorInvalidValue;
+    const unsigned lds = (unsigned)(((BWD ? 2 : 1) * (THREADS / 64 + 1) + 2) * sp.width * 4);      // 72 KB at most
+    if constexpr (BWD) hipLaunchKernelGGL((gn_whole_bwd_kernel<BF16, THREADS, NV>), dim3((unsigned)blocks), dim3(THREADS), lds, s, g, sp);
+    else hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV>), dim3((unsigned)blocks), dim3(THREADS), lds, s, g, sp);
+    return hipGetLastError();
+}
+template <bool BF16, bool BWD, int THREADS>
+hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
+    constexpr int most = (BF16 ? 16 : 8) / (BWD ? 2 : 1);
+    if (p.vectors <= 2) return launch_whole<BF16, BWD, THREADS, 2>(g, p.sp, s);
+    if (p.vectors <= 4) return launch_whole<BF16, BWD, THREADS, 4>(g, p.sp, s);
+    if constexpr (most >= 8) {
+        if (p.vectors <= 8) return launch_whole<BF16, BWD, THREADS, 8>(g, p.sp, s);
+        if constexpr (most >= 16) return launch_whole<BF16, BWD, THREADS, 16>(g, p.sp, s);
+    }
+    return hipErrorInvalidValue;
+}
+template <bool BF16, bool BWD>
+hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
+    return p.threads == 256 ? launch_whole<BF16, BWD, 256>(g, p, s) : p.threads == 512 ? launch_whole<BF16, BWD, 512>(g, p, s) : launch_whole<BF16, BWD, 1024>(g, p, s);
+}
+
+template <bool BF16>
+hipError_t fwd(const GroupNorm& g, hipStream_t s) {
+    const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, false);
+    if (p.threads) return launch_whole<BF16, false>(g, p, s);
+    const int64_t blocks = g.N * p.sp.slabs * p.sp.pieces;
+    if (blocks > INT_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gn_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, p.sp);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((gn_apply_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, p.sp);
+    return hipGetLastError();
+}
+template <bool BF16>
+hipError_t bwd(const GroupNorm& g, hipStream_t s) {
+    const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, true);
+    const bool channels = g.dgain || g.dshift;
+    const int64_t sums = channels ? ceil_div(g.C, 32) : 0;
+    hipError_t e;
+    if (p.threads) {
+        GroupNorm q = g;
+        if (!channels) q.sums = nullptr;
+        e = launch_whole<BF16, true>(q, p, s);
+        if (e != hipSuccess || !channels) return e;
+        hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)sums), dim3(256), 0, s, g, g.N);
+        return hipGetLastError();
+    }
+    const int64_t blocks = g.N * p.sp.slabs * p.sp.pieces;
+    if (blocks + sums > INT_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, p.sp);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t apply = g.Y ? blocks : 0;
+    if (apply + sums == 0) return hipSuccess;
+    hipLaunchKernelGGL((gn_bwd_apply_kernel<BF16>), dim3((unsigned)(apply + sums)), dim3(256), 0, s, g, p.sp, apply);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t group_norm_sum_bytes(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
+    const Plan p = plan_of(N, pixels, C, groups, bf16, backward);
+    if (p.threads && !backward) return 0;
+    return (size_t)N * (size_t)p.sp.pieces * (size_t)C * 8;
+}
+hipError_t launch_group_norm_fwd(const GroupNorm& p, bool bf16, hipStream_t s) { return bf16 ? fwd<true>(p, s) : fwd<false>(p, s); }
+hipError_t launch_group_norm_bwd(const GroupNorm& p, bool bf16, hipStream_t s) { return bf16 ? bwd<true>(p, s) : bwd<false>(p, s); }
+
+}  // namespace abt
