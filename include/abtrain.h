@@ -512,7 +512,8 @@ typedef struct {
 } abt_dropout;
 
 int lr_dense_fwd(const void* X, const void* W, const float* bias, const void* residual, void* Y, void* Z_save,
-                 int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, void* stream);
+                 int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, void* workspace, size_t workspace_bytes, void* stream);
+size_t lr_dense_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n);   /* 0 for shapes that are refused */
 int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, void* dX, float* dW, float* dbias,
                  int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, int accumulate,
                  void* workspace, size_t workspace_bytes, void* stream);

@@ -32,7 +32,7 @@ EXPORTS = (
     "lr_adapters_fwd", "lr_adapters_fwd_q8", "lr_adapters_fwd_workspace_bytes", "lr_adapters_bwd", "lr_adapters_bwd_workspace_bytes",
     "lr_rms_norm_fwd", "lr_rms_norm_bwd", "lr_rms_norm_bwd_workspace_bytes",
     "ab_grad_norm", "ab_clip_grads", "ab_adamw_step_clipped", "ab_grad_norm_workspace_bytes",
-    "lr_dense_fwd", "lr_dense_bwd", "lr_dense_bwd_workspace_bytes", "lr_dropout",
+    "lr_dense_fwd", "lr_dense_fwd_workspace_bytes", "lr_dense_bwd", "lr_dense_bwd_workspace_bytes", "lr_dropout",
     "lr_group_norm_fwd", "lr_group_norm_bwd", "lr_group_norm_workspace_bytes",
 )
 
@@ -206,7 +206,9 @@ def load():
     lib.lr_rms_norm_bwd_workspace_bytes.argtypes = [i64, i64, ci]
     pdr = ctypes.POINTER(DropoutArgs)
     lib.lr_dense_fwd.restype = ci
-    lib.lr_dense_fwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, pdr, ci, vp]
+    lib.lr_dense_fwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, pdr, ci, vp, sz, vp]
+    lib.lr_dense_fwd_workspace_bytes.restype = sz
+    lib.lr_dense_fwd_workspace_bytes.argtypes = [i64, i64, i64]
     lib.lr_dense_bwd.restype = ci
     lib.lr_dense_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, pdr, ci, ci, vp, sz, vp]
     lib.lr_dense_bwd_workspace_bytes.restype = sz
@@ -319,6 +321,16 @@ def adapter_call():
     """The native code of lr_adapters_fwd, lr_adapters_fwd_q8, lr_adapters_bwd, lr_rms_norm_fwd and lr_rms_norm_bwd, or None.  Needs no GPU."""
     return _native_calls("adapter_call", ("lr_adapters_fwd", "lr_adapters_fwd_q8", "lr_adapters_fwd_workspace_bytes", "lr_adapters_bwd", "lr_adapters_bwd_workspace_bytes",
                                           "lr_rms_norm_fwd", "lr_rms_norm_bwd", "lr_rms_norm_bwd_workspace_bytes"))
+
+
+@functools.lru_cache(maxsize=None)
+def dense_call():
+    """The native code of lr_dense_fwd, lr_dense_bwd, lr_dropout, lr_group_norm_fwd and lr_group_norm_bwd, or None.  Needs no GPU."""
+    module = _native_calls("dense_call", ("lr_dense_fwd", "lr_dense_fwd_workspace_bytes", "lr_dense_bwd", "lr_dense_bwd_workspace_bytes", "lr_dropout",
+                                          "lr_group_norm_fwd", "lr_group_norm_bwd", "lr_group_norm_workspace_bytes"))
+    if module is not None:
+        module.dropout_class(Dropout)
+    return module
 
 
 def _dt(t):
@@ -1048,8 +1060,13 @@ class Dropout:
             raise AbtError("state must be a contiguous GPU tensor of two int64: seed, offset")
         if not 0 <= int(site) < 1 << 63:
             raise AbtError("site must be from 0 to 2^63 - 1")
-        self.p, self.state, self.site = float(p), state, int(site)
-        self.args = DropoutArgs(state.data_ptr(), self.site, self.p)
+        self._state = state
+        self.args = DropoutArgs(state.data_ptr(), int(site), float(p))
+        self.address = ctypes.addressof(self.args)
+
+    p = property(lambda self: self.args.p)
+    state = property(lambda self: self._state)
+    site = property(lambda self: self.args.site)
 
 
 def _dropout(dropout, device):
@@ -1076,9 +1093,14 @@ def _on_this_device(first, others):
             raise AbtError(f"tensors must be on the current device (cuda:{index}), not on {t.device}")
 
 
-def lr_dense_fwd(X, W, bias=None, act: str = "none", dropout=None, residual=None, save_Z: bool = False, Y=None, Z=None):
+def lr_dense_fwd(X, W, bias=None, act: str = "none", dropout=None, residual=None, save_Z: bool = False, Y=None, Z=None, workspace=None):
     """Y = residual + drop(act(Z)), Z = X W^T + bias, for X [M, n], W [m, n], residual [M, m] (bf16, GPU) and bias [m] fp32; act is none, relu, gelu,
     gelu_tanh or silu, dropout a Dropout.  Returns (Y, Z) [M, m] bf16, Z for lr_dense_bwd (None without save_Z).  Y may be the residual."""
+    if Y is None and Z is None and workspace is None:
+        native = dense_call()
+        done = native.dense_fwd(X, W, bias, act, dropout, residual, save_Z) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     bf16 = torch.bfloat16
     if X.dim() != 2 or W.dim() != 2:
@@ -1100,9 +1122,11 @@ def lr_dense_fwd(X, W, bias=None, act: str = "none", dropout=None, residual=None
         Z = X.new_empty((M, m))
     else:
         _plain_matrix(Z, "Z", (M, m), bf16)
-    _on_this_device(X, (W, bias, residual, Y, Z))
-    _check(load().lr_dense_fwd(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(), _ptr(Z), M, m, n, _activation(act),
-                               _dropout(dropout, X.device), ABT_BF16, _stream()), "lr_dense_fwd")
+    lib = load()
+    ws = _workspace(lib.lr_dense_fwd_workspace_bytes(M, m, n), X.device, workspace)
+    _on_this_device(X, (W, bias, residual, Y, Z, ws))
+    _check(lib.lr_dense_fwd(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(), _ptr(Z), M, m, n, _activation(act),
+                            _dropout(dropout, X.device), ABT_BF16, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "lr_dense_fwd")
     return Y, Z
 
 
@@ -1110,6 +1134,11 @@ def lr_dense_bwd(dY, X, W, Z=None, act: str = "none", dropout=None, need_dX: boo
                  dX=None, dW=None, dbias=None, accumulate: bool = False, workspace=None):
     """Gradients of lr_dense_fwd from dY [M, m] and its X, W, Z (None without an activation), act and dropout: dX [M, n] bf16, dW [m, n] and dbias [m]
     fp32.  Returns (dX, dW, dbias); skipped ones are None.  The residual's gradient is dY."""
+    if dX is None and dW is None and dbias is None and not accumulate and workspace is None:
+        native = dense_call()
+        done = native.dense_bwd(dY, X, W, Z, act, dropout, need_dX, need_dW, need_dbias) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     bf16, f32 = torch.bfloat16, torch.float32
@@ -1145,6 +1174,11 @@ def lr_dense_bwd(dY, X, W, Z=None, act: str = "none", dropout=None, need_dX: boo
 def lr_dropout(X, dropout, residual=None, Y=None):
     """Y = residual + drop(X) for a contiguous X (bf16 or fp32, GPU) of any shape and a residual of the same; the gradient of X is lr_dropout(dY, dropout).
     Y may be X or the residual."""
+    if Y is None:
+        native = dense_call()
+        done = native.dropout(X, dropout, residual) if native is not None else None
+        if done is not None:
+            return done
     if not isinstance(dropout, Dropout):
         raise AbtError("dropout must be a Dropout")
     _dev_tensor(X, "X")
@@ -1173,6 +1207,11 @@ def lr_group_norm_fwd(X, gain, shift, groups: int, eps: float = 1e-5, act: str =
     """Y = act(gain (X - mean) / sqrt(var + eps) + shift) for channels-last images X [N, ..., C] (bf16 or fp32, GPU), mean and var over the pixels and the
     C / groups channels of a group of one image; gain, shift [C] fp32; act as for lr_dense_fwd.  Returns (Y, mean, rstd), the last two [N, groups] fp32.
     Y may be X."""
+    if Y is None and mean is None and rstd is None and workspace is None:
+        native = dense_call()
+        done = native.group_fwd(X, gain, shift, groups, eps, act) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     f32 = torch.float32
@@ -1201,6 +1240,11 @@ def lr_group_norm_bwd(dY, X, gain, shift, mean, rstd, act: str = "none", need_dX
                       dX=None, dgain=None, dshift=None, accumulate: bool = False, workspace=None):
     """Gradients of lr_group_norm_fwd from dY and its X, gain, shift, act and returned mean and rstd: dX like X, dgain and dshift [C] fp32 (added into what is there
     with accumulate).  Returns (dX, dgain, dshift); skipped ones are None.  dX may be dY or X."""
+    if dX is None and dgain is None and dshift is None and not accumulate and workspace is None:
+        native = dense_call()
+        done = native.group_bwd(dY, X, gain, shift, mean, rstd, act, need_dX, need_dgain, need_dshift) if native is not None else None
+        if done is not None:
+            return done
     torch = _torch()
     lib = load()
     f32 = torch.float32

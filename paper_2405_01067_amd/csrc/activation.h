@@ -15,7 +15,7 @@ __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcp
 __device__ __forceinline__ float normal_tail(float z, float& density) {
     const float t = rcp_fast(1.0f + 0.23164189f * __builtin_fabsf(z));             // p / sqrt(2)
     density = exp2_fast(z * z * -0.72134752f);                                     // log2(e) / 2
-    return ((((1.061405429f * t - 1.453152027f) * t + 1.421413741f) * t - 0.284496736f) * t + 0.254829592f) * t * density * 0.5f;
+    return ((((0.5307027145f * t - 0.7265760135f) * t + 0.7107068705f) * t - 0.142248368f) * t + 0.127414796f) * (t * density);            // a / 2
 }
 // 1 / (1 + exp(-2 c (z + 0.044715 z^3))), c = sqrt(2 / pi): the sigmoid by which gelu_tanh multiplies (the tanh form is the same number)
 __device__ __forceinline__ float tanh_gate(float z) {
@@ -29,7 +29,7 @@ __device__ __forceinline__ float activate(float z) {
     if constexpr (ACT == ABT_ACT_GELU) {
         float density;
         const float tail = normal_tail(z, density);
-        return z * (z > 0.0f ? 1.0f - tail : tail);
+        return __builtin_fmaxf(z, 0.0f) - __builtin_fabsf(z) * tail;               // (a NaN is in the tail too)
     }
     if constexpr (ACT == ABT_ACT_GELU_TANH) return z * tanh_gate(z);
     if constexpr (ACT == ABT_ACT_SILU) return z * sigmoid(z);

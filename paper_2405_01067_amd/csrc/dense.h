@@ -16,11 +16,12 @@ struct DenseProduct {
     int Q, K, act;
     float alpha;
     Drop drop;
+    float* parts;                          // dense_part_bytes(M, Q, K)
+    int piece;                             // set by the launchers: slabs of 64 columns of a piece of the contraction
 };
-hipError_t launch_dense_tiles(const DenseProduct& p, hipStream_t s);
-bool dense_few_wanted(int64_t M, int Q, int K);
-hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);
-inline hipError_t launch_dense(const DenseProduct& p, hipStream_t s) { return dense_few_wanted(p.M, p.Q, p.K) ? launch_dense_few(p, s) : launch_dense_tiles(p, s); }
+size_t dense_part_bytes(int64_t M, int Q, int K);
+hipError_t launch_dense(const DenseProduct& p, hipStream_t s);
+hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);        // M <= 64
 
 // What the gradients are made of: dZ = slope(Z) drop(dY) [M, m].  With a smooth activation it is kept as two bf16 values whose sum has 16 bits or more;
 // otherwise one is exact (dropout's factor is left to the products).  Beside it W^T, and sums of dZ over pieces of the rows.

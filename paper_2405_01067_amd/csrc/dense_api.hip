@@ -22,7 +22,7 @@ int check_dense(int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dro
     return sizes_fit(M, m, n) ? ABT_OK : ABT_ESHAPE;
 }
 
-struct Places { size_t Wt, high, low, sums, partials, bytes; };
+struct Places { size_t Wt, high, low, sums, parts, partials, bytes; };
 Places places(int64_t M, int64_t m, int64_t n) {
     Places p{};
     size_t at = 0;
@@ -34,6 +34,7 @@ Places places(int64_t M, int64_t m, int64_t n) {
     take(p.high, (size_t)(M * m * 2));
     take(p.low, (size_t)(M * m * 2));
     take(p.sums, (size_t)(ceil_div(M, dense_piece_rows(M, (int)m)) * m * 4));
+    take(p.parts, dense_part_bytes(M, (int)n, (int)m));
     take(p.partials, dense_grad_partial_bytes(M, (int)m, (int)n));
     p.bytes = at;
     return p;
@@ -43,14 +44,23 @@ Places places(int64_t M, int64_t m, int64_t n) {
 
 extern "C" {
 
+size_t lr_dense_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n) {
+    if (!sizes_fit(M, m, n)) return 0;
+    const size_t bytes = align_up(dense_part_bytes(M, (int)m, (int)n), 256);
+    return bytes < 256 ? 256 : bytes;
+}
+
 int lr_dense_fwd(const void* X, const void* W, const float* bias, const void* residual, void* Y, void* Z_save,
-                 int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, void* stream) {
+                 int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, void* workspace, size_t workspace_bytes, void* stream) {
     if (dt != ABT_BF16) return ABT_EDTYPE;
     if (!X || !W || !Y) return ABT_EINVAL;
     const int st = check_dense(M, m, n, act, dropout);
     if (st != ABT_OK) return st;
     if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(Z_save, 16)) return ABT_EALIGN;
-    const DenseProduct p{(const uint16_t*)X, (const uint16_t*)W, (uint16_t*)Y, bias, (const uint16_t*)residual, (uint16_t*)Z_save, M, (int)m, (int)n, act, 1.0f, drop_of(dropout)};
+    if (!workspace || workspace_bytes < lr_dense_fwd_workspace_bytes(M, m, n)) return ABT_EWORKSPACE;
+    if (!aligned(workspace, 256)) return ABT_EALIGN;
+    const DenseProduct p{(const uint16_t*)X, (const uint16_t*)W, (uint16_t*)Y, bias, (const uint16_t*)residual, (uint16_t*)Z_save, M, (int)m, (int)n, act, 1.0f, drop_of(dropout),
+                         (float*)workspace, 0};
     return launch_dense(p, (hipStream_t)stream) == hipSuccess ? ABT_OK : ABT_EHIP;
 }
 
@@ -84,7 +94,8 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
     const uint16_t* const high = z.high ? z.high : z.dY;
     const float alpha = smooth ? 1.0f : drop.scale;       // what dZ was left without
     if (dX) {
-        const DenseProduct p{high, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f}};
+        const DenseProduct p{high, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f},
+                             (float*)(ws + at.parts), 0};
         if (launch_dense(p, s) != hipSuccess) return ABT_EHIP;
     }
     const DenseGrads g{high, z.low, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, alpha};

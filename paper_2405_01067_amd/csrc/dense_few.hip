@@ -7,15 +7,16 @@
 namespace abt {
 namespace {
 
-constexpr int kFewWaves = 8;
-
-template <int RB, int CB>
-__global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(const DenseProduct g, int row_blocks) {
-    __shared__ f32x4 parts[kFewWaves][RB * CB][64];
+// D steps of a wave are on their way at a time.
+template <int RB, int CB, int NW, int D>
+__global__ __launch_bounds__(64 * NW) void dense_few_kernel(const DenseProduct g, int row_blocks) {
+    __shared__ f32x4 parts[NW][RB * CB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 15, lq = lane >> 4;
-    const int64_t row0 = (int64_t)(blockIdx.x % row_blocks) * (16 * RB);
-    const int col0 = (int)(blockIdx.x / row_blocks) * (16 * CB);
+    // the row blocks of the same columns follow each other on one XCD, whose L2 then has W once
+    const int per = (int)gridDim.x >> 3, rem = (int)gridDim.x & 7, xcd = blockIdx.x & 7, block = xcd * per + (xcd < rem ? xcd : rem) + (blockIdx.x >> 3);
+    const int64_t row0 = (int64_t)(block % row_blocks) * (16 * RB);
+    const int col0 = block / row_blocks * (16 * CB);
     const int rows = g.M - row0 < 16 * RB ? (int)(g.M - row0) : 16 * RB, cols = g.Q - col0 < 16 * CB ? g.Q - col0 : 16 * CB;
     const int bytes = g.K * 2, steps = (bytes + 127) / 128;
     const rsrc_t xres = make_rsrc((const char*)g.X + row0 * bytes, (int64_t)rows * bytes);
@@ -27,29 +28,33 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(const DensePr
         for (int b = 0; b < CB; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
     // a step: 64 columns, of which lane group lq has 16; the same on both sides
     struct Ops { u32x4 w[CB][2], x[RB][2]; };
+    // (work-groups begin at different steps: they read the same rows of X)
+    const int turn = (int)((unsigned)block * 5u % (unsigned)steps);
     auto read = [&](Ops& o, int s) {
-        const int k = s * 128 + lq * 32;
+        const int t = s + turn < steps ? s + turn : s < steps ? s + turn - steps : steps, k = t * 128 + lq * 32;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int at = k + 16 * h < bytes && s < steps ? li * bytes + k + 16 * h : kBufNowhere, step = at == kBufNowhere ? 0 : 16 * bytes;
+            const int at = k + 16 * h < bytes ? li * bytes + k + 16 * h : kBufNowhere, step = at == kBufNowhere ? 0 : 16 * bytes;
 #pragma unroll
             for (int b = 0; b < CB; ++b) o.w[b][h] = buf_load16(wres, at + b * step, 0);
 #pragma unroll
             for (int a = 0; a < RB; ++a) o.x[a][h] = buf_load16(xres, at + a * step, 0);
         }
     };
-    Ops now, next;
-    read(now, wave);
-    for (int s = wave; s < steps; s += kFewWaves) {
-        read(next, s + kFewWaves);
+    Ops ring[D];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int d = 0; d < D; ++d) read(ring[d], wave + d * NW);
+    for (int s = wave; s < steps; s += NW * D)
 #pragma unroll
-            for (int a = 0; a < RB; ++a)
+        for (int d = 0; d < D; ++d) {                     // (steps past the last one are zeros)
 #pragma unroll
-                for (int b = 0; b < CB; ++b) acc[a][b] = mfma16(now.w[b][h], now.x[a][h], acc[a][b]);
-        now = next;
-    }
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int a = 0; a < RB; ++a)
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) acc[a][b] = mfma16(ring[d].w[b][h], ring[d].x[a][h], acc[a][b]);
+            read(ring[d], s + (D + d) * NW);
+        }
     // lane: row li of a block of rows, columns 4 lq .. + 3 of a block of columns
 #pragma unroll
     for (int a = 0; a < RB; ++a)
@@ -58,7 +63,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(const DensePr
     __syncthreads();
     const DropKey key = g.drop.state ? drop_key(g.drop) : DropKey{0, 0, 0, 0};
     // a thread's four columns of a row
-    for (int i = threadIdx.x; i < RB * CB * 64; i += 64 * kFewWaves) {
+    for (int i = threadIdx.x; i < RB * CB * 64; i += 64 * NW) {
         const int blk = i >> 6, l = i & 63, r = 16 * (blk / CB) + (l & 15), c = 16 * (blk % CB) + 4 * (l >> 4);
         if (r >= rows || c >= cols) continue;
         const int64_t at = (row0 + r) * g.Q + col0 + c;
@@ -68,7 +73,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(const DensePr
         if (g.bias) bias = gload(reinterpret_cast<const f32x4*>(g.bias + col0 + c));
         f32x4 sum = parts[0][blk][l];
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) sum += parts[w][blk][l];
+        for (int w = 1; w < NW; ++w) sum += parts[w][blk][l];
         float v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = sum[k] * g.alpha + bias[k];
@@ -90,19 +95,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(const DensePr
     }
 }
 
-template <int RB, int CB>
+template <int RB, int CB, int NW, int D>
 hipError_t launch_few(const DenseProduct& p, hipStream_t s) {
     const int64_t row_blocks = ceil_div(p.M, 16 * RB), blocks = row_blocks * ceil_div(p.Q, 16 * CB);
     if (blocks > (1 << 30)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((dense_few_kernel<RB, CB>), dim3((unsigned)blocks), dim3(64 * kFewWaves), 0, s, p, (int)row_blocks);
+    hipLaunchKernelGGL((dense_few_kernel<RB, CB, NW, D>), dim3((unsigned)blocks), dim3(64 * NW), 0, s, p, (int)row_blocks);
     return hipGetLastError();
 }
 
 }  // namespace
 
-bool dense_few_wanted(int64_t M, int, int) { return M <= 64; }
 hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s) {
-    return p.M <= 16 ? launch_few<1, 1>(p, s) : p.M <= 32 ? launch_few<2, 1>(p, s) : launch_few<4, 1>(p, s);
+    return p.M <= 16 ? launch_few<1, 1, 8, 2>(p, s) : p.M <= 32 ? launch_few<2, 1, 8, 1>(p, s) : launch_few<4, 1, 8, 1>(p, s);
 }
 
 }  // namespace abt

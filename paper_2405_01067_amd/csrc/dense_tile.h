@@ -50,8 +50,9 @@ struct OutRows {
     }
 };
 
-template <class L>
-__device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& order, int block, unsigned char* lds) {
+// PARTS: the sum over the slabs of piece `part` only, as fp32 to g.parts [pieces, M, Q]; what makes a result of them is another launch.
+template <class L, bool PARTS>
+__device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& order, int block, int part, unsigned char* lds) {
     constexpr int RB = L::RB, CB = L::CB, NW = L::NW;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5;
@@ -67,7 +68,7 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
     // is the same for all j).  Rows past the last one read zeros, and so do chunks past the end of a row.
     const int lrow = 8 * wave + (lane >> 3);
     const int chunk = ((lane & 7) ^ ((lrow >> 1) & 7)) * 16;
-    const int bytes = g.K * 2, slabs = (bytes + 127) / 128;
+    const int bytes = g.K * 2, all = (bytes + 127) / 128, slab0 = PARTS ? part * g.piece : 0, slabs = PARTS && all - slab0 > g.piece ? g.piece : all - slab0;
     const rsrc_t xres = make_rsrc((const char*)g.X + row0 * bytes, (int64_t)rows * bytes);
     const rsrc_t wres = make_rsrc((const char*)g.W + (int64_t)col0 * bytes, (int64_t)cols * bytes);
     int xslot = 0, wslot = L::wbase;                      // of the next parts to be requested
@@ -75,8 +76,9 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
         unsigned char *const w = lds + wslot + wave * 1024, *const x = lds + xslot + wave * 1024;
         wslot = wslot == L::wbase + L::AHEAD * L::wpart ? L::wbase : wslot + L::wpart;
         xslot = xslot == L::AHEAD * L::xpart ? 0 : xslot + L::xpart;
-        const bool there = s * 128 + chunk < bytes;
-        const int off = there ? lrow * bytes + s * 128 + chunk : kBufNowhere, step = there ? 8 * NW * bytes : 0;
+        const int k = (slab0 + s) * 128 + chunk;
+        const bool there = k < bytes;
+        const int off = there ? lrow * bytes + k : kBufNowhere, step = there ? 8 * NW * bytes : 0;
 #pragma unroll
         for (int j = 0; j < L::NF; ++j) load_lds16(wres, w + j * (NW * 1024), off + j * step, 0);
 #pragma unroll
@@ -85,7 +87,6 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
 #pragma unroll
     for (int s = 0; s < L::AHEAD; ++s)
         if (s < slabs) issue(s);
-
     f32x16 acc[RB][CB];
 #pragma unroll
     for (int a = 0; a < RB; ++a)
@@ -140,87 +141,95 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
     }
     mma(o[1]);
 
-    // This lane has row lj of each block, and columns 16 lh .. + 15 of it.
-    lds_barrier();                                        // every wave has read its last slab, and nothing is on its way to LDS
-    using O = OutRows<L>;
-    if (g.residual && !g.Z) O::load(g.residual, row0, col0, rows, cols, g.Q, wave, lane, lds);       // comes while the rest is computed
-    const rsrc_t bres = make_rsrc(g.bias + col0, g.bias ? cols * 4 : 0);      // zeros without a bias
-#pragma unroll
-    for (int b = 0; b < CB; ++b)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 bias = __builtin_bit_cast(f32x4, buf_load16(bres, ((wc * CB + b) * 32 + 16 * lh + 4 * q) * 4, 0));
-#pragma unroll
-            for (int a = 0; a < RB; ++a)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[a][b][4 * q + v] = acc[a][b][4 * q + v] * g.alpha + bias[v];
-        }
-    auto chunk_at = [&](int a, int b, int h) { return lds + O::at((wr * RB + a) * 32 + lj, (wc * CB + b) * 4 + 2 * lh + h); };
-    auto put = [&]() {                                    // rounded
+    if constexpr (PARTS) {
+        float* const to = g.parts + ((int64_t)part * g.M + row0) * g.Q + col0;
 #pragma unroll
         for (int a = 0; a < RB; ++a)
 #pragma unroll
             for (int b = 0; b < CB; ++b)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x4 v;
+                for (int h = 0; h < 2; ++h) {             // eight columns, all there or none
+                    const int r = (wr * RB + a) * 32 + lj, c = (wc * CB + b) * 32 + 16 * lh + 8 * h;
+                    if (r >= rows || c >= cols) continue;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = pack2_bf16(acc[a][b][8 * h + 2 * i], acc[a][b][8 * h + 2 * i + 1]);
-                    *reinterpret_cast<u32x4*>(chunk_at(a, b, h)) = v;
+                    for (int q = 0; q < 2; ++q) {
+                        f32x4 v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = acc[a][b][8 * h + 4 * q + i];
+                        gstore(reinterpret_cast<f32x4*>(to + (int64_t)r * g.Q + c + 4 * q), v);
+                    }
                 }
+        return;
+    }
+    // This lane has row lj of each block, and columns 16 lh .. + 15 of it; a block's bias is asked for one block ahead.
+    const rsrc_t bres = make_rsrc(g.bias + col0, g.bias ? cols * 4 : 0);      // zeros without a bias
+    struct Bias { f32x4 v[4]; };
+    auto bias_of = [&](int b) {
+        Bias bias;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) bias.v[q] = __builtin_bit_cast(f32x4, buf_load16(bres, ((wc * CB + b) * 32 + 16 * lh + 4 * q) * 4, 0));
+        return bias;
+    };
+    const Bias first = bias_of(0);
+    lds_barrier();                                        // every wave has read its last slab, and nothing is on its way to LDS
+    using O = OutRows<L>;
+    if (g.residual && !g.Z) O::load(g.residual, row0, col0, rows, cols, g.Q, wave, lane, lds);       // comes while the rest is computed
+    const DropKey key = g.drop.state ? drop_key(g.drop) : DropKey{0, 0, 0, 0};
+    // Block after block, all the way to LDS: mixed by the scheduler, or with all sums alive across the choice of the activation, 113 registers of the largest tile
+    // spilled.
+    auto finish = [&](bool rounded_sum) {
+        Bias bias = first, next = first;
+#pragma unroll
+        for (int b = 0; b < CB; ++b) {
+            if (b + 1 < CB) next = bias_of(b + 1);
+#pragma unroll
+            for (int a = 0; a < RB; ++a) {
+                const int r = (wr * RB + a) * 32 + lj, c = (wc * CB + b) * 32 + 16 * lh;
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = acc[a][b][i] * g.alpha + bias.v[i >> 2][i & 3];
+                if (!rounded_sum) {
+                    if (g.act != ABT_ACT_NONE)
+                        with_activation(g.act, [&](auto act) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = activate<decltype(act)::value>(v[i]);
+                        });
+                    if (g.drop.state) {
+                        const uint64_t e = ((uint64_t)(row0 + r) * (uint32_t)g.Q + (uint32_t)(col0 + c)) >> 3;
+                        drop8(g.drop, key, e, v);
+                        drop8(g.drop, key, e + 1, v + 8);
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x4* const place = reinterpret_cast<u32x4*>(lds + O::at(r, (c >> 3) + h));
+                    if (!rounded_sum && g.residual) {     // every lane writes where it has read
+                        const u32x4 more = *place;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[8 * h + i] += __builtin_bit_cast(float, i & 1 ? more[i >> 1] & 0xffff0000u : more[i >> 1] << 16);
+                    }
+                    u32x4 out;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) out[i] = pack2_bf16(v[8 * h + 2 * i], v[8 * h + 2 * i + 1]);
+                    *place = out;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            bias = next;
+        }
+        lds_barrier();
     };
     if (g.Z) {
-        put();
-        lds_barrier();
+        finish(true);
         O::store(g.Z, row0, col0, rows, cols, g.Q, wave, lane, lds);
         lds_barrier();
         if (g.residual) O::load(g.residual, row0, col0, rows, cols, g.Q, wave, lane, lds);
     }
-    if (g.act != ABT_ACT_NONE)
-        with_activation(g.act, [&](auto act) {
-#pragma unroll
-            for (int a = 0; a < RB; ++a)
-#pragma unroll
-                for (int b = 0; b < CB; ++b)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[a][b][v] = activate<decltype(act)::value>(acc[a][b][v]);
-        });
-    if (g.drop.state) {
-        const DropKey key = drop_key(g.drop);
-#pragma unroll
-        for (int a = 0; a < RB; ++a)
-#pragma unroll
-            for (int b = 0; b < CB; ++b)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint64_t e = (uint64_t)(row0 + (wr * RB + a) * 32 + lj) * (uint32_t)g.Q + (uint32_t)(col0 + (wc * CB + b) * 32 + 16 * lh + 8 * h);
-                    float v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = acc[a][b][8 * h + i];
-                    drop8(g.drop, key, e >> 3, v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[a][b][8 * h + i] = v[i];
-                }
-    }
     if (g.residual) {
         wait_newest<0>();
         lds_barrier();
-#pragma unroll
-        for (int a = 0; a < RB; ++a)
-#pragma unroll
-            for (int b = 0; b < CB; ++b)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {             // every lane writes where it has read
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(chunk_at(a, b, h));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        acc[a][b][8 * h + 2 * i] += __builtin_bit_cast(float, v[i] << 16);
-                        acc[a][b][8 * h + 2 * i + 1] += __builtin_bit_cast(float, v[i] & 0xffff0000u);
-                    }
-                }
     }
-    put();
-    lds_barrier();
+    finish(false);
     O::store(g.Y, row0, col0, rows, cols, g.Q, wave, lane, lds);
 }
 

@@ -34,9 +34,9 @@ __device__ __forceinline__ u32x4 drop_bits(const DropKey& key, uint64_t block) {
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
         const uint64_t p = (uint64_t)0xD2511F53u * c0, q = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
+        c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(q >> 32), c1, k0, 0x96);          // a ^ b ^ c
         c1 = (uint32_t)q;
-        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p >> 32), c3, k1, 0x96);
         c3 = (uint32_t)p;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -45,7 +45,7 @@ __device__ __forceinline__ u32x4 drop_bits(const DropKey& key, uint64_t block) {
 }
 __device__ __forceinline__ bool drop_keeps(const Drop& d, const u32x4& bits, int i) { return ((bits[i >> 1] >> (16 * (i & 1))) & 0xffffu) >= d.threshold; }
 // eight elements from 8 block on: 0 where dropped, whatever is there
-__device__ __forceinline__ void drop8(const Drop& d, const DropKey& key, uint64_t block, float (&v)[8]) {
+__device__ __forceinline__ void drop8(const Drop& d, const DropKey& key, uint64_t block, float* v) {
     const u32x4 bits = drop_bits(key, block);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = drop_keeps(d, bits, i) ? v[i] * d.scale : 0.0f;

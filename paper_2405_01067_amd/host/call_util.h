@@ -1,4 +1,4 @@
-// What the native calls from Python share (layer_call.cpp, adapter_call.cpp): which tensors they take, the stream, the results.
+// What the native calls from Python share (layer_call.cpp, adapter_call.cpp, dense_call.cpp): which tensors they take, the stream, the results.
 #pragma once
 
 #include <Python.h>

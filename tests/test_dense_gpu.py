@@ -66,7 +66,7 @@ def check_forward(t, act, p, site=3, seed=77, offset=5):
 
 
 SIZES = [(1, 8, 8), (1, 768, 768), (2, 24, 40), (16, 64, 64), (17, 136, 72), (33, 16, 520), (48, 256, 1024), (64, 72, 64), (65, 128, 64), (100, 200, 136), (129, 136, 264),
-         (257, 384, 200), (300, 264, 768), (513, 520, 328), (1000, 72, 96)]
+         (257, 384, 200), (300, 264, 768), (513, 520, 328), (1000, 72, 96), (48, 520, 2304), (300, 264, 1600), (2000, 520, 264)]
 
 
 @pytest.mark.parametrize("M,m,n", SIZES)
