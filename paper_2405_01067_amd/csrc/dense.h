@@ -23,11 +23,14 @@ size_t dense_part_bytes(int64_t M, int Q, int K);
 hipError_t launch_dense(const DenseProduct& p, hipStream_t s);
 hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);        // M <= 64
 
-// What the gradients are made of: dZ = slope(Z) drop(dY) [M, m].  With a smooth activation it is kept as two bf16 values whose sum has 16 bits or more;
-// otherwise one is exact (dropout's factor is left to the products).  Beside it W^T, and sums of dZ over pieces of the rows.
+// What the gradients are made of: dZ = slope(Z) drop(dY) [M, m] as the sum of one, two or three bf16 values.  Without an activation or with ABT_ACT_RELU one is
+// exact (dropout's factor is left to the products).  Otherwise two have 17 bits (1.3e-6 of the size on average) and three all of fp32: three where
+// dW's own sums, fp32 over M rows, are off by less than that.
+constexpr int kDenseThreeValues = 4096;        // rows
+// Beside it W^T, and sums of dZ over pieces of the rows.
 struct DenseSlope {
     const uint16_t* dY; const uint16_t* Z; // Z NULL without an activation
-    uint16_t* high; uint16_t* low;         // high NULL: dY itself is dZ; low NULL: one value
+    uint16_t* value[3];                    // NULL: dY itself is dZ; not kept
     float* sums;                           // [pieces, m] of dZ, without the factor where that is left out; NULL: not wanted
     const uint16_t* W; uint16_t* Wt;       // [m, n] -> [n, m]; NULL: not wanted
     int64_t M;
@@ -38,9 +41,9 @@ struct DenseSlope {
 int dense_piece_rows(int64_t M, int m);
 hipError_t launch_dense_slope(const DenseSlope& p, hipStream_t s);
 
-// dW [m, n] (+)= alpha (high + low)^T X, and dbias [m] (+)= alpha times the sum of `sums`; either may be NULL
+// dW [m, n] (+)= alpha (sum of the values)^T X, and dbias [m] (+)= alpha times the sum of `sums`; either may be NULL
 struct DenseGrads {
-    const uint16_t* high; const uint16_t* low; const uint16_t* X;
+    const uint16_t* value[3]; const uint16_t* X;
     float* dW; float* partials;
     const float* sums; float* dbias;
     int64_t M;
@@ -49,5 +52,8 @@ struct DenseGrads {
 };
 size_t dense_grad_partial_bytes(int64_t M, int m, int n);
 hipError_t launch_dense_grads(const DenseGrads& p, hipStream_t s);
+// Few rows: dX (x.Y NULL: not wanted), dW and dbias in one launch
+constexpr int kDenseFewRows = 1024;
+hipError_t launch_dense_few_rows(const DenseProduct& x, const DenseGrads& g, hipStream_t s);
 
 }  // namespace abt

@@ -22,7 +22,7 @@ int check_dense(int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dro
     return sizes_fit(M, m, n) ? ABT_OK : ABT_ESHAPE;
 }
 
-struct Places { size_t Wt, high, low, sums, parts, partials, bytes; };
+struct Places { size_t Wt, value[3], sums, parts, partials, bytes; };
 Places places(int64_t M, int64_t m, int64_t n) {
     Places p{};
     size_t at = 0;
@@ -31,8 +31,7 @@ Places places(int64_t M, int64_t m, int64_t n) {
         at = align_up(at + bytes, 256);
     };
     take(p.Wt, (size_t)(m * n * 2));
-    take(p.high, (size_t)(M * m * 2));
-    take(p.low, (size_t)(M * m * 2));
+    for (int q = 0; q < (M <= kDenseThreeValues ? 3 : 2); ++q) take(p.value[q], (size_t)(M * m * 2));
     take(p.sums, (size_t)(ceil_div(M, dense_piece_rows(M, (int)m)) * m * 4));
     take(p.parts, dense_part_bytes(M, (int)n, (int)m));
     take(p.partials, dense_grad_partial_bytes(M, (int)m, (int)n));
@@ -85,20 +84,18 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
 
     DenseSlope z{};
     z.dY = (const uint16_t*)dY; z.Z = act == ABT_ACT_NONE ? nullptr : (const uint16_t*)Z;
-    if ((dX || dW) && (z.Z || drop.state)) z.high = (uint16_t*)(ws + at.high);
-    if (smooth && dW) z.low = (uint16_t*)(ws + at.low);
+    if ((dX || dW) && (z.Z || drop.state))
+        for (int q = 0; q < (!smooth || !dW ? 1 : M <= kDenseThreeValues ? 3 : 2); ++q) z.value[q] = (uint16_t*)(ws + at.value[q]);
     if (dbias) z.sums = (float*)(ws + at.sums);
     if (dX) { z.W = (const uint16_t*)W; z.Wt = (uint16_t*)(ws + at.Wt); }
     z.M = M; z.m = (int)m; z.n = (int)n; z.act = act; z.scaled = smooth; z.rows = dense_piece_rows(M, (int)m); z.drop = drop;
     if (launch_dense_slope(z, s) != hipSuccess) return ABT_EHIP;
-    const uint16_t* const high = z.high ? z.high : z.dY;
+    const uint16_t* const dZ = z.value[0] ? z.value[0] : z.dY;
     const float alpha = smooth ? 1.0f : drop.scale;       // what dZ was left without
-    if (dX) {
-        const DenseProduct p{high, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f},
-                             (float*)(ws + at.parts), 0};
-        if (launch_dense(p, s) != hipSuccess) return ABT_EHIP;
-    }
-    const DenseGrads g{high, z.low, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, alpha};
+    const DenseProduct x{dZ, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f}, (float*)(ws + at.parts), 0};
+    const DenseGrads g{{dZ, z.value[1], z.value[2]}, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, alpha};
+    if (M <= kDenseFewRows) return launch_dense_few_rows(x, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
+    if (dX && launch_dense(x, s) != hipSuccess) return ABT_EHIP;
     return launch_dense_grads(g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
 }
 

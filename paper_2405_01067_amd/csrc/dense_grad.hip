@@ -1,9 +1,8 @@
 // Gradients of the dense layer: what its products are made of, and dW = dZ^T X, a contraction over the rows.
-#include <atomic>
 #include <climits>
+#include <cmath>
 
-#include "activation.h"
-#include "dense.h"
+#include "dense_tile.h"
 
 namespace abt {
 namespace {
@@ -20,7 +19,16 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
 }
 __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) { return u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])}; }
 
+// what is left of eight values behind their rounding to bf16: 0 where that is not finite (infinities and NaN are in it)
+__device__ __forceinline__ void rest_of(u32x4 rounded, float (&v)[8]) {
+    float h[8];
+    unpack8(rounded, h);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = __builtin_fabsf(h[k]) < __builtin_inff() ? v[k] - h[k] : 0.0f;
+}
+
 __device__ __forceinline__ void slope_piece(const DenseSlope& g, int piece, int col0, float (*sums)[kSlopeCols]) {
+    constexpr int B = 4;                                  // rows of a wave on their way at a time
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = col0 + 8 * lane;
     const bool there = col < g.m;
     const int64_t first = (int64_t)piece * g.rows, last = first + g.rows < g.M ? first + g.rows : g.M;
@@ -31,30 +39,40 @@ __device__ __forceinline__ void slope_piece(const DenseSlope& g, int piece, int 
     Drop drop = g.drop;
     if (!g.scaled) drop.scale = 1.0f;
     if (there)
-        for (int64_t r = first + wave; r < last; r += 4) {
-            const int64_t at = r * g.m + col;
-            float v[8];
-            unpack8(gload(reinterpret_cast<const u32x4*>(g.dY + at)), v);
-            if (g.Z) {
-                float z[8];
-                unpack8(gload(reinterpret_cast<const u32x4*>(g.Z + at)), z);
-                with_activation(g.act, [&](auto act) {
+        for (int64_t r = first + wave; r < last; r += 4 * B) {
+            u32x4 dy[B], z[B];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] *= slope<decltype(act)::value>(z[k]);
-                });
+            for (int i = 0; i < B; ++i) {
+                const int64_t at = (r + 4 * i < last ? r + 4 * i : r) * g.m + col;
+                dy[i] = gload(reinterpret_cast<const u32x4*>(g.dY + at));
+                if (g.Z) z[i] = gload(reinterpret_cast<const u32x4*>(g.Z + at));
             }
-            if (g.drop.state) drop8(drop, key, (uint64_t)at >> 3, v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) total[k] += v[k];
-            if (!g.high) continue;
-            const u32x4 high = pack8(v);
-            gstore(reinterpret_cast<u32x4*>(g.high + at), high);
-            if (!g.low) continue;
-            float h[8], l[8];
-            unpack8(high, h);
+            for (int i = 0; i < B; ++i) {
+                if (r + 4 * i >= last) break;
+                const int64_t at = (r + 4 * i) * g.m + col;
+                float v[8];
+                unpack8(dy[i], v);
+                if (g.Z) {
+                    float zz[8];
+                    unpack8(z[i], zz);
+                    with_activation(g.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) l[k] = __builtin_fabsf(h[k]) < __builtin_inff() ? v[k] - h[k] : 0.0f;      // (infinities and NaN are in h)
-            gstore(reinterpret_cast<u32x4*>(g.low + at), pack8(l));
+                        for (int k = 0; k < 8; ++k) v[k] *= slope<decltype(act)::value>(zz[k]);
+                    });
+                }
+                if (g.drop.state) drop8(drop, key, (uint64_t)at >> 3, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) total[k] += v[k];
+                if (!g.value[0]) continue;
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    if (!g.value[q]) break;
+                    const u32x4 rounded = pack8(v);
+                    gstore(reinterpret_cast<u32x4*>(g.value[q] + at), rounded);
+                    rest_of(rounded, v);
+                }
+            }
         }
     if (!g.sums) return;
 #pragma unroll
@@ -91,32 +109,54 @@ __global__ __launch_bounds__(256) void dense_slope_kernel(const DenseSlope g, in
 }
 
 // ------------------------------------------------------------------------------------------ dW
-// TP x TQ of dW by WP x WQ waves of RB x CB blocks of 32 x 32; a slab is 32 rows of both sides as they lie, in a ring of NS slots.  Both are read with the
-// transposing load: sixteen lanes ask for four rows of sixteen columns, and lane i gets the four of column i.
-template <int TP_, int TQ_, int WP_, int WQ_, int PLANES_, int NS_>
+// TP x TQ of dW by WP x WQ waves of RB x CB blocks of 32 x 32; a slab is 32 rows of X and of each of dZ's values as they lie, in a ring of NS slots.  All are read with
+// the transposing load: sixteen lanes ask for four rows of sixteen columns, and lane i gets the four of column i.
+template <int TP_, int TQ_, int WP_, int WQ_, int VALUES_, int NS_>
 struct GradTile {
-    static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, PLANES = PLANES_, NS = NS_, NW = WP * WQ;
+    static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, VALUES = VALUES_, NS = NS_, NW = WP * WQ;
     static constexpr int RB = TP / (32 * WP), CB = TQ / (32 * WQ);
-    static constexpr int ppart = 32 * TP * 2, qpart = 32 * TQ * 2, xbase = PLANES * ppart, slab = xbase + qpart, lds = NS * slab;
-    static constexpr int NP = ppart / 1024 / NW, NQ = qpart / 1024 / NW, NL = PLANES * NP + NQ;        // load instructions per wave and slab
-    static_assert(NP * NW * 1024 == ppart && NQ * NW * 1024 == qpart && RB * 32 * WP == TP && CB * 32 * WQ == TQ && TP >= 128 && TQ >= 128, "");
-    static_assert(lds <= 160 * 1024 && (NS - 2) * NL < 64, "");
+    static constexpr int ppart = 32 * TP * 2, qpart = 32 * TQ * 2, xbase = VALUES * ppart, slab = xbase + qpart, lds = NS * slab;
+    static constexpr int NP = ppart / 1024 / NW, NQ = qpart / 1024 / NW, NL = VALUES * NP + NQ;        // load instructions per wave and slab
+    static_assert(NP * NW * 1024 == ppart && NQ * NW * 1024 == qpart && RB * 32 * WP == TP && CB * 32 * WQ == TQ && TP >= 64 && TQ >= 64, "");
+    static_assert(NS >= 2 && lds <= 160 * 1024 && (NS - 2) * NL < 64, "");
+    // Chunk c of row r lies at c ^ turn(r): the four rows of 64 bytes that half a wave asks for fall on all banks.
+    static __device__ __forceinline__ int turn(int width, int r) { return width == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
 };
 
-__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
-// Two operands of 16 rows, whose halves are BACK bytes apart.  Before the transposing load in its builtin form the compiler waits for every load to LDS on its way,
-// whichever slot of the ring it goes to: here they are issued with a wait of their own.
+// An operand of 16 rows, whose halves are BACK bytes apart; two of them.  Before the transposing load in its builtin form the compiler waits for every load to LDS on its
+// way, whichever slot of the ring it goes to: here they are issued with a wait of their own.
 template <int OFF, int BACK>
-__device__ __forceinline__ void read_two(uint32_t at0, uint32_t at1, u32x4& v0, u32x4& v1) {
+__device__ __forceinline__ void read_operands(uint32_t at, u32x4 (&v)[1], const uint32_t (&from)[1]) {
+    u32x2 a, b;
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b) : "v"(at + from[0]), "n"(OFF), "n"(OFF + BACK) : "memory");
+    v[0] = u32x4{a[0], a[1], b[0], b[1]};
+}
+template <int OFF, int BACK>
+__device__ __forceinline__ void read_operands(uint32_t at, u32x4 (&v)[2], const uint32_t (&from)[2]) {
     u32x2 a, b, c, d;
     asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\tds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
                  "ds_read_b64_tr_b16 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d) : "v"(at0), "v"(at1), "n"(OFF), "n"(OFF + BACK) : "memory");
-    v0 = u32x4{a[0], a[1], b[0], b[1]};
-    v1 = u32x4{c[0], c[1], d[0], d[1]};
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d) : "v"(at + from[0]), "v"(at + from[1]), "n"(OFF), "n"(OFF + BACK) : "memory");
+    v[0] = u32x4{a[0], a[1], b[0], b[1]};
+    v[1] = u32x4{c[0], c[1], d[0], d[1]};
 }
+template <int OFF, int BACK>
+__device__ __forceinline__ void read_operands(uint32_t at, u32x4 (&v)[4], const uint32_t (&from)[4]) {
+    u32x2 a, b, c, d, e, f, g, h;
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\tds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%13\n\tds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(f), "=&v"(g), "=&v"(h)
+                 : "v"(at + from[0]), "v"(at + from[1]), "v"(at + from[2]), "v"(at + from[3]), "n"(OFF), "n"(OFF + BACK) : "memory");
+    v[0] = u32x4{a[0], a[1], b[0], b[1]};
+    v[1] = u32x4{c[0], c[1], d[0], d[1]};
+    v[2] = u32x4{e[0], e[1], f[0], f[1]};
+    v[3] = u32x4{g[0], g[1], h[0], h[1]};
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
-struct GradOrder { int col_tiles, splits, slabs; };       // tiles across; pieces of the rows and their length in slabs
+struct GradOrder { int col_tiles, tiles, splits, slabs; };       // pieces of the rows and their length in slabs
 
 template <class L>
 __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& o, int block, unsigned char* lds) {
@@ -124,16 +164,15 @@ __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lj = lane & 31, lh = lane >> 5, li = lane & 15;
     const int wp = wave / L::WQ, wq = wave % L::WQ;
-    const int split = block % o.splits, tile = block / o.splits;
+    const int split = block / o.tiles, tile = block % o.tiles;
     const int p0 = tile / o.col_tiles * L::TP, q0 = tile % o.col_tiles * L::TQ;
     const int pcols = g.m - p0 < L::TP ? g.m - p0 : L::TP, qcols = g.n - q0 < L::TQ ? g.n - q0 : L::TQ;
     const int64_t first = (int64_t)split * o.slabs * 32, last = first + (int64_t)o.slabs * 32 < g.M ? first + (int64_t)o.slabs * 32 : g.M;
     const int ns = (int)((last - first + 31) / 32);
 
-    // chunk c of row r lies at c ^ 4 (r & 3): the eight rows of 64 bytes that a load asks for fall on all banks
-    auto lane_offset = [&](int pitch, int width, int cols, int j) {
-        const int pos = (j * NW + wave) * 64 + lane, r = pos / (pitch / 8), c = ((pos % (pitch / 8)) ^ ((r & 3) << 2)) * 8;
-        return c < cols ? (r * width + c) * 2 : kBufNowhere;
+    auto lane_offset = [&](int width, int pitch, int cols, int j) {
+        const int pos = (j * NW + wave) * 64 + lane, r = pos / (width / 8), c = ((pos % (width / 8)) ^ L::turn(width, r)) * 8;
+        return c < cols ? (r * pitch + c) * 2 : kBufNowhere;
     };
     int poff[L::NP], qoff[L::NQ];
 #pragma unroll
@@ -145,16 +184,15 @@ __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& 
         const int64_t row = first + (int64_t)s * 32;
         const int rows = last - row < 32 ? (int)(last - row) : 32;            // rows past the last one read zeros
         const int64_t pbytes = ((int64_t)(rows - 1) * g.m + pcols) * 2, qbytes = ((int64_t)(rows - 1) * g.n + qcols) * 2;
-        const rsrc_t high = make_rsrc(g.high + row * g.m + p0, pbytes), x = make_rsrc(g.X + row * g.n + q0, qbytes);
 #pragma unroll
-        for (int j = 0; j < L::NP; ++j) load_lds16(high, dst + j * (NW * 1024), poff[j], 0);
-        if (L::PLANES == 2) {
-            const rsrc_t low = make_rsrc(g.low + row * g.m + p0, pbytes);
+        for (int q = 0; q < L::VALUES; ++q) {
+            const rsrc_t res = make_rsrc(g.value[q] + row * g.m + p0, pbytes);
 #pragma unroll
-            for (int j = 0; j < L::NP; ++j) load_lds16(low, dst + L::ppart + j * (NW * 1024), poff[j], 0);
+            for (int j = 0; j < L::NP; ++j) load_lds16(res, dst + q * L::ppart + j * (NW * 1024), poff[j], 0);
         }
+        const rsrc_t res = make_rsrc(g.X + row * g.n + q0, qbytes);
 #pragma unroll
-        for (int j = 0; j < L::NQ; ++j) load_lds16(x, dst + L::xbase + j * (NW * 1024), qoff[j], 0);
+        for (int j = 0; j < L::NQ; ++j) load_lds16(res, dst + L::xbase + j * (NW * 1024), qoff[j], 0);
     };
 
     f32x16 acc[RB][CB];
@@ -166,29 +204,26 @@ __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& 
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
     // Rows 4 lh + li / 4 and 8 more of a step of sixteen; quad t of a block's columns, taken in the order of out_row on X's side, so that a lane's sums are
     // sixteen consecutive columns of a row of dW.
-    const int t = 4 * ((lane >> 4) & 1) + (li & 3), tx = 4 * (t & 1) + (t >> 1), trow = 4 * lh + (li >> 2), swz = ((li >> 2) & 3) << 2;
+    const int t = 4 * ((lane >> 4) & 1) + (li & 3), tx = 4 * (t & 1) + (t >> 1), trow = 4 * lh + (li >> 2);
     uint32_t pat[RB], qat[CB];
 #pragma unroll
-    for (int a = 0; a < RB; ++a) pat[a] = trow * (L::TP * 2) + ((((wp * RB + a) * 4 + (t >> 1)) ^ swz) * 16) + (t & 1) * 8;
+    for (int a = 0; a < RB; ++a) pat[a] = trow * (L::TP * 2) + ((((wp * RB + a) * 4 + (t >> 1)) ^ L::turn(L::TP, trow)) * 16) + (t & 1) * 8;
 #pragma unroll
-    for (int b = 0; b < CB; ++b) qat[b] = L::xbase + trow * (L::TQ * 2) + ((((wq * CB + b) * 4 + (tx >> 1)) ^ swz) * 16) + (tx & 1) * 8;
+    for (int b = 0; b < CB; ++b) qat[b] = L::xbase + trow * (L::TQ * 2) + ((((wq * CB + b) * 4 + (tx >> 1)) ^ L::turn(L::TQ, trow)) * 16) + (tx & 1) * 8;
     auto step = [&](uint32_t base, auto half) {
         constexpr int H = decltype(half)::value, PO = H * 16 * L::TP * 2, QO = H * 16 * L::TQ * 2;
-        static_assert(RB % 2 == 0 && CB % 2 == 0, "");
-        u32x4 x[CB], z[L::PLANES][RB];
-#pragma unroll
-        for (int b = 0; b < CB; b += 2) read_two<QO, 8 * L::TQ * 2>(base + qat[b], base + qat[b + 1], x[b], x[b + 1]);
-#pragma unroll
-        for (int a = 0; a < RB; a += 2) read_two<PO, 8 * L::TP * 2>(base + pat[a], base + pat[a + 1], z[0][a], z[0][a + 1]);
-        if constexpr (L::PLANES == 2)
-#pragma unroll
-            for (int a = 0; a < RB; a += 2) read_two<PO + L::ppart, 8 * L::TP * 2>(base + pat[a], base + pat[a + 1], z[1][a], z[1][a + 1]);
-#pragma unroll
-        for (int q = 0; q < L::PLANES; ++q)
+        u32x4 x[CB], z[RB];
+        read_operands<QO, 8 * L::TQ * 2>(base, x, qat);
+        auto products = [&](auto value) {
+            read_operands<PO + decltype(value)::value * L::ppart, 8 * L::TP * 2>(base, z, pat);
 #pragma unroll
             for (int a = 0; a < RB; ++a)
 #pragma unroll
-                for (int b = 0; b < CB; ++b) acc[a][b] = mfma_bf16(x[b], z[q][a], acc[a][b]);
+                for (int b = 0; b < CB; ++b) acc[a][b] = mfma_bf16(x[b], z[a], acc[a][b]);
+        };
+        products(std::integral_constant<int, 0>{});
+        if constexpr (L::VALUES > 1) products(std::integral_constant<int, 1>{});
+        if constexpr (L::VALUES > 2) products(std::integral_constant<int, 2>{});
     };
     int issued = 0;
     for (; issued < L::NS - 1 && issued < ns; ++issued) issue(issued, issued);
@@ -224,65 +259,126 @@ __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& 
     }
 }
 
-template <class L>
-__global__ __launch_bounds__(64 * L::NW) void dense_grad_kernel(const DenseGrads g, const GradOrder o) {
+// 32 columns of dbias from the sums of the pieces
+__device__ __forceinline__ void bias_block(const DenseGrads& g, int block, float (*lds)[32]) {
+    const int c = block * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    float s = 0.0f;
+    if (c < g.m) {
+        const float* const from = g.sums + c;
+        int r = part;
+        for (; r + 56 < g.pieces; r += 64) {              // eight loads on their way at a time
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = gload(from + (int64_t)(r + 8 * k) * g.m);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
+        for (; r < g.pieces; r += 8) s += gload(from + (int64_t)r * g.m);
+    }
+    lds[part][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (part || c >= g.m) return;
+    for (int k = 1; k < 8; ++k) s += lds[k][threadIdx.x];
+    s *= g.alpha;
+    gstore(g.dbias + c, g.accumulate ? gload(g.dbias + c) + s : s);
+}
+
+template <class L, int PER_CU>
+__global__ __launch_bounds__(64 * L::NW, PER_CU * L::NW / 4) void dense_grad_kernel(const DenseGrads g, const GradOrder o) {
     extern __shared__ __align__(1024) unsigned char lds[];
     grad_tile<L>(g, o, blockIdx.x, lds);
 }
 
-// dW (+)= the sum of the partials in order; behind those work-groups, 64 columns of dbias each
+// dW (+)= the sum of the partials in order; behind those work-groups the ones of dbias
 __global__ __launch_bounds__(256) void dense_sum_kernel(const DenseGrads g, int splits, int blocks) {
-    if ((int)blockIdx.x < blocks) {
-        const int64_t size = (int64_t)g.m * g.n, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-        if (i >= size) return;
-        f32x4 v = {0, 0, 0, 0};
-        for (int p = 0; p < splits; p += 8) {             // eight loads on their way at a time
-            f32x4 x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = gload(reinterpret_cast<const f32x4*>(g.partials + (p + k < splits ? p + k : p) * size + i));
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (p + k < splits) v += x[k];
-        }
-        f32x4* const d = reinterpret_cast<f32x4*>(g.dW + i);
-        if (g.accumulate) v += gload(d);
-        gstore(d, v);
+    __shared__ float lds[8][32];
+    if ((int)blockIdx.x >= blocks) {
+        bias_block(g, (int)blockIdx.x - blocks, lds);
         return;
     }
-    __shared__ float sums[4][64];
-    const int c = ((int)blockIdx.x - blocks) * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6;
-    float v = 0.0f;
-    if (c < g.m)
-        for (int p = part; p < g.pieces; p += 4) v += gload(g.sums + (int64_t)p * g.m + c);
-    sums[part][threadIdx.x & 63] = v;
-    __syncthreads();
-    if (part || c >= g.m) return;
-    v = ((sums[0][c & 63] + sums[1][c & 63]) + (sums[2][c & 63] + sums[3][c & 63])) * g.alpha;
-    gstore(g.dbias + c, g.accumulate ? gload(g.dbias + c) + v : v);
+    const int64_t size = (int64_t)g.m * g.n, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= size) return;
+    f32x4 v = {0, 0, 0, 0};
+    for (int p = 0; p < splits; p += 4) {                 // four loads on their way at a time
+        f32x4 x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = gload(reinterpret_cast<const f32x4*>(g.partials + (p + k < splits ? p + k : p) * size + i));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (p + k < splits) v += x[k];
+    }
+    f32x4* const d = reinterpret_cast<f32x4*>(g.dW + i);
+    if (g.accumulate) v += gload(d);
+    gstore(d, v);
 }
 
-using Grad2 = GradTile<128, 256, 2, 4, 2, 4>;
-using Grad1 = GradTile<128, 256, 2, 4, 1, 4>;
-
-GradOrder grad_order(int64_t M, int m, int n) {
-    const int64_t tiles = ceil_div(m, Grad2::TP) * ceil_div(n, Grad2::TQ), slabs = ceil_div(M, 32);
-    int64_t splits = tiles >= 256 ? 1 : 256 / tiles;
-    if (splits > slabs / 4) splits = slabs / 4 < 1 ? 1 : slabs / 4;
-    const int64_t each = ceil_div(slabs, splits);
-    return GradOrder{(int)ceil_div(n, Grad2::TQ), (int)ceil_div(slabs, each), (int)each};
-}
-
+// Everything behind dZ for few rows in one launch: the tiles of dX, of dW, and dbias.
 template <class L>
+__global__ __launch_bounds__(256, 2) void dense_few_rows_kernel(const DenseProduct x, const Order order, const DenseGrads g, const GradOrder o) {
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tiles = order.row_tiles * order.col_tiles, i = (int)blockIdx.x - tiles;
+    if (i < 0) dense_tile<Tile<64, 64, 2, 2, 2>, false>(x, order, blockIdx.x, 0, lds);
+    else if (i < o.tiles) grad_tile<L>(g, o, i, lds);
+    else bias_block(g, i - o.tiles, reinterpret_cast<float (*)[32]>(lds));
+}
+
+template <int V> using Grad256 = GradTile<256, 256, 4, 2, V, V == 1 ? 4 : V == 2 ? 3 : 2>;
+template <int V> using Grad128 = GradTile<128, 128, 2, 2, V, V == 3 ? 2 : 3>;
+template <int V> using Grad64 = GradTile<64, 64, 2, 2, V, 4>;
+
+struct GradCost { int t, per_cu; float slab, rest; };
+constexpr GradCost kGrads[] = {{256, 1, 1.1f, 8.0f}, {128, 2, 0.5f, 4.0f}, {64, 3, 0.25f, 2.0f}};
+struct GradWay { int tile; GradOrder order; };
+GradOrder grad_order(int t, int64_t M, int m, int n, int64_t splits) {
+    const int64_t slabs = ceil_div(M, 32), each = ceil_div(slabs, splits);
+    return GradOrder{(int)ceil_div(n, t), (int)(ceil_div(m, t) * ceil_div(n, t)), (int)ceil_div(slabs, each), (int)each};
+}
+GradWay grad_way(int64_t M, int m, int n) {
+    GradWay best{};
+    float cost = 1e30f;
+    for (int i = 0; i < 3; ++i)
+        for (int64_t splits = 1; splits <= 32 && (splits == 1 || splits * 4 <= ceil_div(M, 32)); ++splits) {
+            const GradOrder o = grad_order(kGrads[i].t, M, m, n, splits);
+            const float groups = (float)o.tiles * (float)o.splits, work = (float)o.slabs * kGrads[i].slab + kGrads[i].rest;
+            float c = ceilf(groups / 256.0f) * work;
+            if (o.splits > 1) c += 2.8f + 2.0e-6f * (float)o.splits * (float)m * (float)n;
+            if (c < cost) cost = c, best = GradWay{i, o};
+        }
+    return best;
+}
+
+template <class L, int PER_CU>
 hipError_t launch_grad(const DenseGrads& p, const GradOrder& o, hipStream_t s) {
     static std::atomic<bool> attr_set{false};
-    if (!attr_set.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&dense_grad_kernel<L>), hipFuncAttributeMaxDynamicSharedMemorySize, L::lds);
-        if (e != hipSuccess) return e;
-        attr_set.store(true, std::memory_order_release);
-    }
-    const int64_t blocks = ceil_div(p.m, L::TP) * o.col_tiles * o.splits;
+    const hipError_t e = lds_allowed(reinterpret_cast<const void*>(&dense_grad_kernel<L, PER_CU>), L::lds, attr_set);
+    if (e != hipSuccess) return e;
+    const int64_t blocks = (int64_t)o.tiles * o.splits;
     if (blocks > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((dense_grad_kernel<L>), dim3((unsigned)blocks), dim3(64 * L::NW), L::lds, s, p, o);
+    hipLaunchKernelGGL((dense_grad_kernel<L, PER_CU>), dim3((unsigned)blocks), dim3(64 * L::NW), L::lds, s, p, o);
+    return hipGetLastError();
+}
+template <int V>
+hipError_t launch_grad(const DenseGrads& p, const GradWay& w, hipStream_t s) {
+    switch (w.tile) {
+        case 0: return launch_grad<Grad256<V>, 1>(p, w.order, s);
+        case 1: return launch_grad<Grad128<V>, 2>(p, w.order, s);
+        default: return launch_grad<Grad64<V>, 2>(p, w.order, s);
+    }
+}
+template <int V>
+hipError_t launch_few_rows(const DenseProduct& x, const DenseGrads& g, hipStream_t s) {
+    using L = Grad64<V>;
+    constexpr int lds = L::lds > Tile<64, 64, 2, 2, 2>::lds ? L::lds : Tile<64, 64, 2, 2, 2>::lds;
+    static std::atomic<bool> attr_set{false};
+    const hipError_t e = lds_allowed(reinterpret_cast<const void*>(&dense_few_rows_kernel<L>), lds, attr_set);
+    if (e != hipSuccess) return e;
+    const int64_t rt = x.Y ? ceil_div(x.M, 64) : 0, ct = ceil_div(x.Q, 64);
+    GradOrder o = grad_order(64, g.M, g.m, g.n, 1);
+    if (!g.dW) o.tiles = 0;
+    const int64_t blocks = rt * ct + o.tiles + (g.dbias ? ceil_div(g.m, 32) : 0);
+    if (blocks > INT_MAX) return hipErrorInvalidValue;
+    if (blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL((dense_few_rows_kernel<L>), dim3((unsigned)blocks), dim3(256), lds, s, x, Order{(int)rt, (int)ct}, g, o);
     return hipGetLastError();
 }
 
@@ -294,7 +390,7 @@ int dense_piece_rows(int64_t M, int m) {
     return rows < 8 ? 8 : (int)rows;
 }
 hipError_t launch_dense_slope(const DenseSlope& p, hipStream_t s) {
-    const bool rows = p.high || p.sums;
+    const bool rows = p.value[0] || p.sums;
     const int64_t pieces = rows ? ceil_div(p.M, p.rows) : 0, slabs = ceil_div(p.m, kSlopeCols);
     const int64_t blocks = pieces * slabs + (p.Wt ? ceil_div(p.m, 64) * ceil_div(p.n, 64) : 0);
     if (blocks == 0) return hipSuccess;
@@ -304,20 +400,23 @@ hipError_t launch_dense_slope(const DenseSlope& p, hipStream_t s) {
 }
 
 size_t dense_grad_partial_bytes(int64_t M, int m, int n) {
-    const GradOrder o = grad_order(M, m, n);
-    return o.splits == 1 ? 0 : (size_t)o.splits * (size_t)m * (size_t)n * 4;
+    const GradWay w = grad_way(M, m, n);
+    return w.order.splits == 1 ? 0 : (size_t)w.order.splits * (size_t)m * (size_t)n * 4;
 }
 hipError_t launch_dense_grads(const DenseGrads& p, hipStream_t s) {
-    const GradOrder o = grad_order(p.M, p.m, p.n);
+    const GradWay w = grad_way(p.M, p.m, p.n);
     if (p.dW) {
-        const hipError_t e = p.low ? launch_grad<Grad2>(p, o, s) : launch_grad<Grad1>(p, o, s);
+        const hipError_t e = p.value[2] ? launch_grad<3>(p, w, s) : p.value[1] ? launch_grad<2>(p, w, s) : launch_grad<1>(p, w, s);
         if (e != hipSuccess) return e;
     }
-    const int64_t blocks = p.dW && o.splits > 1 ? ceil_div((int64_t)p.m * p.n, 1024) : 0, more = p.dbias ? ceil_div(p.m, 64) : 0;
+    const int64_t blocks = p.dW && w.order.splits > 1 ? ceil_div((int64_t)p.m * p.n, 1024) : 0, more = p.dbias ? ceil_div(p.m, 32) : 0;
     if (blocks + more == 0) return hipSuccess;
     if (blocks + more > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(dense_sum_kernel, dim3((unsigned)(blocks + more)), dim3(256), 0, s, p, o.splits, (int)blocks);
+    hipLaunchKernelGGL(dense_sum_kernel, dim3((unsigned)(blocks + more)), dim3(256), 0, s, p, w.order.splits, (int)blocks);
     return hipGetLastError();
+}
+hipError_t launch_dense_few_rows(const DenseProduct& x, const DenseGrads& g, hipStream_t s) {
+    return g.value[2] ? launch_few_rows<3>(x, g, s) : g.value[1] ? launch_few_rows<2>(x, g, s) : launch_few_rows<1>(x, g, s);
 }
 
 }  // namespace abt
