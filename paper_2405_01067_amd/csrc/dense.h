@@ -21,6 +21,10 @@ struct DenseProduct {
 };
 size_t dense_part_bytes(int64_t M, int Q, int K);
 hipError_t launch_dense(const DenseProduct& p, hipStream_t s);
+// What it costs, us, without an epilogue, and with tiles of 64 x 64: the longest of them, and what they keep the chip busy
+float dense_cost(int64_t M, int Q, int K);
+struct SmallCost { float longest, load; };
+SmallCost dense_small_cost(int64_t M, int Q, int K);
 hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);        // M <= 64
 
 // What the gradients are made of: dZ = slope(Z) drop(dY) [M, m] as the sum of one, two or three bf16 values.  Without an activation or with ABT_ACT_RELU one is
@@ -51,9 +55,7 @@ struct DenseGrads {
     float alpha;
 };
 size_t dense_grad_partial_bytes(int64_t M, int m, int n);
-hipError_t launch_dense_grads(const DenseGrads& p, hipStream_t s);
-// Few rows: dX (x.Y NULL: not wanted), dW and dbias in one launch
-constexpr int kDenseFewRows = 1024;
-hipError_t launch_dense_few_rows(const DenseProduct& x, const DenseGrads& g, hipStream_t s);
+// dX (x.Y NULL: not wanted), dW and dbias in one launch, or each in its own
+hipError_t launch_dense_bwd(const DenseProduct& x, const DenseGrads& g, hipStream_t s);
 
 }  // namespace abt

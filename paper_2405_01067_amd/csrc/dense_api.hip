@@ -94,9 +94,7 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
     const float alpha = smooth ? 1.0f : drop.scale;       // what dZ was left without
     const DenseProduct x{dZ, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f}, (float*)(ws + at.parts), 0};
     const DenseGrads g{{dZ, z.value[1], z.value[2]}, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, alpha};
-    if (M <= kDenseFewRows) return launch_dense_few_rows(x, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
-    if (dX && launch_dense(x, s) != hipSuccess) return ABT_EHIP;
-    return launch_dense_grads(g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
+    return launch_dense_bwd(x, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
 }
 
 int lr_dropout(const void* X, const void* residual, void* Y, int64_t count, const abt_dropout* dropout, int dt, void* stream) {

@@ -3,6 +3,7 @@
 #include "activation.h"
 #include "adapters_operands.h"
 #include "dense.h"
+#include "nt_tile.h"
 
 namespace abt {
 namespace {
@@ -14,7 +15,7 @@ __global__ __launch_bounds__(64 * NW) void dense_few_kernel(const DenseProduct g
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 15, lq = lane >> 4;
     // the row blocks of the same columns follow each other on one XCD, whose L2 then has W once
-    const int per = (int)gridDim.x >> 3, rem = (int)gridDim.x & 7, xcd = blockIdx.x & 7, block = xcd * per + (xcd < rem ? xcd : rem) + (blockIdx.x >> 3);
+    const int block = xcd_order(blockIdx.x, gridDim.x);
     const int64_t row0 = (int64_t)(block % row_blocks) * (16 * RB);
     const int col0 = block / row_blocks * (16 * CB);
     const int rows = g.M - row0 < 16 * RB ? (int)(g.M - row0) : 16 * RB, cols = g.Q - col0 < 16 * CB ? g.Q - col0 : 16 * CB;

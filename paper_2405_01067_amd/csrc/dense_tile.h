@@ -50,7 +50,7 @@ struct OutRows {
     }
 };
 
-// PARTS: the sum over the slabs of piece `part` only, as fp32 to g.parts [pieces, M, Q]; what makes a result of them is another launch.
+// `block` in the order of tile_at.  PARTS: the sum over the slabs of piece `part` only, as fp32 to g.parts [pieces, M, Q]; what makes a result of them is another launch.
 template <class L, bool PARTS>
 __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& order, int block, int part, unsigned char* lds) {
     constexpr int RB = L::RB, CB = L::CB, NW = L::NW;
@@ -58,7 +58,7 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
     const int lj = lane & 31, lh = lane >> 5;
     const int wr = wave / L::WN, wc = wave % L::WN;
     int rt, ct;
-    tile_of(order, block, rt, ct);
+    tile_at(order, block, rt, ct);
     const int64_t row0 = (int64_t)rt * L::TM;
     const int col0 = ct * L::TN;
     const int rows = g.M - row0 < L::TM ? (int)(g.M - row0) : L::TM;

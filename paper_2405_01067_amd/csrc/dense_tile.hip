@@ -12,13 +12,13 @@ namespace {
 template <class L, int PER_CU>
 __global__ __launch_bounds__(64 * L::NW, PER_CU * L::NW / 4) void dense_kernel(const DenseProduct g, const Order order) {
     extern __shared__ __align__(1024) unsigned char lds[];
-    dense_tile<L, false>(g, order, blockIdx.x, 0, lds);
+    dense_tile<L, false>(g, order, xcd_order(blockIdx.x, gridDim.x), 0, lds);
 }
 template <class L, int PER_CU>
 __global__ __launch_bounds__(64 * L::NW, PER_CU * L::NW / 4) void dense_parts_kernel(const DenseProduct g, const Order order) {
     extern __shared__ __align__(1024) unsigned char lds[];
-    const int tiles = order.row_tiles * order.col_tiles;
-    dense_tile<L, true>(g, order, (int)blockIdx.x % tiles, (int)blockIdx.x / tiles, lds);
+    const int tiles = order.row_tiles * order.col_tiles, w = xcd_order(blockIdx.x, gridDim.x);
+    dense_tile<L, true>(g, order, w % tiles, w / tiles, lds);
 }
 
 // The epilogue of a product that lies in parts, eight columns of a row per thread
@@ -114,21 +114,20 @@ float tile_cost(const TileCost& t, int64_t M, int Q, int K, int pieces, bool mor
     return shared > alone ? shared : alone;
 }
 // Which tile, or kFew, and in how many pieces
-struct Way { int tile, pieces; };
+struct Way { int tile, pieces; float cost; };
 Way way_of(int64_t M, int Q, int K, bool more) {
-    Way best{0, 1};
-    float cost = tile_cost(kTiles[0], M, Q, K, 1, more);
-    auto offer = [&](Way w, float c) {
-        if (c < cost) best = w, cost = c;
+    Way best{0, 1, tile_cost(kTiles[0], M, Q, K, 1, more)};
+    auto offer = [&](int tile, int pieces, float cost) {
+        if (cost < best.cost) best = Way{tile, pieces, cost};
     };
-    for (int i = 1; i <= kSmallest; ++i) offer(Way{i, 1}, tile_cost(kTiles[i], M, Q, K, 1, more));
+    for (int i = 1; i <= kSmallest; ++i) offer(i, 1, tile_cost(kTiles[i], M, Q, K, 1, more));
     // four slabs a piece or more; the join is a launch and its bytes
     for (int pieces : {2, 3, 4, 6, 8})
         if (4 * pieces <= (K + 63) / 64)
-            offer(Way{kSmallest, pieces}, tile_cost(kTiles[kSmallest], M, Q, K, pieces, false) + 2.8f + 0.35e-6f * (float)M * (float)Q * (float)(8 * pieces + (more ? 4 : 2)));
+            offer(kSmallest, pieces, tile_cost(kTiles[kSmallest], M, Q, K, pieces, false) + 2.8f + 0.35e-6f * (float)M * (float)Q * (float)(8 * pieces + (more ? 4 : 2)));
     if (M <= 64) {                                        // bytes of a work-group at 35 KB a us
         const float rows = (float)(M <= 16 ? 16 : M <= 32 ? 32 : 64), blocks = (float)Q / 4096.0f;
-        offer(Way{kFew, 1}, 2.8f + (16.0f + rows) * 2.0f * (float)K / 35e3f * (blocks < 1.0f ? 1.0f : blocks));
+        offer(kFew, 1, 2.8f + (16.0f + rows) * 2.0f * (float)K / 35e3f * (blocks < 1.0f ? 1.0f : blocks));
     }
     return best;
 }
@@ -138,6 +137,11 @@ Way way_of(int64_t M, int Q, int K, bool more) {
 size_t dense_part_bytes(int64_t M, int Q, int K) {
     const int a = way_of(M, Q, K, false).pieces, b = way_of(M, Q, K, true).pieces, pieces = a > b ? a : b;
     return pieces == 1 ? 0 : (size_t)pieces * (size_t)M * (size_t)Q * 4;
+}
+float dense_cost(int64_t M, int Q, int K) { return way_of(M, Q, K, false).cost; }
+SmallCost dense_small_cost(int64_t M, int Q, int K) {
+    const TileCost& t = kTiles[kSmallest];
+    return SmallCost{tile_cost(t, M, Q, K, 1, false), (float)(ceil_div(M, t.tm) * ceil_div(Q, t.tn)) / 256.0f * ((float)((K + 63) / 64) * t.slab + t.rest)};
 }
 hipError_t launch_dense(const DenseProduct& p, hipStream_t s) {
     const Way w = way_of(p.M, p.Q, p.K, p.Z || p.residual || p.drop.state || p.act > ABT_ACT_RELU);

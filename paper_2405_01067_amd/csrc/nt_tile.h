@@ -23,16 +23,19 @@ struct Tile {
 
 struct Order { int row_tiles, col_tiles; };
 
-// Tiles in panels of four row tiles, down the panel first; each XCD gets a contiguous eighth: the tiles that run at the same time on one
-// XCD share rows of X and rows of W in its L2.
-__device__ __forceinline__ void tile_of(const Order& o, int block, int& rt, int& ct) {
-    const int nb = o.row_tiles * o.col_tiles, xcd = block & 7, i = block >> 3, per = nb >> 3, rem = nb & 7;
-    const int w = xcd * per + (xcd < rem ? xcd : rem) + i;
+// Work-groups go round the XCDs: of `n` each XCD gets a contiguous eighth of what they stand for.
+__device__ __forceinline__ int xcd_order(int block, int n) {
+    const int xcd = block & 7, per = n >> 3, rem = n & 7;
+    return xcd * per + (xcd < rem ? xcd : rem) + (block >> 3);
+}
+// Tiles in panels of four row tiles, down the panel first: the tiles that run at the same time on one XCD share rows of X and rows of W in its L2.
+__device__ __forceinline__ void tile_at(const Order& o, int w, int& rt, int& ct) {
     const int panel = w / (4 * o.col_tiles), rows = o.row_tiles - 4 * panel < 4 ? o.row_tiles - 4 * panel : 4;
     const int at = w - panel * 4 * o.col_tiles;
     rt = 4 * panel + at % rows;
     ct = at / rows;
 }
+__device__ __forceinline__ void tile_of(const Order& o, int block, int& rt, int& ct) { tile_at(o, xcd_order(block, o.row_tiles * o.col_tiles), rt, ct); }
 
 }  // namespace
 }  // namespace abt
