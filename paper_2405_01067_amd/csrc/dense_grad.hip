@@ -433,20 +433,12 @@ hipError_t launch_dense_bwd(const DenseProduct& x, const DenseGrads& g, hipStrea
     // Together: the longest work-group, or what all of them keep the chip busy; apart: one after the other.  Of 56 shapes (8 to 4000 rows) what this takes is 0.5 % slower than
     // the other on average (33 % at worst).  us, together / apart: 394 rows, 768 x 768, three values 9.4 / 17.5; 1000 rows, 2304 x 768 26.8 / 38.2; 1500 rows, 512 x 512 24.3 / 18.8;
     // 4000 rows, 256 x 256, two values 54.6 / 15.4.
-    float longest = 0.0f, load = 0.0f, apart = -1.7f;
-    if (x.Y) {
-        const SmallCost c = dense_small_cost(x.M, x.Q, x.K);
-        longest = c.longest, load = c.load;
-        apart += dense_cost(x.M, x.Q, x.K) + 1.7f;
-    }
-    if (g.dW) {
-        const GradOrder o = grad_order(64, g.M, g.m, g.n, 1);
-        const float c = grad_cost(kGrads[2], o, g.m, g.n, values);
-        longest = c > longest ? c : longest;
-        load += (float)o.tiles / 256.0f * ((float)o.slabs * (kGrads[2].slab + (float)values * kGrads[2].value) + kGrads[2].rest);
-        apart += w.cost + 1.7f;
-    }
-    if (g.dbias) apart += 1.7f;
+    // (As if all three were wanted: what is not changes no sums.)
+    const SmallCost c = dense_small_cost(x.M, x.Q, x.K);
+    const GradOrder o = grad_order(64, g.M, g.m, g.n, 1);
+    const float dw = grad_cost(kGrads[2], o, g.m, g.n, values), longest = c.longest > dw ? c.longest : dw;
+    const float load = c.load + (float)o.tiles / 256.0f * ((float)o.slabs * (kGrads[2].slab + (float)values * kGrads[2].value) + kGrads[2].rest);
+    const float apart = dense_cost(x.M, x.Q, x.K) + w.cost + 1.7f;
     if (longest < apart && 0.9f * load < apart) return values == 3 ? launch_few_rows<3>(x, g, s) : values == 2 ? launch_few_rows<2>(x, g, s) : launch_few_rows<1>(x, g, s);
 
     hipError_t e = x.Y ? launch_dense(x, s) : hipSuccess;

@@ -23,22 +23,24 @@ __device__ __forceinline__ float lanes_sum(float v, int from, int to) {      // 
     return v;
 }
 
-// The sums of each channel of the slab over all threads, in chan[q pitch ..]: lanes with the same channels first, then the waves.  `waves` holds K pitch values
-// for each wave.
-template <int THREADS, int K>
-__device__ __forceinline__ void channel_sums(float (&v)[K][8], int shift, int width, int pitch, float* waves, float* chan) {
+// The sums of each unit of the slab over all threads, in chan[q pitch ..]: a thread has U units, of its eight channels or of eight / U of them added up; lanes with the same ones
+// first, then the waves.  `waves` holds K pitch values for each wave.
+template <int THREADS, int K, int U>
+__device__ __forceinline__ void channel_sums(float (&v)[K][U], int shift, int units, int pitch, float* waves, float* chan) {
     constexpr int NW = THREADS / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tc = lane & ((1 << shift) - 1);
+    for (int d = 1 << shift; d < 64; d <<= 1)
 #pragma unroll
-    for (int q = 0; q < K; ++q) {
+        for (int q = 0; q < K; ++q)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[q][k] = lanes_sum(v[q][k], 1 << shift, 64);
-        if (lane == tc && 8 * tc < width)
+            for (int k = 0; k < U; ++k) v[q][k] += __shfl_xor(v[q][k], d);
+    if (lane == tc && U * tc < units)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) waves[(q * NW + wave) * pitch + 8 * tc + k] = v[q][k];
-    }
+        for (int q = 0; q < K; ++q)
+#pragma unroll
+            for (int k = 0; k < U; ++k) waves[(q * NW + wave) * pitch + U * tc + k] = v[q][k];
     __syncthreads();
-    for (int c = threadIdx.x; c < width; c += THREADS)
+    for (int c = threadIdx.x; c < units; c += THREADS)
 #pragma unroll
         for (int q = 0; q < K; ++q) {
             float s = waves[q * NW * pitch + c];
@@ -52,14 +54,13 @@ __device__ __forceinline__ void channel_sums(float (&v)[K][8], int shift, int wi
 // f(group, lane of `lanes`, lanes): the work-group's threads in teams of a power of two of up to 64, a team for a group
 template <int THREADS, class F>
 __device__ __forceinline__ void by_group(int groups, int entries, F&& f) {
-    int lanes = 1;
-    while (lanes < entries && lanes < 64) lanes <<= 1;
-    for (int g = threadIdx.x / lanes; g < groups; g += THREADS / lanes) f(g, (int)threadIdx.x & (lanes - 1), lanes);
+    const int ls = entries <= 1 ? 0 : entries > 32 ? 6 : 32 - __builtin_clz(entries - 1);
+    for (int g = threadIdx.x >> ls; g < groups; g += THREADS >> ls) f(g, (int)threadIdx.x & ((1 << ls) - 1), 1 << ls);
 }
 
 // ------------------------------------------------------------------------------------------ everything at once
-// Pixel r of NV: row + r step, where row = thread / TC
-template <bool BF16, int THREADS, int NV>
+// Pixel r of NV: row + r step, where row = thread / TC.  U: units of a thread's eight channels; a group is a whole number of units.
+template <bool BF16, int THREADS, int NV, int U>
 __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g, const Split sp) {
     extern __shared__ float lds[];
     const int pitch = sp.width;
@@ -69,19 +70,22 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
     const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
     const bool there = 8 * tc < width;
     const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
-    const int cpg = g.C / g.groups, groups = width / cpg;
-    const float n = (float)g.pixels * (float)cpg;
     Raw8<BF16> x[NV];
 #pragma unroll
     for (int r = 0; r < NV; ++r)
         if (there && row + r * step < g.pixels) x[r] = raw8<BF16>(g.X, base + (int64_t)(row + r * step) * g.C);
     float gain[8], shift[8];
     if (there) load8<false>(g.gain, c0 + 8 * tc, gain), load8<false>(g.shift, c0 + 8 * tc, shift);
-    float sum[1][8], mean[8], rstd[8];
+    const int cpg = g.C / g.groups, groups = width / cpg, upg = cpg * U / 8;         // units of a group
+    const float inv = 1.0f / ((float)g.pixels * (float)cpg);
+    int mine[U];                                          // the groups of this thread's units
+#pragma unroll
+    for (int k = 0; k < U; ++k) mine[k] = (U * tc + k) / upg;
+    float sum[1][U], mean[U], rstd[U];
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {                // the mean, then the squares around it
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum[0][k] = 0.0f;
+        for (int k = 0; k < U; ++k) sum[0][k] = 0.0f;
 #pragma unroll
         for (int r = 0; r < NV; ++r)
             if (there && row + r * step < g.pixels) {
@@ -89,18 +93,17 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
                 values<BF16>(x[r], v);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float d = pass ? v[k] - mean[k] : v[k];
-                    sum[0][k] += pass ? d * d : d;
+                    const float d = pass ? v[k] - mean[k * U / 8] : v[k];
+                    sum[0][k * U / 8] += pass ? d * d : d;
                 }
             }
-        channel_sums<THREADS, 1>(sum, sp.shift, width, pitch, waves, chan);
-        by_group<THREADS>(groups, cpg, [&](int q, int l, int lanes) {
+        channel_sums<THREADS, 1, U>(sum, sp.shift, width / 8 * U, pitch, waves, chan);
+        by_group<THREADS>(groups, upg, [&](int q, int l, int lanes) {
             float s = 0.0f;
-            if (q < groups)
-                for (int c = l; c < cpg; c += lanes) s += chan[q * cpg + c];
+            for (int c = l; c < upg; c += lanes) s += chan[q * upg + c];
             s = lanes_sum(s, 1, lanes);
             if (l) return;
-            s /= n;
+            s *= inv;
             if (pass) s = 1.0f / __builtin_sqrtf(s + g.eps);
             stat[pass * pitch + q] = s;
             gstore((pass ? g.rstd : g.mean) + image * g.groups + c0 / cpg + q, s);
@@ -108,11 +111,11 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
         __syncthreads();
         if (there)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) (pass ? rstd : mean)[k] = stat[pass * pitch + (8 * tc + k) / cpg];
+            for (int k = 0; k < U; ++k) (pass ? rstd : mean)[k] = stat[pass * pitch + mine[k]];
     }
     if (!there) return;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) gain[k] *= rstd[k];
+    for (int k = 0; k < 8; ++k) gain[k] *= rstd[k * U / 8];
     with_activation(g.act, [&](auto act) {
 #pragma unroll
         for (int r = 0; r < NV; ++r)
@@ -120,7 +123,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
                 float v[8];
                 values<BF16>(x[r], v);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>((v[k] - mean[k]) * gain[k] + shift[k]);
+                for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>((v[k] - mean[k * U / 8]) * gain[k] + shift[k]);
                 store8<BF16>(g.Y, base + (int64_t)(row + r * step) * g.C, v);
             }
     });
@@ -173,7 +176,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
                 }
             }
     });
-    channel_sums<THREADS, 2>(sum, sp.shift, width, pitch, waves, chan);
+    channel_sums<THREADS, 2, 8>(sum, sp.shift, width, pitch, waves, chan);
     if (g.sums)
         for (int c = threadIdx.x; c < width; c += THREADS)
 #pragma unroll
@@ -230,6 +233,29 @@ __device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, i
     return p;
 }
 
+// f(row, X, dY) for this thread's rows of the piece, four rows on their way at a time
+template <bool BF16, bool BOTH, class F>
+__device__ __forceinline__ void by_rows(const GroupNorm& g, const Piece& p, F&& f) {
+    constexpr int B = BF16 ? 4 : 2;
+    for (int r = p.first; r < p.last; r += B * p.step) {
+        Raw8<BF16> x[B], dy[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int64_t at = p.base + (int64_t)(r + i * p.step < p.last ? r + i * p.step : r) * g.C;
+            x[i] = raw8<BF16>(g.X, at);
+            if (BOTH) dy[i] = raw8<BF16>(g.dY, at);
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (r + i * p.step >= p.last) break;
+            float v[8], d[8];
+            values<BF16>(x[i], v);
+            if (BOTH) values<BF16>(dy[i], d);
+            f(r + i * p.step, v, d);
+        }
+    }
+}
+
 // sums [2, N pieces, C]: the mean of a piece's pixels in a channel, and the squares around it
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const Split sp) {
@@ -241,9 +267,7 @@ __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const
     for (int k = 0; k < 8; ++k) mean[k] = square[k] = 0.0f;
     float count = 0.0f;
     if (p.there)
-        for (int r = p.first; r < p.last; r += p.step) {  // each thread's own mean and squares (Welford)
-            float v[8];
-            load8<BF16>(g.X, p.base + (int64_t)r * g.C, v);
+        by_rows<BF16, false>(g, p, [&](int, const float (&v)[8], const float (&)[8]) {           // each thread's own mean and squares (Welford)
             count += 1.0f;
             const float part = 1.0f / count;
 #pragma unroll
@@ -252,10 +276,10 @@ __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const
                 mean[k] += d * part;
                 square[k] += d * (v[k] - mean[k]);
             }
-        }
+        });
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[0][k] = mean[k] * count;
-    channel_sums<256, 1>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    channel_sums<256, 1, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
     float all[8];
     if (p.there)
 #pragma unroll
@@ -266,7 +290,7 @@ __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[0][k] = p.there ? square[k] + count * (mean[k] - all[k]) * (mean[k] - all[k]) : 0.0f;
     __syncthreads();
-    channel_sums<256, 1>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    channel_sums<256, 1, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
     if (writes) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) all[k] = chan[8 * p.tc + k];
@@ -318,14 +342,12 @@ __global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const 
         gain[k] *= stat[1][q];
     }
     with_activation(g.act, [&](auto act) {
-        for (int r = p.first; r < p.last; r += p.step) {
-            const int64_t at = p.base + (int64_t)r * g.C;
-            float v[8];
-            load8<BF16>(g.X, at, v);
+        by_rows<BF16, false>(g, p, [&](int r, const float (&v)[8], const float (&)[8]) {
+            float y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>((v[k] - mean[k]) * gain[k] + shift[k]);
-            store8<BF16>(g.Y, at, v);
-        }
+            for (int k = 0; k < 8; ++k) y[k] = activate<decltype(act)::value>((v[k] - mean[k]) * gain[k] + shift[k]);
+            store8<BF16>(g.Y, p.base + (int64_t)r * g.C, y);
+        });
     });
 }
 
@@ -351,20 +373,18 @@ __global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, c
         float gain[8], shift[8], mean[8], rstd[8];
         load_stats(g, p, cpg, gain, shift, mean, rstd);
         with_activation(g.act, [&](auto act) {
-            for (int r = p.first; r < p.last; r += p.step) {
-                float v[8], d[8];
-                load8<BF16>(g.X, p.base + (int64_t)r * g.C, v), load8<BF16>(g.dY, p.base + (int64_t)r * g.C, d);
+            by_rows<BF16, true>(g, p, [&](int, const float (&x)[8], const float (&dy)[8]) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    v[k] = (v[k] - mean[k]) * rstd[k];
-                    if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
-                    sum[0][k] += d[k];
-                    sum[1][k] += d[k] * v[k];
+                    const float v = (x[k] - mean[k]) * rstd[k];
+                    const float d = decltype(act)::value != ABT_ACT_NONE ? dy[k] * slope<decltype(act)::value>(v * gain[k] + shift[k]) : dy[k];
+                    sum[0][k] += d;
+                    sum[1][k] += d * v;
                 }
-            }
+            });
         });
     }
-    channel_sums<256, 2>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    channel_sums<256, 2, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
     for (int c = threadIdx.x; c < p.width; c += 256)
 #pragma unroll
         for (int q = 0; q < 2; ++q) gstore(g.sums + ((q * g.N + p.image) * sp.pieces + p.piece) * g.C + p.c0 + c, chan[q * kMaxSlab + c]);
@@ -433,18 +453,16 @@ __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, co
         a[k] = stat[0][q], b[k] = stat[1][q];
     }
     with_activation(g.act, [&](auto act) {
-        for (int r = p.first; r < p.last; r += p.step) {
-            const int64_t at = p.base + (int64_t)r * g.C;
-            float v[8], d[8];
-            load8<BF16>(g.X, at, v), load8<BF16>(g.dY, at, d);
+        by_rows<BF16, true>(g, p, [&](int r, const float (&x)[8], const float (&dy)[8]) {
+            float y[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                v[k] = (v[k] - mean[k]) * rstd[k];
-                if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
-                v[k] = rstd[k] * (d[k] * gain[k] - a[k] - v[k] * b[k]);
+                const float v = (x[k] - mean[k]) * rstd[k];
+                const float d = decltype(act)::value != ABT_ACT_NONE ? dy[k] * slope<decltype(act)::value>(v * gain[k] + shift[k]) : dy[k];
+                y[k] = rstd[k] * (d * gain[k] - a[k] - v * b[k]);
             }
-            store8<BF16>(g.Y, at, v);
-        }
+            store8<BF16>(g.Y, p.base + (int64_t)r * g.C, y);
+        });
     });
 }
 
@@ -494,8 +512,12 @@ hipError_t launch_whole(const GroupNorm& g, const Split& sp, hipStream_t s) {
     const int64_t blocks = g.N * sp.slabs;
     if (blocks > INT_MAX) return hipErrorInvalidValue;
     const unsigned lds = (unsigned)(((BWD ? 2 : 1) * (THREADS / 64 + 1) + 2) * sp.width * 4);      // 72 KB at most
-    if constexpr (BWD) hipLaunchKernelGGL((gn_whole_bwd_kernel<BF16, THREADS, NV>), dim3((unsigned)blocks), dim3(THREADS), lds, s, g, sp);
-    else hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV>), dim3((unsigned)blocks), dim3(THREADS), lds, s, g, sp);
+    const dim3 grid((unsigned)blocks);
+    const int cpg = g.C / g.groups;
+    if constexpr (BWD) hipLaunchKernelGGL((gn_whole_bwd_kernel<BF16, THREADS, NV>), grid, dim3(THREADS), lds, s, g, sp);
+    else if (cpg % 8 == 0) hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 1>), grid, dim3(THREADS), lds, s, g, sp);
+    else if (cpg % 4 == 0) hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 2>), grid, dim3(THREADS), lds, s, g, sp);
+    else hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 8>), grid, dim3(THREADS), lds, s, g, sp);
     return hipGetLastError();
 }
 template <bool BF16, bool BWD, int THREADS>
@@ -515,39 +537,41 @@ hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
 }
 
 template <bool BF16>
-hipError_t fwd(const GroupNorm& g, hipStream_t s) {
-    const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, false);
-    if (p.threads) return launch_whole<BF16, false>(g, p, s);
-    const int64_t blocks = g.N * p.sp.slabs * p.sp.pieces;
+hipError_t pieces_fwd(const GroupNorm& g, const Split& sp, hipStream_t s) {
+    const int64_t blocks = g.N * sp.slabs * sp.pieces;
     if (blocks > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gn_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, p.sp);
+    hipLaunchKernelGGL((gn_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gn_apply_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, p.sp);
+    hipLaunchKernelGGL((gn_apply_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
     return hipGetLastError();
+}
+template <bool BF16>
+hipError_t pieces_bwd(const GroupNorm& g, const Split& sp, hipStream_t s) {
+    const int64_t blocks = g.N * sp.slabs * sp.pieces, sums = g.dgain || g.dshift ? ceil_div(g.C, 32) : 0, apply = g.Y ? blocks : 0;
+    if (blocks + sums > INT_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || apply + sums == 0) return e;
+    hipLaunchKernelGGL((gn_bwd_apply_kernel<BF16>), dim3((unsigned)(apply + sums)), dim3(256), 0, s, g, sp, apply);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t fwd(const GroupNorm& g, hipStream_t s) {
+    const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, false);
+    return p.threads ? launch_whole<BF16, false>(g, p, s) : pieces_fwd<BF16>(g, p.sp, s);
 }
 template <bool BF16>
 hipError_t bwd(const GroupNorm& g, hipStream_t s) {
     const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, true);
+    if (!p.threads) return pieces_bwd<BF16>(g, p.sp, s);
     const bool channels = g.dgain || g.dshift;
-    const int64_t sums = channels ? ceil_div(g.C, 32) : 0;
-    hipError_t e;
-    if (p.threads) {
-        GroupNorm q = g;
-        if (!channels) q.sums = nullptr;
-        e = launch_whole<BF16, true>(q, p, s);
-        if (e != hipSuccess || !channels) return e;
-        hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)sums), dim3(256), 0, s, g, g.N);
-        return hipGetLastError();
-    }
-    const int64_t blocks = g.N * p.sp.slabs * p.sp.pieces;
-    if (blocks + sums > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, p.sp);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t apply = g.Y ? blocks : 0;
-    if (apply + sums == 0) return hipSuccess;
-    hipLaunchKernelGGL((gn_bwd_apply_kernel<BF16>), dim3((unsigned)(apply + sums)), dim3(256), 0, s, g, p.sp, apply);
+    GroupNorm q = g;
+    if (!channels) q.sums = nullptr;
+    const hipError_t e = launch_whole<BF16, true>(q, p, s);
+    if (e != hipSuccess || !channels) return e;
+    hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)ceil_div(g.C, 32)), dim3(256), 0, s, g, g.N);
     return hipGetLastError();
 }
 
