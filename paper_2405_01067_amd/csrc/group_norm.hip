@@ -141,7 +141,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
     const bool there = 8 * tc < width;
     const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
     const int cpg = g.C / g.groups, groups = width / cpg;
-    const float n = (float)g.pixels * (float)cpg;
+    const float inv = 1.0f / ((float)g.pixels * (float)cpg);
     Raw8<BF16> x[NV], dy[NV];
 #pragma unroll
     for (int r = 0; r < NV; ++r)
@@ -177,10 +177,14 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
             }
     });
     channel_sums<THREADS, 2, 8>(sum, sp.shift, width, pitch, waves, chan);
-    if (g.sums)
-        for (int c = threadIdx.x; c < width; c += THREADS)
+    for (int c = threadIdx.x; c < width; c += THREADS)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) gstore(g.sums + (q * g.N + image) * g.C + c0 + c, chan[q * pitch + c]);
+        for (int q = 0; q < 2; ++q) {
+            const float s = chan[q * pitch + c];
+            float* const out = q ? g.dgain : g.dshift;
+            if (g.N > 1) gstore(g.sums + (q * g.N + image) * g.C + c0 + c, s);
+            else if (out) gstore(out + c0 + c, g.accumulate ? gload(out + c0 + c) + s : s);      // one image: these are the gradients
+        }
     if (!g.Y) return;
     by_group<THREADS>(groups, cpg, [&](int q, int l, int lanes) {
         float s = 0.0f, t = 0.0f;
@@ -190,7 +194,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
                 t += chan[pitch + q * cpg + c] * w;
             }
         s = lanes_sum(s, 1, lanes), t = lanes_sum(t, 1, lanes);
-        if (l == 0) stat[q] = s / n, stat[pitch + q] = t / n;
+        if (l == 0) stat[q] = s * inv, stat[pitch + q] = t * inv;
     });
     __syncthreads();
     if (!there) return;
@@ -256,12 +260,26 @@ __device__ __forceinline__ void by_rows(const GroupNorm& g, const Piece& p, F&& 
     }
 }
 
-// sums [2, N pieces, C]: the mean of a piece's pixels in a channel, and the squares around it
+// The groups of a slab, of which the first and the last may reach into others.  A group q has a partial of its own in each slab s that it touches, at slot q + s of groups + slabs:
+// from one partial to the next either number grows by one, so no two share a slot.
+struct SlabGroups { int cpg, first, count; };
+__device__ __forceinline__ SlabGroups groups_of(const GroupNorm& g, const Piece& p) {
+    const int cpg = g.C / g.groups, first = p.c0 / cpg;
+    return SlabGroups{cpg, first, (p.c0 + p.width - 1) / cpg - first + 1};
+}
+__device__ __forceinline__ int slots(const GroupNorm& g, const Split& sp) { return g.groups + sp.slabs; }
+// where the slots of an image's piece begin
+__device__ __forceinline__ const float* slots_of(const float* sums, const GroupNorm& g, const Split& sp, int64_t image, int piece) {
+    return sums + (image * sp.pieces + piece) * slots(g, sp) * 2;
+}
+
+// per slot: the mean of a piece's pixels in the group's channels in this slab, and the squares around it
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const Split sp) {
-    __shared__ float waves[4 * kMaxSlab], chan[kMaxSlab];
+    __shared__ float waves[4 * kMaxSlab], chan[kMaxSlab], means[kMaxSlab];
     const Piece p = piece_of(g, sp, blockIdx.x);
-    const int n = p.last - p.piece * sp.rows;
+    const SlabGroups sg = groups_of(g, p);
+    const float inv = 1.0f / (float)(p.last - p.piece * sp.rows);
     float mean[8], square[8], sum[1][8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) mean[k] = square[k] = 0.0f;
@@ -280,56 +298,69 @@ __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[0][k] = mean[k] * count;
     channel_sums<256, 1, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
-    float all[8];
-    if (p.there)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) all[k] = chan[8 * p.tc + k] / (float)n;
-    const int64_t at = (p.image * sp.pieces + p.piece) * g.C + p.c0 + 8 * p.tc;
-    const bool writes = p.there && threadIdx.x < (1u << sp.shift);
-    if (writes) store8<false>(g.sums, at, all);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum[0][k] = p.there ? square[k] + count * (mean[k] - all[k]) * (mean[k] - all[k]) : 0.0f;
+    // what the group has of this slab
+    auto begin = [&](int q) { return q * sg.cpg > p.c0 ? q * sg.cpg - p.c0 : 0; };
+    auto end = [&](int q) { return (q + 1) * sg.cpg < p.c0 + p.width ? (q + 1) * sg.cpg - p.c0 : p.width; };
+    float* const out = const_cast<float*>(slots_of(g.sums, g, sp, p.image, p.piece)) + 2 * (sg.first + p.c0 / sp.width);
+    by_group<256>(sg.count, sg.cpg < p.width ? sg.cpg : p.width, [&](int q, int l, int lanes) {
+        const int b = begin(sg.first + q), e = end(sg.first + q);
+        float s = 0.0f;
+        for (int c = b + l; c < e; c += lanes) s += chan[c];
+        s = lanes_sum(s, 1, lanes) * inv / (float)(e - b);
+        if (l) return;
+        means[q] = s;
+        gstore(out + 2 * q, s);
+    });
     __syncthreads();
-    channel_sums<256, 1, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
-    if (writes) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) all[k] = chan[8 * p.tc + k];
-        store8<false>(g.sums, g.N * sp.pieces * g.C + at, all);
+    for (int k = 0; k < 8; ++k) {
+        const float d = p.there ? mean[k] - means[(p.c0 + 8 * p.tc + k) / sg.cpg - sg.first] : 0.0f;
+        sum[0][k] = square[k] + count * d * d;
     }
+    channel_sums<256, 1, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
+    by_group<256>(sg.count, sg.cpg < p.width ? sg.cpg : p.width, [&](int q, int l, int lanes) {
+        const int b = begin(sg.first + q), e = end(sg.first + q);
+        float s = 0.0f;
+        for (int c = b + l; c < e; c += lanes) s += chan[c];
+        s = lanes_sum(s, 1, lanes);
+        if (l == 0) gstore(out + 2 * q + 1, s);
+    });
 }
+
+// f(slab, piece) for this lane's share of the partials of group q
+template <class F>
+__device__ __forceinline__ void by_partial(const SlabGroups& sg, const Split& sp, int q, int l, int lanes, F&& f) {
+    const int s0 = q * sg.cpg / sp.width, s1 = ((q + 1) * sg.cpg - 1) / sp.width, touched = s1 - s0 + 1;
+    for (int e = l; e < sp.pieces * touched; e += lanes) f(s0 + e % touched, e / touched);
+}
+__device__ __forceinline__ int partials(const SlabGroups& sg, const Split& sp) { return sp.pieces * ((sg.cpg + sp.width - 2) / sp.width + 1); }      // at most
 
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const Split sp) {
     __shared__ float stat[2][kMaxSlab];
     const Piece p = piece_of(g, sp, blockIdx.x);
-    const int cpg = g.C / g.groups, g0 = p.c0 / cpg, groups = (p.c0 + p.width - 1) / cpg - g0 + 1;
-    const float* const means = g.sums + p.image * sp.pieces * g.C;
-    const float* const squares = means + g.N * sp.pieces * g.C;
-    const int entries = cpg * sp.pieces;
-    by_group<256>(groups, entries, [&](int q, int l, int lanes) {
-        const int c = (g0 + q) * cpg;
-        float s = 0.0f, t = 0.0f;
-        const auto of = [&](int e, int& n) {              // an entry's place, and its pixels
-            const int piece = e / cpg;
-            n = g.pixels - piece * sp.rows < sp.rows ? g.pixels - piece * sp.rows : sp.rows;
-            return (int64_t)piece * g.C + c + e % cpg;
+    const SlabGroups sg = groups_of(g, p);
+    const float inv = 1.0f / ((float)g.pixels * (float)sg.cpg);
+    by_group<256>(sg.count, partials(sg, sp), [&](int i, int l, int lanes) {
+        const int q = sg.first + i;
+        auto weight = [&](int slab, int piece) {          // values behind a partial
+            const int c0 = slab * sp.width, b = q * sg.cpg > c0 ? q * sg.cpg : c0, e = (q + 1) * sg.cpg < c0 + sp.width ? (q + 1) * sg.cpg : c0 + sp.width;
+            const int left = g.pixels - piece * sp.rows;
+            return (float)(e - b) * (float)(left < sp.rows ? left : sp.rows);
         };
-        int n;
-        for (int e = l; e < entries; e += lanes) {
-                const int64_t at = of(e, n);
-                s += gload(means + at) * (float)n;
-            }
-        const float mean = lanes_sum(s, 1, lanes) / ((float)g.pixels * (float)cpg);
-        for (int e = l; e < entries; e += lanes) {
-                const int64_t at = of(e, n);
-                const float d = gload(means + at) - mean;
-                t += gload(squares + at) + (float)n * d * d;
-            }
-        t = lanes_sum(t, 1, lanes) / ((float)g.pixels * (float)cpg);
+        float s = 0.0f, t = 0.0f;
+        by_partial(sg, sp, q, l, lanes, [&](int slab, int piece) { s += gload(slots_of(g.sums, g, sp, p.image, piece) + 2 * (q + slab)) * weight(slab, piece); });
+        const float mean = lanes_sum(s, 1, lanes) * inv;
+        by_partial(sg, sp, q, l, lanes, [&](int slab, int piece) {
+            const float* const at = slots_of(g.sums, g, sp, p.image, piece) + 2 * (q + slab);
+            const float d = gload(at) - mean;
+            t += gload(at + 1) + weight(slab, piece) * d * d;
+        });
+        t = lanes_sum(t, 1, lanes) * inv;
         if (l) return;
         const float rstd = 1.0f / __builtin_sqrtf(t + g.eps);
-        stat[0][q] = mean, stat[1][q] = rstd;
-        if (p.piece == 0 && c >= p.c0) gstore(g.mean + p.image * g.groups + g0 + q, mean), gstore(g.rstd + p.image * g.groups + g0 + q, rstd);
+        stat[0][i] = mean, stat[1][i] = rstd;
+        if (p.piece == 0 && q * sg.cpg >= p.c0) gstore(g.mean + p.image * g.groups + q, mean), gstore(g.rstd + p.image * g.groups + q, rstd);
     });
     __syncthreads();
     if (!p.there) return;
@@ -337,7 +368,7 @@ __global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const 
     load8<false>(g.gain, p.c0 + 8 * p.tc, gain), load8<false>(g.shift, p.c0 + 8 * p.tc, shift);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int q = (p.c0 + 8 * p.tc + k) / cpg - g0;
+        const int q = (p.c0 + 8 * p.tc + k) / sg.cpg - sg.first;
         mean[k] = stat[0][q];
         gain[k] *= stat[1][q];
     }
@@ -360,7 +391,8 @@ __device__ __forceinline__ void load_stats(const GroupNorm& g, const Piece& p, i
     }
 }
 
-// sums [2, N pieces, C] of dpre and of dpre x^
+// sums [2, N pieces, C] of dpre and of dpre x^, and behind them per slot the same times the gain, over the group's channels in this slab
+__device__ __forceinline__ float* slot_base(const GroupNorm& g, const Split& sp) { return g.sums + 2 * g.N * sp.pieces * g.C; }
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, const Split sp) {
     __shared__ float waves[8 * kMaxSlab], chan[2 * kMaxSlab];
@@ -388,60 +420,65 @@ __global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, c
     for (int c = threadIdx.x; c < p.width; c += 256)
 #pragma unroll
         for (int q = 0; q < 2; ++q) gstore(g.sums + ((q * g.N + p.image) * sp.pieces + p.piece) * g.C + p.c0 + c, chan[q * kMaxSlab + c]);
+    const SlabGroups sg = groups_of(g, p);
+    float* const out = const_cast<float*>(slots_of(slot_base(g, sp), g, sp, p.image, p.piece)) + 2 * (sg.first + p.c0 / sp.width);
+    by_group<256>(sg.count, cpg < p.width ? cpg : p.width, [&](int i, int l, int lanes) {
+        const int q = sg.first + i, b = q * cpg > p.c0 ? q * cpg - p.c0 : 0, e = (q + 1) * cpg < p.c0 + p.width ? (q + 1) * cpg - p.c0 : p.width;
+        float s = 0.0f, t = 0.0f;
+        for (int c = b + l; c < e; c += lanes) {
+            const float w = gload(g.gain + p.c0 + c);
+            s += chan[c] * w;
+            t += chan[kMaxSlab + c] * w;
+        }
+        s = lanes_sum(s, 1, lanes), t = lanes_sum(t, 1, lanes);
+        if (l == 0) gstore(out + 2 * i, s), gstore(out + 2 * i + 1, t);
+    });
 }
 
-// dshift, dgain of 32 channels from `rows` rows of sums of each
-__device__ __forceinline__ void channel_gradients(const GroupNorm& g, int64_t rows, int block, float (*lds)[32]) {
-    const int c = block * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+// dshift (block even) or dgain of eight channels from `rows` rows of sums
+__device__ __forceinline__ void channel_gradients(const GroupNorm& g, int64_t rows, int block, float (*lds)[8]) {
+    float* const out = block & 1 ? g.dgain : g.dshift;
+    if (!out) return;
+    const int c = block / 2 * 8 + (threadIdx.x & 7), part = threadIdx.x >> 3;
+    const float* const from = g.sums + (block & 1) * rows * g.C + c;          // (C is a multiple of eight)
+    float s = 0.0f;
+    int64_t r = part;
+    for (; r + 224 < rows; r += 256) {                    // eight loads on their way at a time
+        float v[8];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        float s = 0.0f;
-        if (c < g.C) {
-            const float* const from = g.sums + q * rows * g.C + c;
-            int64_t r = part;
-            for (; r + 56 < rows; r += 64) {              // eight loads on their way at a time
-                float v[8];
+        for (int k = 0; k < 8; ++k) v[k] = gload(from + (r + 32 * k) * g.C);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = gload(from + (r + 8 * k) * g.C);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) s += v[k];
-            }
-            for (; r < rows; r += 8) s += gload(from + r * g.C);
-        }
-        __syncthreads();
-        lds[part][threadIdx.x & 31] = s;
-        __syncthreads();
-        float* const out = q ? g.dgain : g.dshift;
-        if (part || c >= g.C || !out) continue;
-        for (int k = 1; k < 8; ++k) s += lds[k][threadIdx.x];
-        gstore(out + c, g.accumulate ? gload(out + c) + s : s);
+        for (int k = 0; k < 8; ++k) s += v[k];
     }
+    for (; r < rows; r += 32) s += gload(from + r * g.C);
+    lds[part][threadIdx.x & 7] = s;
+    __syncthreads();
+    if (part) return;
+    for (int k = 1; k < 32; ++k) s += lds[k][threadIdx.x];
+    gstore(out + c, g.accumulate ? gload(out + c) + s : s);
 }
 
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, const Split sp, int64_t blocks) {
     __shared__ float stat[2][kMaxSlab];
     if (blockIdx.x >= blocks) {
-        channel_gradients(g, g.N * sp.pieces, (int)(blockIdx.x - blocks), reinterpret_cast<float (*)[32]>(&stat[0][0]));
+        channel_gradients(g, g.N * sp.pieces, (int)(blockIdx.x - blocks), reinterpret_cast<float (*)[8]>(&stat[0][0]));
         return;
     }
     const Piece p = piece_of(g, sp, blockIdx.x);
-    const int cpg = g.C / g.groups, g0 = p.c0 / cpg, groups = (p.c0 + p.width - 1) / cpg - g0 + 1;
-    const float* const first = g.sums + p.image * sp.pieces * g.C;
-    const float* const second = first + g.N * sp.pieces * g.C;
-    const int entries = cpg * sp.pieces;
-    const float n = (float)g.pixels * (float)cpg;
-    by_group<256>(groups, entries, [&](int q, int l, int lanes) {
-        const int c = (g0 + q) * cpg;
+    const SlabGroups sg = groups_of(g, p);
+    const int cpg = sg.cpg;
+    const float inv = 1.0f / ((float)g.pixels * (float)cpg);
+    by_group<256>(sg.count, partials(sg, sp), [&](int i, int l, int lanes) {
+        const int q = sg.first + i;
         float s = 0.0f, t = 0.0f;
-        for (int e = l; e < entries; e += lanes) {
-                const int64_t at = (int64_t)(e / cpg) * g.C + c + e % cpg;
-                const float w = gload(g.gain + c + e % cpg);
-                s += gload(first + at) * w;
-                t += gload(second + at) * w;
-            }
+        by_partial(sg, sp, q, l, lanes, [&](int slab, int piece) {
+            const float* const at = slots_of(slot_base(g, sp), g, sp, p.image, piece) + 2 * (q + slab);
+            s += gload(at);
+            t += gload(at + 1);
+        });
         s = lanes_sum(s, 1, lanes), t = lanes_sum(t, 1, lanes);
-        if (l == 0) stat[0][q] = s / n, stat[1][q] = t / n;
+        if (l == 0) stat[0][i] = s * inv, stat[1][i] = t * inv;
     });
     __syncthreads();
     if (!p.there) return;
@@ -449,7 +486,7 @@ __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, co
     load_stats(g, p, cpg, gain, shift, mean, rstd);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int q = (p.c0 + 8 * p.tc + k) / cpg - g0;
+        const int q = (p.c0 + 8 * p.tc + k) / cpg - sg.first;
         a[k] = stat[0][q], b[k] = stat[1][q];
     }
     with_activation(g.act, [&](auto act) {
@@ -467,7 +504,7 @@ __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, co
 }
 
 __global__ __launch_bounds__(256) void gn_channels_kernel(const GroupNorm g, int64_t rows) {
-    __shared__ float lds[8][32];
+    __shared__ float lds[32][8];
     channel_gradients(g, rows, blockIdx.x, lds);
 }
 
@@ -476,32 +513,53 @@ int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 
 // How a call is split; threads, vectors: of the `whole` kernels, threads = 0 for the others
 struct Plan { Split sp; int threads, vectors; };
+int threads_across(int width) {                           // as a power of two's exponent
+    int shift = 0;
+    while ((8 << shift) < width) ++shift;
+    return shift;
+}
 Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
     Plan p{};
-    const int cpg = C / groups, unit = cpg / gcd(cpg, 8) * 8, line = bf16 ? 64 : 32;       // whole groups and vectors; 128 bytes
+    const int cpg = C / groups, unit = cpg / gcd(cpg, 8) * 8, wide = 64;      // whole groups and vectors; 128 bytes in bf16, 256 in fp32
+    const int most = (bf16 ? 16 : 8) / (backward ? 2 : 1);                    // vectors in a thread's registers
     if (unit <= kMaxSlab) {
-        int width = (line + unit - 1) / unit * unit;
-        if (width > kMaxSlab) width = unit;
-        if (width > C) width = C;
-        int shift = 0;
-        while ((8 << shift) < width) ++shift;
-        const int most = (bf16 ? 16 : 8) / (backward ? 2 : 1);                             // vectors in a thread's registers
-        for (int threads = 256; threads <= 1024; threads *= 2) {
-            const int vectors = (int)ceil_div(pixels, threads >> shift);
-            if (vectors > most && threads < 1024) continue;
-            if (vectors > most) break;
-            p.sp = Split{width, (int)ceil_div(C, width), shift, 1, pixels};
-            p.threads = threads;
-            p.vectors = vectors;
-            return p;
+        auto whole = [&](int width) {                     // a multiple of unit
+            const int shift = threads_across(width);
+            for (int few : {4, most})                     // four vectors a thread with as few threads as that takes, or as many as fit
+                for (int threads = 256; threads <= 1024; threads *= 2) {
+                    const int vectors = (int)ceil_div(pixels, threads >> shift);
+                    if (vectors > few || vectors > most) continue;
+                    p.sp = Split{width, (int)ceil_div(C, width), shift, 1, pixels};
+                    p.threads = threads;
+                    p.vectors = vectors;
+                    return true;
+                }
+            return false;
+        };
+        auto units = [&](int width) { return width < unit ? unit : width / unit * unit; };
+        // Two pixels a thread at least, with wider slabs; or enough work-groups for all compute units, with narrower ones.  us, 512 threads unless stated, width 64 / others:
+        // 256 x 196 x 256 13.0 / 14.0 (128), 17.1 (32); 1000 x 16 x 256 with 256 threads 10.9 / 6.5 (256); 4 x 784 x 128 11.5 / 7.8 (32), 6.1 (16), 5.9 (8).
+        int width = wide;
+        while (2 * (256 >> threads_across(width)) > pixels && width < 256 && N * ceil_div(C, 2 * width) >= 256) width *= 2;
+        while (width > 8 && N * ceil_div(C, width) < 256) width /= 2;
+        if (width > C) width = C / 8 * 8;
+        // half lines and less are read at half the rate and less, and a few work-groups of many pixels leave compute units idle: not where there is more than a few MB
+        const bool much = N * pixels * C * (bf16 ? 2 : 4) > (8 << 20);
+        for (; width >= 8; width /= 2) {
+            const int w = units(width);
+            if (much && (w * (bf16 ? 2 : 4) < 64 || N * ceil_div(C, w) < 256)) break;
+            if (whole(w)) return p;
+            if (w > width) break;
         }
+        p = Plan{};
     }
-    int shift = 0;
-    while ((8 << shift) < C && shift < 6) ++shift;
-    const int width = 8 << shift, slabs = (int)ceil_div(C, width), step = 256 >> shift;
-    // some 1024 work-groups, four pixels or more a thread
-    int64_t pieces = ceil_div(1024, N * slabs);
-    if (pieces > ceil_div(pixels, 4 * step)) pieces = ceil_div(pixels, 4 * step);
+    const int width = C < wide ? C : wide, shift = threads_across(width), slabs = (int)ceil_div(C, width), step = 256 >> shift;
+    // Some 512 work-groups, four pixels or more a thread; not more partials than a work-group reads in a few steps.  us, 512 / 1024 of them, forward and backward: 64 x 3136 x 64
+    // 22.7 / 26.9, 29.8 / 40.1; 8 x 1024 x 640 15.5 / 18.1; but 16 x 3136 x 256 22.0 / 21.4, 29.1 / 28.9.
+    int64_t pieces = ceil_div(512, N * slabs);
+    const int64_t rows4 = ceil_div(pixels, 4 * step), read = 8192 / (width / cpg + 2);
+    if (pieces > rows4) pieces = rows4;
+    if (pieces > read) pieces = read;
     const int rows = (int)ceil_div(pixels, pieces);
     p.sp = Split{width, slabs, shift, (int)ceil_div(pixels, rows), rows};
     return p;
@@ -548,7 +606,7 @@ hipError_t pieces_fwd(const GroupNorm& g, const Split& sp, hipStream_t s) {
 }
 template <bool BF16>
 hipError_t pieces_bwd(const GroupNorm& g, const Split& sp, hipStream_t s) {
-    const int64_t blocks = g.N * sp.slabs * sp.pieces, sums = g.dgain || g.dshift ? ceil_div(g.C, 32) : 0, apply = g.Y ? blocks : 0;
+    const int64_t blocks = g.N * sp.slabs * sp.pieces, sums = g.dgain || g.dshift ? g.C / 4 : 0, apply = g.Y ? blocks : 0;
     if (blocks + sums > INT_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
     const hipError_t e = hipGetLastError();
@@ -566,12 +624,9 @@ template <bool BF16>
 hipError_t bwd(const GroupNorm& g, hipStream_t s) {
     const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, true);
     if (!p.threads) return pieces_bwd<BF16>(g, p.sp, s);
-    const bool channels = g.dgain || g.dshift;
-    GroupNorm q = g;
-    if (!channels) q.sums = nullptr;
-    const hipError_t e = launch_whole<BF16, true>(q, p, s);
-    if (e != hipSuccess || !channels) return e;
-    hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)ceil_div(g.C, 32)), dim3(256), 0, s, g, g.N);
+    const hipError_t e = launch_whole<BF16, true>(g, p, s);
+    if (e != hipSuccess || g.N == 1 || (!g.dgain && !g.dshift)) return e;
+    hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)(g.C / 4)), dim3(256), 0, s, g, g.N);
     return hipGetLastError();
 }
 
@@ -579,8 +634,8 @@ hipError_t bwd(const GroupNorm& g, hipStream_t s) {
 
 size_t group_norm_sum_bytes(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
     const Plan p = plan_of(N, pixels, C, groups, bf16, backward);
-    if (p.threads && !backward) return 0;
-    return (size_t)N * (size_t)p.sp.pieces * (size_t)C * 8;
+    const size_t channels = backward ? (size_t)N * (size_t)p.sp.pieces * (size_t)C * 8 : 0;
+    return channels + (p.threads ? 0 : (size_t)N * (size_t)p.sp.pieces * (size_t)(groups + p.sp.slabs) * 8);
 }
 hipError_t launch_group_norm_fwd(const GroupNorm& p, bool bf16, hipStream_t s) { return bf16 ? fwd<true>(p, s) : fwd<false>(p, s); }
 hipError_t launch_group_norm_bwd(const GroupNorm& p, bool bf16, hipStream_t s) { return bf16 ? bwd<true>(p, s) : bwd<false>(p, s); }
