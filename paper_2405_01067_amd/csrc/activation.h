@@ -35,9 +35,8 @@ __device__ __forceinline__ float activate(float z) {
     if constexpr (ACT == ABT_ACT_SILU) return z * sigmoid(z);
     return z;
 }
-template <int ACT>
+template <int ACT>                                        // of the smooth ones
 __device__ __forceinline__ float slope(float z) {
-    if constexpr (ACT == ABT_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
     if constexpr (ACT == ABT_ACT_GELU) {
         float density;
         const float tail = normal_tail(z, density);
@@ -52,7 +51,14 @@ __device__ __forceinline__ float slope(float z) {
         const float s = sigmoid(z);
         return s + z * s * (1.0f - s);
     }
-    return 1.0f;
+}
+
+// the gradient d behind the activation, in front of it
+template <int ACT>
+__device__ __forceinline__ float through(float z, float d) {
+    if constexpr (ACT == ABT_ACT_NONE) return d;
+    if constexpr (ACT == ABT_ACT_RELU) return z > 0.0f ? d : 0.0f;
+    return d * slope<ACT>(z);
 }
 
 // f(std::integral_constant<int, ACT>) for the activation of a launch, which is the same for all its threads: one branch around what f does

@@ -28,9 +28,9 @@ SmallCost dense_small_cost(int64_t M, int Q, int K);
 hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);        // M <= 64
 
 // What the gradients are made of: dZ = slope(Z) drop(dY) [M, m] as the sum of one, two or three bf16 values.  Without an activation or with ABT_ACT_RELU one is
-// exact (dropout's factor is left to the products).  Otherwise two have 17 bits (1.3e-6 of the size on average) and three all of fp32: three where
-// dW's own sums, fp32 over M rows, are off by less than that.
-constexpr int kDenseThreeValues = 4096;        // rows
+// exact (dropout's factor is left to the products).  Otherwise three have all of fp32, and two are 2.4e-6 of the size off on average: two where sums of fp32 products over
+// that many rows, one after the other, are off by about as much (measured with the library's product in fp32: 1.2e-6 at 4200 rows, 1.7e-6 at 9216, 2.0e-6 at 12608).
+constexpr int kDenseThreeValues = 9216;        // rows
 // Beside it W^T, and sums of dZ over pieces of the rows.
 struct DenseSlope {
     const uint16_t* dY; const uint16_t* Z; // Z NULL without an activation

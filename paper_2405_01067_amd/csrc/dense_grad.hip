@@ -58,7 +58,7 @@ __device__ __forceinline__ void slope_piece(const DenseSlope& g, int piece, int 
                     unpack8(z[i], zz);
                     with_activation(g.act, [&](auto act) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] *= slope<decltype(act)::value>(zz[k]);
+                        for (int k = 0; k < 8; ++k) v[k] = through<decltype(act)::value>(zz[k], v[k]);
                     });
                 }
                 if (g.drop.state) drop8(drop, key, (uint64_t)at >> 3, v);

@@ -115,7 +115,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
     }
     if (!there) return;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) gain[k] *= rstd[k * U / 8];
+    for (int k = 0; k < 8; ++k) gain[k] *= rstd[k * U / 8], shift[k] -= mean[k * U / 8] * gain[k];
     with_activation(g.act, [&](auto act) {
 #pragma unroll
         for (int r = 0; r < NV; ++r)
@@ -123,10 +123,38 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
                 float v[8];
                 values<BF16>(x[r], v);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>((v[k] - mean[k * U / 8]) * gain[k] + shift[k]);
+                for (int k = 0; k < 8; ++k) v[k] = activate<decltype(act)::value>(v[k] * gain[k] + shift[k]);
                 store8<BF16>(g.Y, base + (int64_t)(row + r * step) * g.C, v);
             }
     });
+}
+
+// A channel in front of the activation, x G + S; and its dX = rstd (dpre gain - first - x^ second) as dpre G + (x P + Q)
+struct Front {
+    float G, S, mean;
+    __device__ __forceinline__ float pre(float x) const { return x * G + S; }
+};
+// of eight channels; and 1 / sqrt(var + eps) of their groups
+__device__ __forceinline__ void fronts_of(const GroupNorm& g, int64_t image, int channel, int cpg, Front (&f)[8], float (&rstd)[8]) {
+    float gain[8], shift[8];
+    load8<false>(g.gain, channel, gain), load8<false>(g.shift, channel, shift);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t q = image * g.groups + (channel + k) / cpg;
+        rstd[k] = gload(g.rstd + q);
+        f[k].mean = gload(g.mean + q);
+        f[k].G = gain[k] * rstd[k];
+        f[k].S = shift[k] - f[k].mean * f[k].G;
+    }
+}
+struct Slopes {
+    float G, S, P, Q;
+    __device__ __forceinline__ float pre(float x) const { return x * G + S; }
+    __device__ __forceinline__ float of(float x, float dpre) const { return dpre * G + (x * P + Q); }
+};
+__device__ __forceinline__ Slopes slopes_of(const Front& f, float rstd, float first, float second) {
+    const float P = -rstd * rstd * second;
+    return Slopes{f.G, f.S, P, -rstd * first - f.mean * P};
 }
 
 // sums [2, N, C] of dpre and of dpre x^
@@ -149,15 +177,9 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
             x[r] = raw8<BF16>(g.X, base + (int64_t)(row + r * step) * g.C);
             dy[r] = raw8<BF16>(g.dY, base + (int64_t)(row + r * step) * g.C);
         }
-    float gain[8], shift[8], mean[8], rstd[8];
-    if (there) {
-        load8<false>(g.gain, c0 + 8 * tc, gain), load8<false>(g.shift, c0 + 8 * tc, shift);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t q = image * g.groups + (c0 + 8 * tc + k) / cpg;
-            mean[k] = gload(g.mean + q), rstd[k] = gload(g.rstd + q);
-        }
-    }
+    Front f[8];
+    float rstd[8];
+    if (there) fronts_of(g, image, c0 + 8 * tc, cpg, f, rstd);
     float sum[2][8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[0][k] = sum[1][k] = 0.0f;
@@ -169,13 +191,15 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
                 values<BF16>(x[r], v), values<BF16>(dy[r], d);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    v[k] = (v[k] - mean[k]) * rstd[k];
-                    if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
-                    sum[0][k] += d[k];
-                    sum[1][k] += d[k] * v[k];
+                    const float dpre = through<decltype(act)::value>(f[k].pre(v[k]), d[k]);
+                    sum[0][k] += dpre;
+                    sum[1][k] += dpre * (v[k] - f[k].mean);
                 }
             }
     });
+    if (there)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[1][k] *= rstd[k];
     channel_sums<THREADS, 2, 8>(sum, sp.shift, width, pitch, waves, chan);
     for (int c = threadIdx.x; c < width; c += THREADS)
 #pragma unroll
@@ -198,9 +222,14 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
     });
     __syncthreads();
     if (!there) return;
-    float first[8], second[8];
+    // (computed again from what lies in registers: kept, the values in between spilled)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) first[k] = stat[(8 * tc + k) / cpg], second[k] = stat[pitch + (8 * tc + k) / cpg];
+    for (int r = 0; r < NV; ++r)
+#pragma unroll
+        for (int k = 0; k < (BF16 ? 4 : 8); ++k) asm volatile("" : "+v"(x[r].w[k]), "+v"(dy[r].w[k]));
+    Slopes c[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c[k] = slopes_of(f[k], rstd[k], stat[(8 * tc + k) / cpg], stat[pitch + (8 * tc + k) / cpg]);
     with_activation(g.act, [&](auto act) {
 #pragma unroll
         for (int r = 0; r < NV; ++r)
@@ -208,11 +237,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
                 float v[8], d[8];
                 values<BF16>(x[r], v), values<BF16>(dy[r], d);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = (v[k] - mean[k]) * rstd[k];
-                    if (decltype(act)::value != ABT_ACT_NONE) d[k] *= slope<decltype(act)::value>(v[k] * gain[k] + shift[k]);
-                    v[k] = rstd[k] * (d[k] * gain[k] - first[k] - v[k] * second[k]);
-                }
+                for (int k = 0; k < 8; ++k) v[k] = c[k].of(v[k], through<decltype(act)::value>(c[k].pre(v[k]), d[k]));
                 store8<BF16>(g.Y, base + (int64_t)(row + r * step) * g.C, v);
             }
     });
@@ -364,31 +389,22 @@ __global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const 
     });
     __syncthreads();
     if (!p.there) return;
-    float gain[8], shift[8], mean[8];
+    float gain[8], shift[8];
     load8<false>(g.gain, p.c0 + 8 * p.tc, gain), load8<false>(g.shift, p.c0 + 8 * p.tc, shift);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int q = (p.c0 + 8 * p.tc + k) / sg.cpg - sg.first;
-        mean[k] = stat[0][q];
         gain[k] *= stat[1][q];
+        shift[k] -= stat[0][q] * gain[k];
     }
     with_activation(g.act, [&](auto act) {
         by_rows<BF16, false>(g, p, [&](int r, const float (&v)[8], const float (&)[8]) {
             float y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = activate<decltype(act)::value>((v[k] - mean[k]) * gain[k] + shift[k]);
+            for (int k = 0; k < 8; ++k) y[k] = activate<decltype(act)::value>(v[k] * gain[k] + shift[k]);
             store8<BF16>(g.Y, p.base + (int64_t)r * g.C, y);
         });
     });
-}
-
-__device__ __forceinline__ void load_stats(const GroupNorm& g, const Piece& p, int cpg, float (&gain)[8], float (&shift)[8], float (&mean)[8], float (&rstd)[8]) {
-    load8<false>(g.gain, p.c0 + 8 * p.tc, gain), load8<false>(g.shift, p.c0 + 8 * p.tc, shift);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int64_t q = p.image * g.groups + (p.c0 + 8 * p.tc + k) / cpg;
-        mean[k] = gload(g.mean + q), rstd[k] = gload(g.rstd + q);
-    }
 }
 
 // sums [2, N pieces, C] of dpre and of dpre x^, and behind them per slot the same times the gain, over the group's channels in this slab
@@ -402,19 +418,21 @@ __global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, c
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[0][k] = sum[1][k] = 0.0f;
     if (p.there) {
-        float gain[8], shift[8], mean[8], rstd[8];
-        load_stats(g, p, cpg, gain, shift, mean, rstd);
+        Front f[8];
+        float rstd[8];
+        fronts_of(g, p.image, p.c0 + 8 * p.tc, cpg, f, rstd);
         with_activation(g.act, [&](auto act) {
             by_rows<BF16, true>(g, p, [&](int, const float (&x)[8], const float (&dy)[8]) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float v = (x[k] - mean[k]) * rstd[k];
-                    const float d = decltype(act)::value != ABT_ACT_NONE ? dy[k] * slope<decltype(act)::value>(v * gain[k] + shift[k]) : dy[k];
-                    sum[0][k] += d;
-                    sum[1][k] += d * v;
+                    const float dpre = through<decltype(act)::value>(f[k].pre(x[k]), dy[k]);
+                    sum[0][k] += dpre;
+                    sum[1][k] += dpre * (x[k] - f[k].mean);
                 }
             });
         });
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[1][k] *= rstd[k];
     }
     channel_sums<256, 2, 8>(sum, sp.shift, p.width, kMaxSlab, waves, chan);
     for (int c = threadIdx.x; c < p.width; c += 256)
@@ -482,22 +500,20 @@ __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, co
     });
     __syncthreads();
     if (!p.there) return;
-    float gain[8], shift[8], mean[8], rstd[8], a[8], b[8];
-    load_stats(g, p, cpg, gain, shift, mean, rstd);
+    Front f[8];
+    Slopes c[8];
+    float rstd[8];
+    fronts_of(g, p.image, p.c0 + 8 * p.tc, cpg, f, rstd);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int q = (p.c0 + 8 * p.tc + k) / cpg - sg.first;
-        a[k] = stat[0][q], b[k] = stat[1][q];
+        c[k] = slopes_of(f[k], rstd[k], stat[0][q], stat[1][q]);
     }
     with_activation(g.act, [&](auto act) {
         by_rows<BF16, true>(g, p, [&](int r, const float (&x)[8], const float (&dy)[8]) {
             float y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float v = (x[k] - mean[k]) * rstd[k];
-                const float d = decltype(act)::value != ABT_ACT_NONE ? dy[k] * slope<decltype(act)::value>(v * gain[k] + shift[k]) : dy[k];
-                y[k] = rstd[k] * (d * gain[k] - a[k] - v * b[k]);
-            }
+            for (int k = 0; k < 8; ++k) y[k] = c[k].of(x[k], through<decltype(act)::value>(c[k].pre(x[k]), dy[k]));
             store8<BF16>(g.Y, p.base + (int64_t)r * g.C, y);
         });
     });
@@ -513,6 +529,8 @@ int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 
 // How a call is split; threads, vectors: of the `whole` kernels, threads = 0 for the others
 struct Plan { Split sp; int threads, vectors; };
+// Vectors that fit a thread's registers: 128 of them with 1024 threads, 256 with fewer; the backward has two tensors
+constexpr int most_vectors(bool bf16, bool backward, int threads) { return (bf16 ? 16 : 8) / (backward && threads == 1024 ? 4 : 1); }
 int threads_across(int width) {                           // as a power of two's exponent
     int shift = 0;
     while ((8 << shift) < width) ++shift;
@@ -521,14 +539,14 @@ int threads_across(int width) {                           // as a power of two's
 Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
     Plan p{};
     const int cpg = C / groups, unit = cpg / gcd(cpg, 8) * 8, wide = 64;      // whole groups and vectors; 128 bytes in bf16, 256 in fp32
-    const int most = (bf16 ? 16 : 8) / (backward ? 2 : 1);                    // vectors in a thread's registers
     if (unit <= kMaxSlab) {
         auto whole = [&](int width) {                     // a multiple of unit
             const int shift = threads_across(width);
-            for (int few : {4, most})                     // four vectors a thread with as few threads as that takes, or as many as fit
+            // four vectors a thread (backward: eight) with as few threads as that takes, or as many as fit
+            for (int few : {backward ? 8 : 4, 16})
                 for (int threads = 256; threads <= 1024; threads *= 2) {
                     const int vectors = (int)ceil_div(pixels, threads >> shift);
-                    if (vectors > few || vectors > most) continue;
+                    if (vectors > few || vectors > most_vectors(bf16, backward, threads)) continue;
                     p.sp = Split{width, (int)ceil_div(C, width), shift, 1, pixels};
                     p.threads = threads;
                     p.vectors = vectors;
@@ -580,13 +598,14 @@ hipError_t launch_whole(const GroupNorm& g, const Split& sp, hipStream_t s) {
 }
 template <bool BF16, bool BWD, int THREADS>
 hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
-    constexpr int most = (BF16 ? 16 : 8) / (BWD ? 2 : 1);
+    constexpr int most = most_vectors(BF16, BWD, THREADS);
     if (p.vectors <= 2) return launch_whole<BF16, BWD, THREADS, 2>(g, p.sp, s);
-    if (p.vectors <= 4) return launch_whole<BF16, BWD, THREADS, 4>(g, p.sp, s);
-    if constexpr (most >= 8) {
+    if constexpr (most >= 4)
+        if (p.vectors <= 4) return launch_whole<BF16, BWD, THREADS, 4>(g, p.sp, s);
+    if constexpr (most >= 8)
         if (p.vectors <= 8) return launch_whole<BF16, BWD, THREADS, 8>(g, p.sp, s);
-        if constexpr (most >= 16) return launch_whole<BF16, BWD, THREADS, 16>(g, p.sp, s);
-    }
+    if constexpr (most >= 16)
+        if (p.vectors <= 16) return launch_whole<BF16, BWD, THREADS, 16>(g, p.sp, s);
     return hipErrorInvalidValue;
 }
 template <bool BF16, bool BWD>
