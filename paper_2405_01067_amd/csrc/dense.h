@@ -52,6 +52,7 @@ struct DenseGrads {
     const float* sums; float* dbias;
     int64_t M;
     int m, n, pieces, accumulate;
+    int values;                            // of dZ where dW is wanted: how the launches are made does not go by what is wanted
     float alpha;
 };
 size_t dense_grad_partial_bytes(int64_t M, int m, int n);

@@ -84,8 +84,9 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
 
     DenseSlope z{};
     z.dY = (const uint16_t*)dY; z.Z = act == ABT_ACT_NONE ? nullptr : (const uint16_t*)Z;
+    const int values = !smooth ? 1 : M <= kDenseThreeValues ? 3 : 2;
     if ((dX || dW) && (z.Z || drop.state))
-        for (int q = 0; q < (!smooth || !dW ? 1 : M <= kDenseThreeValues ? 3 : 2); ++q) z.value[q] = (uint16_t*)(ws + at.value[q]);
+        for (int q = 0; q < (dW ? values : 1); ++q) z.value[q] = (uint16_t*)(ws + at.value[q]);
     if (dbias) z.sums = (float*)(ws + at.sums);
     if (dX) { z.W = (const uint16_t*)W; z.Wt = (uint16_t*)(ws + at.Wt); }
     z.M = M; z.m = (int)m; z.n = (int)n; z.act = act; z.scaled = smooth; z.rows = dense_piece_rows(M, (int)m); z.drop = drop;
@@ -93,7 +94,7 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
     const uint16_t* const dZ = z.value[0] ? z.value[0] : z.dY;
     const float alpha = smooth ? 1.0f : drop.scale;       // what dZ was left without
     const DenseProduct x{dZ, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f}, (float*)(ws + at.parts), 0};
-    const DenseGrads g{{dZ, z.value[1], z.value[2]}, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, alpha};
+    const DenseGrads g{{dZ, z.value[1], z.value[2]}, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, values, alpha};
     return launch_dense_bwd(x, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
 }
 

@@ -29,10 +29,8 @@ __global__ __launch_bounds__(64 * NW) void dense_few_kernel(const DenseProduct g
         for (int b = 0; b < CB; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
     // a step: 64 columns, of which lane group lq has 16; the same on both sides
     struct Ops { u32x4 w[CB][2], x[RB][2]; };
-    // (work-groups begin at different steps: they read the same rows of X)
-    const int turn = (int)((unsigned)block * 5u % (unsigned)steps);
     auto read = [&](Ops& o, int s) {
-        const int t = s + turn < steps ? s + turn : s < steps ? s + turn - steps : steps, k = t * 128 + lq * 32;
+        const int k = s * 128 + lq * 32;                  // (steps past the last one are zeros)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = k + 16 * h < bytes ? li * bytes + k + 16 * h : kBufNowhere, step = at == kBufNowhere ? 0 : 16 * bytes;
@@ -47,7 +45,7 @@ __global__ __launch_bounds__(64 * NW) void dense_few_kernel(const DenseProduct g
     for (int d = 0; d < D; ++d) read(ring[d], wave + d * NW);
     for (int s = wave; s < steps; s += NW * D)
 #pragma unroll
-        for (int d = 0; d < D; ++d) {                     // (steps past the last one are zeros)
+        for (int d = 0; d < D; ++d) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll

@@ -428,7 +428,7 @@ size_t dense_grad_partial_bytes(int64_t M, int m, int n) {
     return splits == 1 ? 0 : (size_t)splits * (size_t)m * (size_t)n * 4;
 }
 hipError_t launch_dense_bwd(const DenseProduct& x, const DenseGrads& g, hipStream_t s) {
-    const int values = g.value[2] ? 3 : g.value[1] ? 2 : 1;
+    const int values = g.values;
     const GradWay w = grad_way(g.M, g.m, g.n, values);
     // Together: the longest work-group, or what all of them keep the chip busy; apart: one after the other.  Of 56 shapes (8 to 4000 rows) what this takes is 0.5 % slower than
     // the other on average (33 % at worst).  us, together / apart: 394 rows, 768 x 768, three values 9.4 / 17.5; 1000 rows, 2304 x 768 26.8 / 38.2; 1500 rows, 512 x 512 24.3 / 18.8;

@@ -14,6 +14,7 @@ struct GroupNorm {
     float* sums;                           // workspace
     float* dgain; float* dshift;           // may be NULL
     int64_t N;
+    int64_t image0;                        // set by the launchers: the first image of a launch
     int pixels, C, groups, act, accumulate;
     float eps;
 };

@@ -65,8 +65,8 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
     extern __shared__ float lds[];
     const int pitch = sp.width;
     float *const waves = lds, *const chan = waves + THREADS / 64 * pitch, *const stat = chan + pitch;
-    const int slab = blockIdx.x % sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
-    const int64_t image = blockIdx.x / sp.slabs;
+    const int slab = blockIdx.x % (unsigned)sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
+    const int64_t image = g.image0 + blockIdx.x / (unsigned)sp.slabs;
     const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
     const bool there = 8 * tc < width;
     const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
@@ -163,8 +163,8 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
     extern __shared__ float lds[];
     const int pitch = sp.width;
     float *const waves = lds, *const chan = waves + 2 * (THREADS / 64) * pitch, *const stat = chan + 2 * pitch;
-    const int slab = blockIdx.x % sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
-    const int64_t image = blockIdx.x / sp.slabs;
+    const int slab = blockIdx.x % (unsigned)sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
+    const int64_t image = g.image0 + blockIdx.x / (unsigned)sp.slabs;
     const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
     const bool there = 8 * tc < width;
     const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
@@ -245,12 +245,12 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
 
 // ------------------------------------------------------------------------------------------ in pieces
 struct Piece { int c0, width, piece, tc, first, last, step; int64_t image, base; bool there; };
-__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, int64_t block) {
+__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, unsigned block) {
     Piece p;
-    const int slab = (int)(block % sp.slabs);
-    block /= sp.slabs;
-    p.piece = (int)(block % sp.pieces);
-    p.image = block / sp.pieces;
+    const int slab = (int)(block % (unsigned)sp.slabs);
+    block /= (unsigned)sp.slabs;
+    p.piece = (int)(block % (unsigned)sp.pieces);
+    p.image = g.image0 + block / (unsigned)sp.pieces;
     p.c0 = slab * sp.width;
     p.width = g.C - p.c0 < sp.width ? g.C - p.c0 : sp.width;
     p.tc = threadIdx.x & ((1 << sp.shift) - 1);
@@ -477,7 +477,7 @@ __device__ __forceinline__ void channel_gradients(const GroupNorm& g, int64_t ro
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, const Split sp, int64_t blocks) {
+__global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, const Split sp, unsigned blocks) {
     __shared__ float stat[2][kMaxSlab];
     if (blockIdx.x >= blocks) {
         channel_gradients(g, g.N * sp.pieces, (int)(blockIdx.x - blocks), reinterpret_cast<float (*)[8]>(&stat[0][0]));
@@ -522,6 +522,26 @@ __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, co
 __global__ __launch_bounds__(256) void gn_channels_kernel(const GroupNorm g, int64_t rows) {
     __shared__ float lds[32][8];
     channel_gradients(g, rows, blockIdx.x, lds);
+}
+// Many rows: sums of 1024 of them each first, [2, rows / 1024, C] behind what the other launches leave
+constexpr int kManyRows = 4096, kRowsOfSum = 1024;
+__global__ __launch_bounds__(256) void gn_rows_kernel(const GroupNorm g, int64_t rows, float* out) {
+    __shared__ float lds[32][8];
+    const unsigned chunks = (unsigned)((rows + kRowsOfSum - 1) / kRowsOfSum), chunk = blockIdx.x % chunks, block = blockIdx.x / chunks;
+    const int c = (int)(block / 2) * 8 + (threadIdx.x & 7), part = threadIdx.x >> 3, q = block & 1;
+    const int64_t first = (int64_t)chunk * kRowsOfSum, last = first + kRowsOfSum < rows ? first + kRowsOfSum : rows;
+    const float* const from = g.sums + q * rows * g.C + c;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < kRowsOfSum / 32; ++i) {
+        const int64_t r = first + part + 32 * i;
+        if (r < last) s += gload(from + r * g.C);
+    }
+    lds[part][threadIdx.x & 7] = s;
+    __syncthreads();
+    if (part) return;
+    for (int k = 1; k < 32; ++k) s += lds[k][threadIdx.x];
+    gstore(out + ((int64_t)q * chunks + chunk) * g.C + c, s);
 }
 
 // ------------------------------------------------------------------------------------------ which
@@ -583,18 +603,29 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
     return p;
 }
 
+// f(g, blocks, last) for launches of fewer than 2^32 threads, some images each
+template <class F>
+hipError_t by_images(GroupNorm g, int64_t blocks_per_image, F&& f) {
+    const int64_t most = (1 << 21) / blocks_per_image;
+    for (g.image0 = 0; g.image0 < g.N; g.image0 += most) {
+        const int64_t left = g.N - g.image0;
+        f(g, (unsigned)((left < most ? left : most) * blocks_per_image), left <= most);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <bool BF16, bool BWD, int THREADS, int NV>
-hipError_t launch_whole(const GroupNorm& g, const Split& sp, hipStream_t s) {
-    const int64_t blocks = g.N * sp.slabs;
-    if (blocks > INT_MAX) return hipErrorInvalidValue;
-    const unsigned lds = (unsigned)(((BWD ? 2 : 1) * (THREADS / 64 + 1) + 2) * sp.width * 4);      // 72 KB at most
-    const dim3 grid((unsigned)blocks);
-    const int cpg = g.C / g.groups;
-    if constexpr (BWD) hipLaunchKernelGGL((gn_whole_bwd_kernel<BF16, THREADS, NV>), grid, dim3(THREADS), lds, s, g, sp);
-    else if (cpg % 8 == 0) hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 1>), grid, dim3(THREADS), lds, s, g, sp);
-    else if (cpg % 4 == 0) hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 2>), grid, dim3(THREADS), lds, s, g, sp);
-    else hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 8>), grid, dim3(THREADS), lds, s, g, sp);
-    return hipGetLastError();
+hipError_t launch_whole(const GroupNorm& all, const Split& sp, hipStream_t s) {
+    const unsigned lds = (unsigned)(((BWD ? 2 : 1) * (THREADS / 64 + 1) + 2) * sp.width * 4);      // 40 KB at most: 512 threads backward, or 1024 forward, and 512 channels
+    const int cpg = all.C / all.groups;
+    return by_images(all, sp.slabs, [&](const GroupNorm& g, unsigned blocks, bool) {
+        if constexpr (BWD) hipLaunchKernelGGL((gn_whole_bwd_kernel<BF16, THREADS, NV>), dim3(blocks), dim3(THREADS), lds, s, g, sp);
+        else if (cpg % 8 == 0) hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 1>), dim3(blocks), dim3(THREADS), lds, s, g, sp);
+        else if (cpg % 4 == 0) hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 2>), dim3(blocks), dim3(THREADS), lds, s, g, sp);
+        else hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 8>), dim3(blocks), dim3(THREADS), lds, s, g, sp);
+    });
 }
 template <bool BF16, bool BWD, int THREADS>
 hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
@@ -614,24 +645,40 @@ hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
 }
 
 template <bool BF16>
-hipError_t pieces_fwd(const GroupNorm& g, const Split& sp, hipStream_t s) {
-    const int64_t blocks = g.N * sp.slabs * sp.pieces;
-    if (blocks > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gn_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
-    const hipError_t e = hipGetLastError();
+hipError_t pieces_fwd(const GroupNorm& all, const Split& sp, hipStream_t s) {
+    const int64_t per_image = (int64_t)sp.slabs * sp.pieces;
+    const hipError_t e = by_images(all, per_image, [&](const GroupNorm& g, unsigned blocks, bool) { hipLaunchKernelGGL((gn_pieces_kernel<BF16>), dim3(blocks), dim3(256), 0, s, g, sp); });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gn_apply_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
+    return by_images(all, per_image, [&](const GroupNorm& g, unsigned blocks, bool) { hipLaunchKernelGGL((gn_apply_kernel<BF16>), dim3(blocks), dim3(256), 0, s, g, sp); });
+}
+// dgain and dshift from `rows` rows of sums
+hipError_t channel_sums_of(GroupNorm g, int64_t rows, float* more, hipStream_t s) {
+    if (rows > kManyRows) {
+        const int64_t chunks = ceil_div(rows, kRowsOfSum), blocks = chunks * (g.C / 4);
+        if (blocks >= 1 << 24) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(gn_rows_kernel, dim3((unsigned)blocks), dim3(256), 0, s, g, rows, more);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        g.sums = more;
+        rows = chunks;
+    }
+    hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)(g.C / 4)), dim3(256), 0, s, g, rows);
     return hipGetLastError();
 }
+// Where those sums lie: behind the sums of the channels and the partials
+int64_t floats_before(int64_t N, int C, int groups, const Plan& p) { return N * p.sp.pieces * (2 * (int64_t)C + (p.threads ? 0 : 2 * (int64_t)(groups + p.sp.slabs))); }
+
 template <bool BF16>
-hipError_t pieces_bwd(const GroupNorm& g, const Split& sp, hipStream_t s) {
-    const int64_t blocks = g.N * sp.slabs * sp.pieces, sums = g.dgain || g.dshift ? g.C / 4 : 0, apply = g.Y ? blocks : 0;
-    if (blocks + sums > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3((unsigned)blocks), dim3(256), 0, s, g, sp);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || apply + sums == 0) return e;
-    hipLaunchKernelGGL((gn_bwd_apply_kernel<BF16>), dim3((unsigned)(apply + sums)), dim3(256), 0, s, g, sp, apply);
-    return hipGetLastError();
+hipError_t pieces_bwd(const GroupNorm& all, const Split& sp, float* more, hipStream_t s) {
+    const int64_t per_image = (int64_t)sp.slabs * sp.pieces, rows = all.N * sp.pieces;
+    const bool channels = all.dgain || all.dshift;
+    hipError_t e = by_images(all, per_image, [&](const GroupNorm& g, unsigned blocks, bool) { hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3(blocks), dim3(256), 0, s, g, sp); });
+    if (e != hipSuccess) return e;
+    if (!all.Y) return channel_sums_of(all, rows, more, s);
+    e = by_images(all, per_image, [&](const GroupNorm& g, unsigned blocks, bool last) {      // the gradients of the channels beside the last images
+        hipLaunchKernelGGL((gn_bwd_apply_kernel<BF16>), dim3(blocks + (last && channels && rows <= kManyRows ? (unsigned)g.C / 4 : 0)), dim3(256), 0, s, g, sp, blocks);
+    });
+    return e != hipSuccess || !channels || rows <= kManyRows ? e : channel_sums_of(all, rows, more, s);
 }
 
 template <bool BF16>
@@ -642,19 +689,19 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
 template <bool BF16>
 hipError_t bwd(const GroupNorm& g, hipStream_t s) {
     const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, true);
-    if (!p.threads) return pieces_bwd<BF16>(g, p.sp, s);
+    float* const more = g.sums + floats_before(g.N, g.C, g.groups, p);
+    if (!p.threads) return pieces_bwd<BF16>(g, p.sp, more, s);
     const hipError_t e = launch_whole<BF16, true>(g, p, s);
-    if (e != hipSuccess || g.N == 1 || (!g.dgain && !g.dshift)) return e;
-    hipLaunchKernelGGL(gn_channels_kernel, dim3((unsigned)(g.C / 4)), dim3(256), 0, s, g, g.N);
-    return hipGetLastError();
+    return e != hipSuccess || g.N == 1 || (!g.dgain && !g.dshift) ? e : channel_sums_of(g, g.N, more, s);
 }
 
 }  // namespace
 
 size_t group_norm_sum_bytes(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
     const Plan p = plan_of(N, pixels, C, groups, bf16, backward);
-    const size_t channels = backward ? (size_t)N * (size_t)p.sp.pieces * (size_t)C * 8 : 0;
-    return channels + (p.threads ? 0 : (size_t)N * (size_t)p.sp.pieces * (size_t)(groups + p.sp.slabs) * 8);
+    if (!backward) return p.threads ? 0 : (size_t)(N * p.sp.pieces * (groups + p.sp.slabs)) * 8;
+    const int64_t rows = N * p.sp.pieces;
+    return (size_t)(floats_before(N, C, groups, p) + (rows > kManyRows ? ceil_div(rows, kRowsOfSum) * 2 * C : 0)) * 4;
 }
 hipError_t launch_group_norm_fwd(const GroupNorm& p, bool bf16, hipStream_t s) { return bf16 ? fwd<true>(p, s) : fwd<false>(p, s); }
 hipError_t launch_group_norm_bwd(const GroupNorm& p, bool bf16, hipStream_t s) { return bf16 ? bwd<true>(p, s) : bwd<false>(p, s); }

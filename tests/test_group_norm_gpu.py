@@ -12,7 +12,7 @@ ACT_ERR = 4e-6                                # of an activation or its slope, s
 ACTS = ("none", "relu", "gelu", "gelu_tanh", "silu")
 # N, pixels, C, groups: everything at once (several numbers of threads and pixels per thread), in pieces; groups of one channel, of all, of 3 and 12; slabs that cut a group
 SHAPES = [(1, 1, 8, 1), (1, 1, 8, 8), (2, 49, 64, 32), (3, 196, 256, 32), (2, 7, 96, 32), (5, 50, 24, 2), (1, 784, 128, 32), (2, 300, 1024, 1), (1, 600, 2048, 2), (1, 3136, 64, 32), (1, 5000, 64, 8),
-          (2, 1023, 72, 24), (1, 2049, 1160, 5), (3, 33, 8, 4), (1, 9000, 16, 16), (1, 3, 65536, 64), (70, 4, 520, 13)]
+          (2, 1023, 72, 24), (1, 2049, 1160, 5), (3, 33, 8, 4), (1, 9000, 16, 16), (1, 3, 65536, 64), (70, 4, 520, 13), (5000, 2, 16, 2), (40, 3000, 8, 2)]
 
 
 def make(shape, dtype, seed, offset=1.0):
@@ -168,3 +168,28 @@ def test_channels_last_image():
     flat = abt.lr_group_norm_fwd(X.reshape(2, 30, 16), g, s, 4)[0]
     assert Y.shape == X.shape and bool((Y.reshape(2, 30, 16) == flat).all()) and mean.shape == (2, 4)
     assert abt.lr_group_norm_bwd(X, X, g, s, mean, rstd)[0].shape == X.shape
+
+
+def test_more_images_than_a_launch_takes():
+    """Launches of fewer than 2^32 threads: 2^21 work-groups."""
+    import torch
+    N, C = (1 << 21) + 777, 8
+    X = torch.randn((N, 1, C), device="cuda")
+    g, s = torch.full((C,), 2.0, device="cuda"), torch.full((C,), 0.5, device="cuda")
+    Y, mean, rstd = abt.lr_group_norm_fwd(X, g, s, 2)
+    dX, dgain, dshift = abt.lr_group_norm_bwd(X, X, g, s, mean, rstd)
+    x = X.double().reshape(N, 2, 4)
+    m, v = x.mean(2, keepdim=True), x.var(2, correction=0, keepdim=True)
+    unit = (x - m) / (v + 1e-5).sqrt()
+    assert bool(((Y.double().reshape(N, 2, 4) - (unit * 2 + 0.5)).abs() <= 1e-3 * (1 + unit.abs())).all())        # (var of four values may be next to nothing)
+    assert float((mean.double() - m[:, :, 0]).abs().max()) < 1e-6
+    u = x * 2
+    want = (u - u.mean(2, keepdim=True) - unit * (u * unit).mean(2, keepdim=True)) / (v + 1e-5).sqrt()
+    # X lies in the span of 1 and x^, so dX is what eps leaves of terms some 1e4 times its size: fp32 errors of the terms count, not dX's own.  x^ is off by the roundings of
+    # mean, rstd and their product, x (P) and Q by those of their sum, eight at most of the size (|x| + |m|) rstd; u, its mean and the products by eight of their own.
+    r, mean_of = 1 / (v + 1e-5).sqrt(), lambda a: a.abs().mean(2, keepdim=True)
+    off = 8 * F32 * ((x.abs() + m.abs()) * r + unit.abs())
+    err = r * (8 * F32 * (u.abs() + mean_of(u) + unit.abs() * mean_of(u * unit)) + off * mean_of(u * unit) + unit.abs() * mean_of(u * off) + off.amax(2, keepdim=True) * u.abs())
+    assert bool(((dX.double().reshape(N, 2, 4) - want).abs() <= err + 1e-30).all())
+    for got, ref in ((dgain, (x * unit).sum(0).reshape(-1)), (dshift, x.sum(0).reshape(-1))):
+        assert bool(((got.double() - ref).abs() <= 1e-6 * x.abs().sum() / C + 1e-5 * ref.abs()).all())
