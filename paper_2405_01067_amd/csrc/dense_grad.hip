@@ -1,4 +1,6 @@
 // Gradients of the dense layer: what its products are made of, and dW = dZ^T X, a contraction over the rows.
+// 12608 rows, 2304 x 768, gelu (two values): dZ 46 us, bound by memory (232 MB at 5.0 TB/s); dX 53 (dense_tile.hip); dW 96 (89 GFLOP of two products at 930 TFLOP/s, and 64 MB of partials);
+// their sum 13 (5.2 TB/s).  394 rows, 768 x 768, silu (three values): dZ 5.8 us, everything else 9.5: latency.
 #include <climits>
 #include <cmath>
 
