@@ -514,7 +514,7 @@ typedef struct {
 
 int lr_dense_fwd(const void* X, const void* W, const float* bias, const void* residual, void* Y, void* Z_save,
                  int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, void* workspace, size_t workspace_bytes, void* stream);
-size_t lr_dense_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n);   /* 0 for shapes that are refused */
+size_t lr_dense_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n);   /* 0: none is needed, or the shape is refused */
 int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, void* dX, float* dW, float* dbias,
                  int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dropout, int dt, int accumulate,
                  void* workspace, size_t workspace_bytes, void* stream);
@@ -543,7 +543,7 @@ int lr_group_norm_fwd(const void* X, const float* gain, const float* shift, doub
 int lr_group_norm_bwd(const void* dY, const void* X, const float* gain, const float* shift, const float* mean, const float* rstd,
                       void* dX, float* dgain, float* dshift, int64_t N, int64_t pixels, int64_t C, int64_t groups, int act, int dt, int accumulate,
                       void* workspace, size_t workspace_bytes, void* stream);
-size_t lr_group_norm_workspace_bytes(int64_t N, int64_t pixels, int64_t C, int64_t groups, int dt, int backward);   /* 0 for shapes that are refused */
+size_t lr_group_norm_workspace_bytes(int64_t N, int64_t pixels, int64_t C, int64_t groups, int dt, int backward);   /* 0: none is needed, or the shape is refused */
 
 /* Work-group height of the bf16 chain kernel (T = X B^T, Y = T A^T and the dT / dX half of the
  * backward): 0 = chosen from the batch size (default), 64 or 128 = forced where the rank allows it.

@@ -1123,7 +1123,7 @@ def lr_dense_fwd(X, W, bias=None, act: str = "none", dropout=None, residual=None
     else:
         _plain_matrix(Z, "Z", (M, m), bf16)
     lib = load()
-    ws = _workspace(lib.lr_dense_fwd_workspace_bytes(M, m, n), X.device, workspace)
+    ws = _workspace(lib.lr_dense_fwd_workspace_bytes(M, m, n), X.device, workspace)      # 256 bytes where none is needed
     _on_this_device(X, (W, bias, residual, Y, Z, ws))
     _check(lib.lr_dense_fwd(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(), _ptr(Z), M, m, n, _activation(act),
                             _dropout(dropout, X.device), ABT_BF16, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "lr_dense_fwd")
@@ -1218,9 +1218,9 @@ def lr_group_norm_fwd(X, gain, shift, groups: int, eps: float = 1e-5, act: str =
     N, pixels, C = _images(X)
     dt = _dt(X)
     _plain_matrix(gain, "gain", (C,), f32), _plain_matrix(shift, "shift", (C,), f32)
+    if C % 8 or groups < 1 or C % groups:
+        raise AbtError(f"lr_group_norm_fwd: {C} channels are no multiple of 8 and of {groups} groups")
     need = lib.lr_group_norm_workspace_bytes(N, pixels, C, int(groups), dt, 0)
-    if need == 0:
-        raise AbtError(f"lr_group_norm_fwd: unsupported shape {tuple(X.shape)} with {groups} groups (C a multiple of 8 and of groups)")
     out = []
     for t, nm, shape, dtype in ((Y, "Y", X.shape, X.dtype), (mean, "mean", (N, int(groups)), f32), (rstd, "rstd", (N, int(groups)), f32)):
         if t is None:
@@ -1256,9 +1256,9 @@ def lr_group_norm_bwd(dY, X, gain, shift, mean, rstd, act: str = "none", need_dX
     _plain_matrix(dY, "dY", X.shape, X.dtype)
     for t, nm, shape in ((gain, "gain", (C,)), (shift, "shift", (C,)), (mean, "mean", (N, groups)), (rstd, "rstd", (N, groups))):
         _plain_matrix(t, nm, shape, f32)
+    if C % 8 or groups < 1 or C % groups:
+        raise AbtError(f"lr_group_norm_bwd: {C} channels are no multiple of 8 and of {groups} groups")
     need = lib.lr_group_norm_workspace_bytes(N, pixels, C, groups, dt, 1)
-    if need == 0:
-        raise AbtError(f"lr_group_norm_bwd: unsupported shape {tuple(X.shape)} with {groups} groups (C a multiple of 8 and of groups)")
     out = []
     for t, nm, wanted, shape, dtype in ((dX, "dX", need_dX, X.shape, X.dtype), (dgain, "dgain", need_dgain, (C,), f32), (dshift, "dshift", need_dshift, (C,), f32)):
         if not wanted:

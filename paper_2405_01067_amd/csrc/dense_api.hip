@@ -44,9 +44,7 @@ Places places(int64_t M, int64_t m, int64_t n) {
 extern "C" {
 
 size_t lr_dense_fwd_workspace_bytes(int64_t M, int64_t m, int64_t n) {
-    if (!sizes_fit(M, m, n)) return 0;
-    const size_t bytes = align_up(dense_part_bytes(M, (int)m, (int)n), 256);
-    return bytes < 256 ? 256 : bytes;
+    return sizes_fit(M, m, n) ? align_up(dense_part_bytes(M, (int)m, (int)n), 256) : 0;
 }
 
 int lr_dense_fwd(const void* X, const void* W, const float* bias, const void* residual, void* Y, void* Z_save,
@@ -56,8 +54,9 @@ int lr_dense_fwd(const void* X, const void* W, const float* bias, const void* re
     const int st = check_dense(M, m, n, act, dropout);
     if (st != ABT_OK) return st;
     if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(Z_save, 16)) return ABT_EALIGN;
-    if (!workspace || workspace_bytes < lr_dense_fwd_workspace_bytes(M, m, n)) return ABT_EWORKSPACE;
-    if (!aligned(workspace, 256)) return ABT_EALIGN;
+    const size_t need = lr_dense_fwd_workspace_bytes(M, m, n);
+    if (need && (!workspace || workspace_bytes < need)) return ABT_EWORKSPACE;
+    if (need && !aligned(workspace, 256)) return ABT_EALIGN;
     const DenseProduct p{(const uint16_t*)X, (const uint16_t*)W, (uint16_t*)Y, bias, (const uint16_t*)residual, (uint16_t*)Z_save, M, (int)m, (int)n, act, 1.0f, drop_of(dropout),
                          (float*)workspace, 0};
     return launch_dense(p, (hipStream_t)stream) == hipSuccess ? ABT_OK : ABT_EHIP;

@@ -703,6 +703,7 @@ hipError_t bwd(const GroupNorm& g, hipStream_t s) {
 size_t group_norm_sum_bytes(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
     const Plan p = plan_of(N, pixels, C, groups, bf16, backward);
     if (!backward) return p.threads ? 0 : (size_t)(N * p.sp.pieces * (groups + p.sp.slabs)) * 8;
+    if (p.threads && N == 1) return 0;
     const int64_t rows = N * p.sp.pieces;
     return (size_t)(floats_before(N, C, groups, p) + (rows > kManyRows ? ceil_div(rows, kRowsOfSum) * 2 * C : 0)) * 4;
 }

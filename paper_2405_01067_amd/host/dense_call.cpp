@@ -61,7 +61,9 @@ bool stream_of(const at::Tensor& X, std::initializer_list<const at::Tensor*> oth
     PyErr_Clear();
     return false;
 }
-at::Tensor space(size_t bytes, const at::TensorOptions& opt) { return at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, opt.dtype(at::kByte)); }
+// undefined where none is needed
+at::Tensor space(size_t bytes, const at::TensorOptions& opt) { return bytes ? at::empty({(int64_t)bytes}, opt.dtype(at::kByte)) : at::Tensor(); }
+size_t bytes_of(const at::Tensor& t) { return t.defined() ? (size_t)t.numel() : 0; }
 bool type_of(const at::Tensor& t, int& dt) {
     dt = t.scalar_type() == at::kBFloat16 ? ABT_BF16 : ABT_F32;
     return dt == ABT_BF16 || t.scalar_type() == at::kFloat;
@@ -102,7 +104,7 @@ PyObject* dense_fwd(PyObject*, PyObject* const* args, Py_ssize_t k) {
         Py_RETURN_NONE;                                  // out of memory and the like: the Python code meets it again and says so
     }
     if (!results) return nullptr;
-    return finished(results, dense_fwd_fn(x, w, (const float*)b, r, y, z, M, m, n, act, drop, ABT_BF16, ws.data_ptr(), (size_t)ws.numel(), stream),
+    return finished(results, dense_fwd_fn(x, w, (const float*)b, r, y, z, M, m, n, act, drop, ABT_BF16, address(ws), bytes_of(ws), stream),
                     "lr_dense_fwd");
 }
 
@@ -136,7 +138,7 @@ PyObject* dense_bwd(PyObject*, PyObject* const* args, Py_ssize_t k) {
         Py_RETURN_NONE;
     }
     if (!results) return nullptr;
-    return finished(results, dense_bwd_fn(dy, x, w, z, to[0], (float*)to[1], (float*)to[2], M, m, n, act, drop, ABT_BF16, 0, ws.data_ptr(), (size_t)ws.numel(), stream), "lr_dense_bwd");
+    return finished(results, dense_bwd_fn(dy, x, w, z, to[0], (float*)to[1], (float*)to[2], M, m, n, act, drop, ABT_BF16, 0, address(ws), bytes_of(ws), stream), "lr_dense_bwd");
 }
 
 // (X, dropout, residual) -> Y, or None
@@ -193,8 +195,9 @@ PyObject* group_fwd(PyObject*, PyObject* const* args, Py_ssize_t k) {
         groups = PyLong_AsSsize_t(args[3]);
         eps = PyFloat_AS_DOUBLE(args[4]);
         if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+        if (groups < 1 || C % 8 || C % groups) Py_RETURN_NONE;
         const size_t need = group_bytes_fn(N, pixels, C, groups, dt, 0);
-        if (need == 0 || !stream_of(*X, {gain, shift}, &stream)) Py_RETURN_NONE;
+        if (!stream_of(*X, {gain, shift}, &stream)) Py_RETURN_NONE;
         const auto opt = X->options().requires_grad(false);
         out[0] = at::empty(X->sizes(), opt);
         out[1] = at::empty({N, groups}, opt.dtype(at::kFloat));
@@ -208,8 +211,8 @@ PyObject* group_fwd(PyObject*, PyObject* const* args, Py_ssize_t k) {
         Py_RETURN_NONE;
     }
     if (!results) return nullptr;
-    return finished(results, group_fwd_fn(in[0], (const float*)in[1], (const float*)in[2], eps, to[0], (float*)to[1], (float*)to[2], N, pixels, C, groups, act, dt, ws.data_ptr(),
-                                          (size_t)ws.numel(), stream), "lr_group_norm_fwd");
+    return finished(results, group_fwd_fn(in[0], (const float*)in[1], (const float*)in[2], eps, to[0], (float*)to[1], (float*)to[2], N, pixels, C, groups, act, dt, address(ws),
+                                          bytes_of(ws), stream), "lr_group_norm_fwd");
 }
 
 // (dY, X, gain, shift, mean, rstd, act, need_dX, need_dgain, need_dshift) -> (dX, dgain, dshift), or None
@@ -230,8 +233,9 @@ PyObject* group_bwd(PyObject*, PyObject* const* args, Py_ssize_t k) {
         if (t[0]->scalar_type() != X->scalar_type() || t[0]->sizes() != X->sizes() || !is(t[2], at::kFloat, {C}) || !is(t[3], at::kFloat, {C}) || !is(t[4], at::kFloat, {N, groups}) ||
             !is(t[5], at::kFloat, {N, groups}))
             Py_RETURN_NONE;
+        if (groups < 1 || C % 8 || C % groups) Py_RETURN_NONE;
         const size_t bytes = group_bytes_fn(N, pixels, C, groups, dt, 1);
-        if (bytes == 0 || !stream_of(*X, {t[0], t[2], t[3], t[4], t[5]}, &stream)) Py_RETURN_NONE;
+        if (!stream_of(*X, {t[0], t[2], t[3], t[4], t[5]}, &stream)) Py_RETURN_NONE;
         const auto opt = X->options().requires_grad(false);
         if (need[0]) out[0] = at::empty(X->sizes(), opt);
         for (int i = 1; i < 3; ++i)
@@ -246,7 +250,7 @@ PyObject* group_bwd(PyObject*, PyObject* const* args, Py_ssize_t k) {
     }
     if (!results) return nullptr;
     return finished(results, group_bwd_fn(in[0], in[1], (const float*)in[2], (const float*)in[3], (const float*)in[4], (const float*)in[5], to[0], (float*)to[1], (float*)to[2], N, pixels, C,
-                                          groups, act, dt, 0, ws.data_ptr(), (size_t)ws.numel(), stream), "lr_group_norm_bwd");
+                                          groups, act, dt, 0, address(ws), bytes_of(ws), stream), "lr_group_norm_bwd");
 }
 
 // (addresses in the order of the functions above, the three callables); the type of binding.Dropout by itself
