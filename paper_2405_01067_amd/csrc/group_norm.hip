@@ -11,6 +11,7 @@
 
 #include "activation.h"
 #include "group_norm.h"
+#include "nt_tile.h"
 #include "vec8.h"
 
 namespace abt {
@@ -68,8 +69,9 @@ __global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g
     extern __shared__ float lds[];
     const int pitch = sp.width;
     float *const waves = lds, *const chan = waves + THREADS / 64 * pitch, *const stat = chan + pitch;
-    const int slab = blockIdx.x % (unsigned)sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
-    const int64_t image = g.image0 + blockIdx.x / (unsigned)sp.slabs;
+    const unsigned block = xcd_order(blockIdx.x, gridDim.x);                 // the slabs of an image, which share lines of memory, on one XCD
+    const int slab = block % (unsigned)sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
+    const int64_t image = g.image0 + block / (unsigned)sp.slabs;
     const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
     const bool there = 8 * tc < width;
     const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
@@ -166,8 +168,9 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
     extern __shared__ float lds[];
     const int pitch = sp.width;
     float *const waves = lds, *const chan = waves + 2 * (THREADS / 64) * pitch, *const stat = chan + 2 * pitch;
-    const int slab = blockIdx.x % (unsigned)sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
-    const int64_t image = g.image0 + blockIdx.x / (unsigned)sp.slabs;
+    const unsigned block = xcd_order(blockIdx.x, gridDim.x);                 // the slabs of an image, which share lines of memory, on one XCD
+    const int slab = block % (unsigned)sp.slabs, c0 = slab * sp.width, width = g.C - c0 < sp.width ? g.C - c0 : sp.width;
+    const int64_t image = g.image0 + block / (unsigned)sp.slabs;
     const int tc = threadIdx.x & ((1 << sp.shift) - 1), row = threadIdx.x >> sp.shift, step = THREADS >> sp.shift;
     const bool there = 8 * tc < width;
     const int64_t base = image * g.pixels * g.C + c0 + 8 * tc;
@@ -248,8 +251,9 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
 
 // ------------------------------------------------------------------------------------------ in pieces
 struct Piece { int c0, width, piece, tc, first, last, step; int64_t image, base; bool there; };
-__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, unsigned block) {
+__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, unsigned blocks) {
     Piece p;
+    unsigned block = xcd_order(blockIdx.x, blocks);
     const int slab = (int)(block % (unsigned)sp.slabs);
     block /= (unsigned)sp.slabs;
     p.piece = (int)(block % (unsigned)sp.pieces);
@@ -305,7 +309,7 @@ __device__ __forceinline__ const float* slots_of(const float* sums, const GroupN
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const Split sp) {
     __shared__ float waves[4 * kMaxSlab], chan[kMaxSlab], means[kMaxSlab];
-    const Piece p = piece_of(g, sp, blockIdx.x);
+    const Piece p = piece_of(g, sp, gridDim.x);
     const SlabGroups sg = groups_of(g, p);
     const float inv = 1.0f / (float)(p.last - p.piece * sp.rows);
     float mean[8], square[8], sum[1][8];
@@ -366,7 +370,7 @@ __device__ __forceinline__ int partials(const SlabGroups& sg, const Split& sp) {
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const Split sp) {
     __shared__ float stat[2][kMaxSlab];
-    const Piece p = piece_of(g, sp, blockIdx.x);
+    const Piece p = piece_of(g, sp, gridDim.x);
     const SlabGroups sg = groups_of(g, p);
     const float inv = 1.0f / ((float)g.pixels * (float)sg.cpg);
     by_group<256>(sg.count, partials(sg, sp), [&](int i, int l, int lanes) {
@@ -415,7 +419,7 @@ __device__ __forceinline__ float* slot_base(const GroupNorm& g, const Split& sp)
 template <bool BF16>
 __global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, const Split sp) {
     __shared__ float waves[8 * kMaxSlab], chan[2 * kMaxSlab];
-    const Piece p = piece_of(g, sp, blockIdx.x);
+    const Piece p = piece_of(g, sp, gridDim.x);
     const int cpg = g.C / g.groups;
     float sum[2][8];
 #pragma unroll
@@ -486,7 +490,7 @@ __global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, co
         channel_gradients(g, g.N * sp.pieces, (int)(blockIdx.x - blocks), reinterpret_cast<float (*)[8]>(&stat[0][0]));
         return;
     }
-    const Piece p = piece_of(g, sp, blockIdx.x);
+    const Piece p = piece_of(g, sp, blocks);
     const SlabGroups sg = groups_of(g, p);
     const int cpg = sg.cpg;
     const float inv = 1.0f / ((float)g.pixels * (float)cpg);
@@ -565,8 +569,8 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
     if (unit <= kMaxSlab) {
         auto whole = [&](int width) {                     // a multiple of unit
             const int shift = threads_across(width);
-            // four vectors a thread (backward: eight) with as few threads as that takes, or as many as fit
-            for (int few : {backward ? 8 : 4, 16})
+            // eight vectors a thread with as few threads as that takes, or as many as fit
+            for (int few : {8, 16})
                 for (int threads = 256; threads <= 1024; threads *= 2) {
                     const int vectors = (int)ceil_div(pixels, threads >> shift);
                     if (vectors > few || vectors > most_vectors(bf16, backward, threads)) continue;
@@ -578,17 +582,20 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
             return false;
         };
         auto units = [&](int width) { return width < unit ? unit : width / unit * unit; };
-        // Two pixels a thread at least, with wider slabs; or enough work-groups for all compute units, with narrower ones.  us, 512 threads unless stated, width 64 / others:
-        // 256 x 196 x 256 13.0 / 14.0 (128), 17.1 (32); 1000 x 16 x 256 with 256 threads 10.9 / 6.5 (256); 4 x 784 x 128 11.5 / 7.8 (32), 6.1 (16), 5.9 (8).
+        // Two pixels a thread at least, with wider slabs; or two work-groups for each compute unit (backward, where sums of more work-groups cost more: one), with narrower ones, which read
+        // no more from memory as the slabs of an image are on one XCD.  Where there is more than a few MB: of 16 channels at least (backward: 64 bytes), and not with fewer work-groups than
+        // compute units.  us, width (threads): 256 x 196 x 256 13.2 at 64 (256), 13.5 at 32 (256), 15.8 at 16 (256); 1000 x 16 x 256 11.0 at 64 (256), 6.4 at 256 (256); 128 x 784 x 128 15.3
+        // at 64 (512), 13.8 at 32 (512), 14.2 at 16 (256); 64 x 3136 x 64 21.2 at 32 (1024), 17.5 at 16 (512), 22.0 at 8 (512), in pieces 22; 4 x 784 x 128 10.4 at 64 (512), 5.6 at 8 (512);
+        // backward, sums of the channels included, 16 x 3136 x 256 30.3 at 16 (512), in pieces 28.9.
+        const bool much = N * pixels * C * (bf16 ? 2 : 4) > (8 << 20);
+        const int least = !much ? 8 : backward && bf16 ? 32 : 16;
         int width = wide;
         while (2 * (256 >> threads_across(width)) > pixels && width < 256 && N * ceil_div(C, 2 * width) >= 256) width *= 2;
-        while (width > 8 && N * ceil_div(C, width) < 256) width /= 2;
+        while (width > least && N * ceil_div(C, width) < (backward ? 256 : 512)) width /= 2;
         if (width > C) width = C / 8 * 8;
-        // half lines and less are read at half the rate and less, and a few work-groups of many pixels leave compute units idle: not where there is more than a few MB
-        const bool much = N * pixels * C * (bf16 ? 2 : 4) > (8 << 20);
         for (; width >= 8; width /= 2) {
             const int w = units(width);
-            if (much && (w * (bf16 ? 2 : 4) < 64 || N * ceil_div(C, w) < 256)) break;
+            if (much && (w < least || N * ceil_div(C, w) < 256)) break;
             if (whole(w)) return p;
             if (w > width) break;
         }
