@@ -479,8 +479,8 @@ size_t ab_grad_norm_workspace_bytes(int n);
  * X [M, n], W [m, n], residual, Y, Z_save [M, m] bf16, bias [m] fp32; bias, residual, dropout may be NULL, and so may Z_save, which receives Z rounded to
  * bf16 (what lr_dense_bwd needs where there is an activation).  Y comes from Z before it is rounded; the only rounding is Y's own.
  * A factored layer has the same end with two calls, T = lr_dense_fwd(X, B) and Y = lr_dense_fwd(T, A, bias, ..).
- *   act: ABT_ACT_RELU max(z, 0), ABT_ACT_GELU z Phi(z), ABT_ACT_GELU_TANH its form with tanh, ABT_ACT_SILU z / (1 + exp(-z)), in fp32.  NaN stays NaN; at
- *   infinities the last three are what the formulas give in floating point, which may be NaN.
+ *   act: ABT_ACT_RELU max(z, 0), ABT_ACT_GELU z Phi(z), ABT_ACT_GELU_TANH its form with tanh, ABT_ACT_SILU z / (1 + exp(-z)), in fp32.  NaN stays NaN, and
+ *   infinity infinity; at minus infinity, and for the slopes at either, the last three are what the formulas give in floating point, which may be NaN.
  *   dropout: see abt_dropout; element (i, j) of Y is element i m + j of its mask.
  * lr_dense_bwd, from dY [M, m] bf16 and the forward's X, W, Z (bf16, NULL without an activation), act and dropout:
  *     dZ = act'(Z) drop(dY),   dX = dZ W (bf16),   dW = dZ^T X [m, n],   dbias = sum of the rows of dZ [m]   (fp32; accumulate != 0 adds into dW and dbias)

@@ -29,7 +29,7 @@ __device__ __forceinline__ float activate(float z) {
     if constexpr (ACT == ABT_ACT_GELU) {
         float density;
         const float tail = normal_tail(z, density);
-        return __builtin_fmaxf(z, 0.0f) - __builtin_fabsf(z) * tail;               // (a NaN is in the tail too)
+        return __builtin_fmaxf(z, 0.0f) - __builtin_fminf(__builtin_fabsf(z), 16.0f) * tail;       // (beyond 16 the tail is 0, also at infinity; a NaN is in it)
     }
     if constexpr (ACT == ABT_ACT_GELU_TANH) return z * tanh_gate(z);
     if constexpr (ACT == ABT_ACT_SILU) return z * sigmoid(z);

@@ -131,3 +131,27 @@ def test_backward(M, m, n, act, p):
 @pytest.mark.parametrize("p", (None, 0.3))
 def test_backward_epilogues(M, act, p):
     check_backward(make(M, 104, 80, 4), act, p)
+
+
+@pytest.mark.parametrize("M", (3, 48, 200))
+@pytest.mark.parametrize("act", ACTS)
+def test_sums_that_are_not_finite(M, act):
+    """Infinity stays infinity, minus infinity is no infinity behind the smooth activations, NaN stays NaN; the largest and smallest finite sums stay what they are, or 0."""
+    import torch
+    m, n = 40, 1024
+    X, W = torch.zeros((M, n)), torch.zeros((m, n))
+    X[:, 0] = 1.0
+    special = [float("inf"), -float("inf"), float("nan"), 2.0 ** 127, -2.0 ** 127, 2.0 ** 64, -2.0 ** 64, 20.0, -200.0]
+    W[:len(special), 0] = torch.tensor(special)
+    Y, Z = abt.lr_dense_fwd(X.bfloat16().cuda(), W.bfloat16().cuda(), act=act, save_Z=True)
+    Y, Z = Y.float().cpu(), Z.float().cpu()
+    assert bool((Y == Y[0]).logical_or(Y.isnan()).all()) and bool((Z[:, 3:len(special)] == torch.tensor(special[3:])).all())
+    y = Y[0]
+    assert y[0] == float("inf") and bool(y[2].isnan()) and [float(v) for v in y[3:9:2]] == special[3:9:2]
+    if act == "none":
+        assert [float(v) for v in y[4:9:2]] == special[4:9:2] and y[1] == -float("inf")
+    else:
+        assert bool((y[4:9:2].abs() < 1e-30).all()) and not bool(y[1].isinf())
+        if act in ("relu", "gelu"):
+            assert y[1] == 0
+    assert bool((y[len(special):] == 0).all())
