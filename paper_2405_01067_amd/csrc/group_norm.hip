@@ -5,8 +5,8 @@
 // otherwise pieces of the pixels leave sums per channel in a first launch and are normalised in a second, which reads again.
 // Threads: eight channels each, TC of them (a power of two) across the slab, the others down the pixels.
 // Bound by memory and, little less, by vector work: a value is looked at three times, 16 instructions forward (silu) and 17 backward (relu) where there is one pass over memory; loads,
-// sums and stores of a work-group follow each other, and two work-groups or more per compute unit overlap them in part.  us (GB/s): 256 x 196 x 256 bf16 forward 13.5 (3800), 128 x 784 x 128
-// backward 21 (3600) and 4 for the gradients of the channels; in pieces 64 x 3136 x 64 22 and 30, 1 x 4096 x 2048 17.5 and 22; 1 x 49 x 512 fp32 4.0.
+// sums and stores of a work-group follow each other, and two work-groups or more per compute unit overlap them in part.  us (GB/s): 256 x 196 x 256 bf16 forward 13.3 (3900), 64 x 3136 x 64
+// 17.3 (3000), 128 x 784 x 128 backward 20 (3900) and 4 for the gradients of the channels; in pieces 64 x 3136 x 64 backward 30, 1 x 4096 x 2048 17 and 21; 1 x 49 x 512 fp32 4.6.
 #include <climits>
 
 #include "activation.h"
@@ -566,11 +566,12 @@ int threads_across(int width) {                           // as a power of two's
 Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
     Plan p{};
     const int cpg = C / groups, unit = cpg / gcd(cpg, 8) * 8, wide = 64;      // whole groups and vectors; 128 bytes in bf16, 256 in fp32
+    const bool much = N * pixels * C * (bf16 ? 2 : 4) > (8 << 20);            // more than a few MB
     if (unit <= kMaxSlab) {
         auto whole = [&](int width) {                     // a multiple of unit
             const int shift = threads_across(width);
-            // eight vectors a thread with as few threads as that takes, or as many as fit
-            for (int few : {8, 16})
+            // eight vectors a thread (four where there is little) with as few threads as that takes, or as many as fit
+            for (int few : {much || backward ? 8 : 4, 16})
                 for (int threads = 256; threads <= 1024; threads *= 2) {
                     const int vectors = (int)ceil_div(pixels, threads >> shift);
                     if (vectors > few || vectors > most_vectors(bf16, backward, threads)) continue;
@@ -582,16 +583,15 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
             return false;
         };
         auto units = [&](int width) { return width < unit ? unit : width / unit * unit; };
-        // Two pixels a thread at least, with wider slabs; or two work-groups for each compute unit (backward, where sums of more work-groups cost more: one), with narrower ones, which read
-        // no more from memory as the slabs of an image are on one XCD.  Where there is more than a few MB: of 16 channels at least (backward: 64 bytes), and not with fewer work-groups than
-        // compute units.  us, width (threads): 256 x 196 x 256 13.2 at 64 (256), 13.5 at 32 (256), 15.8 at 16 (256); 1000 x 16 x 256 11.0 at 64 (256), 6.4 at 256 (256); 128 x 784 x 128 15.3
-        // at 64 (512), 13.8 at 32 (512), 14.2 at 16 (256); 64 x 3136 x 64 21.2 at 32 (1024), 17.5 at 16 (512), 22.0 at 8 (512), in pieces 22; 4 x 784 x 128 10.4 at 64 (512), 5.6 at 8 (512);
+        // Two pixels a thread at least, with wider slabs; or enough work-groups for all compute units, with narrower ones, which read no more from memory as the slabs of an image are on one
+        // XCD: two each in the forward of more than a few MB.  There 16 channels at least (backward: 64 bytes), and not fewer work-groups than compute units.  us, width (threads):
+        // 256 x 196 x 256 13.2 at 64 (256), 13.5 at 32 (256), 15.8 at 16 (256); 1000 x 16 x 256 11.0 at 64 (256), 6.4 at 256 (256); 128 x 784 x 128 15.3 at 64 (512), 13.8 at 32 (512), 14.2 at 16
+        // (256); 64 x 3136 x 64 21.2 at 32 (1024), 17.5 at 16 (512), 22.0 at 8 (512), in pieces 22; 32 x 49 x 512 4.5 at 64 (256), 6.3 at 16 (256); 4 x 784 x 128 10.4 at 64 (512), 5.6 at 8 (512);
         // backward, sums of the channels included, 16 x 3136 x 256 30.3 at 16 (512), in pieces 28.9.
-        const bool much = N * pixels * C * (bf16 ? 2 : 4) > (8 << 20);
         const int least = !much ? 8 : backward && bf16 ? 32 : 16;
         int width = wide;
         while (2 * (256 >> threads_across(width)) > pixels && width < 256 && N * ceil_div(C, 2 * width) >= 256) width *= 2;
-        while (width > least && N * ceil_div(C, width) < (backward ? 256 : 512)) width /= 2;
+        while (width > least && N * ceil_div(C, width) < (much && !backward ? 512 : 256)) width /= 2;
         if (width > C) width = C / 8 * 8;
         for (; width >= 8; width /= 2) {
             const int w = units(width);
@@ -603,7 +603,7 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
     }
     const int width = C < wide ? C : wide, shift = threads_across(width), slabs = (int)ceil_div(C, width), step = 256 >> shift;
     // Some 512 work-groups, four pixels or more a thread; not more partials than a work-group reads in a few steps.  us, 512 / 1024 of them, forward and backward: 64 x 3136 x 64
-    // 22.7 / 26.9, 29.8 / 40.1; 8 x 1024 x 640 15.5 / 18.1; but 16 x 3136 x 256 22.0 / 21.4, 29.1 / 28.9.
+    // 22.7 / 26.9 (with 32 channels; now whole, 17.2), 29.8 / 40.1; 8 x 1024 x 640 15.5 / 18.1; but 16 x 3136 x 256 backward 29.1 / 28.9.
     int64_t pieces = ceil_div(512, N * slabs);
     const int64_t rows4 = ceil_div(pixels, 4 * step), read = 8192 / (width / cpg + 2);
     if (pieces > rows4) pieces = rows4;
