@@ -584,10 +584,13 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
         };
         auto units = [&](int width) { return width < unit ? unit : width / unit * unit; };
         // Two pixels a thread at least, with wider slabs; or enough work-groups for all compute units, with narrower ones, which read no more from memory as the slabs of an image are on one
-        // XCD: two each in the forward of more than a few MB.  There 16 channels at least (backward: 64 bytes), and not fewer work-groups than compute units.  us, width (threads):
+        // XCD: two each in the forward of more than a few MB.  There 16 channels at least (backward: 64 bytes), and not fewer work-groups than compute units; with less than
+        // that, fewer work-groups only where a work-group does not take longer than two launches.  us, width (threads):
         // 256 x 196 x 256 13.2 at 64 (256), 13.5 at 32 (256), 15.8 at 16 (256); 1000 x 16 x 256 11.0 at 64 (256), 6.4 at 256 (256); 128 x 784 x 128 15.3 at 64 (512), 13.8 at 32 (512), 14.2 at 16
         // (256); 64 x 3136 x 64 21.2 at 32 (1024), 17.5 at 16 (512), 22.0 at 8 (512), in pieces 22; 32 x 49 x 512 4.5 at 64 (256), 6.3 at 16 (256); 4 x 784 x 128 10.4 at 64 (512), 5.6 at 8 (512);
-        // backward, sums of the channels included, 16 x 3136 x 256 30.3 at 16 (512), in pieces 28.9.
+        // 2 x 1024 x 640 12.5 at 40 (512), in pieces 10.7; backward, sums of the channels included, 24.7 and 11.3; 4 x 784 x 128 18.0 at 64 (512), 12.0 at 32, in pieces 10.9, 9.1 at 8 (512);
+        // 16 x 3136 x 256 30.3 at 16 (512), in pieces 28.9.
+        const int64_t most = backward ? 20480 : 32768;    // values of a work-group
         const int least = !much ? 8 : backward && bf16 ? 32 : 16;
         int width = wide;
         while (2 * (256 >> threads_across(width)) > pixels && width < 256 && N * ceil_div(C, 2 * width) >= 256) width *= 2;
@@ -595,7 +598,11 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
         if (width > C) width = C / 8 * 8;
         for (; width >= 8; width /= 2) {
             const int w = units(width);
-            if (much && (w < least || N * ceil_div(C, w) < 256)) break;
+            if (much && w < least) break;
+            if (N * ceil_div(C, w) < 256 && (much || (int64_t)pixels * w > most)) {
+                if (much || w > width) break;
+                continue;
+            }
             if (whole(w)) return p;
             if (w > width) break;
         }
