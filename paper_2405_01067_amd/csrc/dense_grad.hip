@@ -274,15 +274,13 @@ __device__ __forceinline__ void bias_block(const DenseGrads& g, int block, float
     float s = 0.0f;
     if (c < g.m) {
         const float* const from = g.sums + c;
-        int r = part;
-        for (; r + 56 < g.pieces; r += 64) {              // eight loads on their way at a time
+        for (int r = part; r < g.pieces; r += 64) {       // eight loads on their way at a time
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = gload(from + (int64_t)(r + 8 * k) * g.m);
+            for (int k = 0; k < 8; ++k) v[k] = gload(from + (int64_t)(r + 8 * k < g.pieces ? r + 8 * k : r) * g.m);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += v[k];
+            for (int k = 0; k < 8; ++k) s += r + 8 * k < g.pieces ? v[k] : 0.0f;
         }
-        for (; r < g.pieces; r += 8) s += gload(from + (int64_t)r * g.m);
     }
     lds[part][threadIdx.x & 31] = s;
     __syncthreads();

@@ -467,15 +467,13 @@ __device__ __forceinline__ void channel_gradients(const GroupNorm& g, int64_t ro
     const int c = block / 2 * 8 + (threadIdx.x & 7), part = threadIdx.x >> 3;
     const float* const from = g.sums + (block & 1) * rows * g.C + c;          // (C is a multiple of eight)
     float s = 0.0f;
-    int64_t r = part;
-    for (; r + 224 < rows; r += 256) {                    // eight loads on their way at a time
+    for (int64_t r = part; r < rows; r += 256) {          // eight loads on their way at a time
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = gload(from + (r + 32 * k) * g.C);
+        for (int k = 0; k < 8; ++k) v[k] = gload(from + (r + 32 * k < rows ? r + 32 * k : r) * g.C);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += v[k];
+        for (int k = 0; k < 8; ++k) s += r + 32 * k < rows ? v[k] : 0.0f;
     }
-    for (; r < rows; r += 32) s += gload(from + r * g.C);
     lds[part][threadIdx.x & 7] = s;
     __syncthreads();
     if (part) return;
