@@ -589,6 +589,14 @@ Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward)
         // (256); 64 x 3136 x 64 21.2 at 32 (1024), 17.5 at 16 (512), 22.0 at 8 (512), in pieces 22; 32 x 49 x 512 4.5 at 64 (256), 6.3 at 16 (256); 4 x 784 x 128 10.4 at 64 (512), 5.6 at 8 (512);
         // 2 x 1024 x 640 12.5 at 40 (512), in pieces 10.7; backward, sums of the channels included, 24.7 and 11.3; 4 x 784 x 128 18.0 at 64 (512), 12.0 at 32, in pieces 10.9, 9.1 at 8 (512);
         // 16 x 3136 x 256 30.3 at 16 (512), in pieces 28.9.
+        // Backward of more than a few MB, where that makes two work-groups for each compute unit: the widest slab that 256 threads hold.  us, width (threads), without the sums of the channels:
+        // 128 x 784 x 128 24.6 at 32 (256), 25.5 at 64 (512); 256 x 196 x 256 24.7 at 128 (256), 26.6 at 64 (256); 256 x 49 x 512 15.7 at 128 (256), 18.7 at 64 (256).
+        if (backward && much)
+            for (int wider : {256, 128, 64, 32}) {
+                const int w = units(wider), vectors = (int)ceil_div(pixels, 256 >> threads_across(w));
+                if (w > C || N * ceil_div(C, w) < 512 || vectors > most_vectors(bf16, true, 256)) continue;
+                return Plan{Split{w, (int)ceil_div(C, w), threads_across(w), 1, pixels}, 256, vectors};
+            }
         const int64_t most = backward ? 20480 : 32768;    // values of a work-group
         const int least = !much ? 8 : backward && bf16 ? 32 : 16;
         int width = wide;
