@@ -6,7 +6,7 @@
 // Threads: eight channels each, TC of them (a power of two) across the slab, the others down the pixels.
 // Bound by memory and, little less, by vector work: a value is looked at three times, 16 instructions forward (silu) and 17 backward (relu) where there is one pass over memory; loads,
 // sums and stores of a work-group follow each other, and two work-groups or more per compute unit overlap them in part.  us (GB/s): 256 x 196 x 256 bf16 forward 13.3 (3900), 64 x 3136 x 64
-// 17.3 (3000), 128 x 784 x 128 backward 20 (3900) and 4 for the gradients of the channels; in pieces 64 x 3136 x 64 backward 30, 1 x 4096 x 2048 17 and 21; 1 x 49 x 512 fp32 4.6.
+// 17.3 (3000), 128 x 784 x 128 backward, relu, 20 (3900) and 4 for the gradients of the channels; in pieces 64 x 3136 x 64 backward 30, 1 x 4096 x 2048 17 and 21; 1 x 49 x 512 fp32 4.6.
 #include <climits>
 
 #include "activation.h"
