@@ -112,6 +112,13 @@ def test_shapes(shape, dtype, act):
     check(shape, dtype, act)
 
 
+@pytest.mark.parametrize("dtype", ("bfloat16", "float32"))
+@pytest.mark.parametrize("shape", [(70, 1000, 64, 16), (520, 49, 256, 8), (130, 400, 96, 8), (64, 300, 264, 3), (300, 1, 16384, 64), (33, 777, 200, 25)], ids=str)
+def test_more_than_a_few_megabytes(shape, dtype):
+    """Where slabs, threads and vectors are chosen otherwise."""
+    check(shape, dtype, "silu")
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("shape", [(2, 49, 64, 32), (1, 9000, 48, 4)], ids=str)
 def test_activations(shape, act):
