@@ -173,11 +173,14 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
     const Bias first = bias_of(0);
     lds_barrier();                                        // every wave has read its last slab, and nothing is on its way to LDS
     using O = OutRows<L>;
-    if (g.residual && !g.Z) O::load(g.residual, row0, col0, rows, cols, g.Q, wave, lane, lds);       // comes while the rest is computed
+    // Where LDS has room for two tiles of results, Z and Y are made in one pass: Z lies behind Y (1379 rows, 2304 x 768, gelu, Z: 15.5 -> 15.2 us).
+    constexpr int z_at = L::TM * L::TN * 2;
+    constexpr bool both = 2 * z_at <= L::lds;
+    if (g.residual && (both || !g.Z)) O::load(g.residual, row0, col0, rows, cols, g.Q, wave, lane, lds);       // comes while the rest is computed
     const DropKey key = g.drop.state ? drop_key(g.drop) : DropKey{0, 0, 0, 0};
     // Block after block, all the way to LDS: mixed by the scheduler, or with all sums alive across the choice of the activation, 113 registers of the largest tile
     // spilled.
-    auto finish = [&](bool rounded_sum) {
+    auto finish = [&](bool rounded_sum) {                 // Z alone, or Y (and Z)
         Bias bias = first, next = first;
 #pragma unroll
         for (int b = 0; b < CB; ++b) {
@@ -188,6 +191,11 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
                 float v[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = acc[a][b][i] * g.alpha + bias.v[i >> 2][i & 3];
+                if (both && g.Z)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        *reinterpret_cast<u32x4*>(lds + z_at + O::at(r, (c >> 3) + h)) =
+                            u32x4{pack2_bf16(v[8 * h], v[8 * h + 1]), pack2_bf16(v[8 * h + 2], v[8 * h + 3]), pack2_bf16(v[8 * h + 4], v[8 * h + 5]), pack2_bf16(v[8 * h + 6], v[8 * h + 7])};
                 if (!rounded_sum) {
                     if (g.act != ABT_ACT_NONE)
                         with_activation(g.act, [&](auto act) {
@@ -219,7 +227,7 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
         }
         lds_barrier();
     };
-    if (g.Z) {
+    if (!both && g.Z) {
         finish(true);
         O::store(g.Z, row0, col0, rows, cols, g.Q, wave, lane, lds);
         lds_barrier();
@@ -230,6 +238,7 @@ __device__ __forceinline__ void dense_tile(const DenseProduct& g, const Order& o
         lds_barrier();
     }
     finish(false);
+    if (both && g.Z) O::store(g.Z, row0, col0, rows, cols, g.Q, wave, lane, lds + z_at);
     O::store(g.Y, row0, col0, rows, cols, g.Q, wave, lane, lds);
 }
 
