@@ -486,7 +486,7 @@ size_t ab_grad_norm_workspace_bytes(int n);
  *     dZ = act'(Z) drop(dY),   dX = dZ W (bf16),   dW = dZ^T X [m, n],   dbias = sum of the rows of dZ [m]   (fp32; accumulate != 0 adds into dW and dbias)
  *   The residual's gradient is dY.  dX, dW, dbias: any may be NULL; W may then be NULL without dX, X without dW; what is left out changes nothing of the rest.
  *   dZ is rounded to bf16 once for dX (not without an activation or with ABT_ACT_RELU: then it is exact), and enters dW as the sum of three bf16 values, which has
- *   all of fp32, or beyond 9216 rows of two (2.4e-6 of its size off on average).  ABT_ACT_RELU lets dY through where Z > 0 and is 0 elsewhere, whatever dY is there.
+ *   all of fp32.  ABT_ACT_RELU lets dY through where Z > 0 and is 0 elsewhere, whatever dY is there.
  *   Fixed summation order: two calls on the same inputs give bit-identical results.
  * M from 1 to 2^28; m and n multiples of 8, at most 2^20.  bf16 only.  The outputs must not overlap the inputs (but Y may be the residual) or each other.
  * Nothing blocks the host; all calls can be captured.

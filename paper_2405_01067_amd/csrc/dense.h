@@ -27,10 +27,8 @@ struct SmallCost { float longest, load; };
 SmallCost dense_small_cost(int64_t M, int Q, int K);
 hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);        // M <= 64
 
-// What the gradients are made of: dZ = slope(Z) drop(dY) [M, m] as the sum of one, two or three bf16 values.  Without an activation or with ABT_ACT_RELU one is
-// exact (dropout's factor is left to the products).  Otherwise three have all of fp32, and two are 2.4e-6 of the size off on average: two where sums of fp32 products over
-// that many rows, one after the other, are off by about as much (measured with the library's product in fp32: 1.2e-6 at 4200 rows, 1.7e-6 at 9216, 2.0e-6 at 12608).
-constexpr int kDenseThreeValues = 9216;        // rows
+// What the gradients are made of: dZ = slope(Z) drop(dY) [M, m] as the sum of one or three bf16 values.  Without an activation or with ABT_ACT_RELU one is
+// exact (dropout's factor is left to the products).  Otherwise it takes three to have all of fp32.
 // Beside it W^T, and sums of dZ over pieces of the rows.
 struct DenseSlope {
     const uint16_t* dY; const uint16_t* Z; // Z NULL without an activation

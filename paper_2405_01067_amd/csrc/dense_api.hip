@@ -31,7 +31,7 @@ Places places(int64_t M, int64_t m, int64_t n) {
         at = align_up(at + bytes, 256);
     };
     take(p.Wt, (size_t)(m * n * 2));
-    for (int q = 0; q < (M <= kDenseThreeValues ? 3 : 2); ++q) take(p.value[q], (size_t)(M * m * 2));
+    for (int q = 0; q < 3; ++q) take(p.value[q], (size_t)(M * m * 2));
     take(p.sums, (size_t)(ceil_div(M, dense_piece_rows(M, (int)m)) * m * 4));
     take(p.parts, dense_part_bytes(M, (int)n, (int)m));
     take(p.partials, dense_grad_partial_bytes(M, (int)m, (int)n));
@@ -83,7 +83,7 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
 
     DenseSlope z{};
     z.dY = (const uint16_t*)dY; z.Z = act == ABT_ACT_NONE ? nullptr : (const uint16_t*)Z;
-    const int values = !smooth ? 1 : M <= kDenseThreeValues ? 3 : 2;
+    const int values = smooth ? 3 : 1;
     if ((dX || dW) && (z.Z || drop.state))
         for (int q = 0; q < (dW ? values : 1); ++q) z.value[q] = (uint16_t*)(ws + at.value[q]);
     if (dbias) z.sums = (float*)(ws + at.sums);

@@ -421,7 +421,7 @@ hipError_t launch_dense_slope(const DenseSlope& p, hipStream_t s) {
 
 size_t dense_grad_partial_bytes(int64_t M, int m, int n) {
     int splits = 1;
-    for (int values = 1; values <= 3; ++values) {
+    for (int values : {1, 3}) {
         const int k = grad_way(M, m, n, values).order.splits;
         if (k > splits) splits = k;
     }
@@ -439,12 +439,12 @@ hipError_t launch_dense_bwd(const DenseProduct& x, const DenseGrads& g, hipStrea
     const float dw = grad_cost(kGrads[2], o, g.m, g.n, values), longest = c.longest > dw ? c.longest : dw;
     const float load = c.load + (float)o.tiles / 256.0f * ((float)o.slabs * (kGrads[2].slab + (float)values * kGrads[2].value) + kGrads[2].rest);
     const float apart = dense_cost(x.M, x.Q, x.K) + w.cost + 1.7f;
-    if (longest < apart && 0.9f * load < apart) return values == 3 ? launch_few_rows<3>(x, g, s) : values == 2 ? launch_few_rows<2>(x, g, s) : launch_few_rows<1>(x, g, s);
+    if (longest < apart && 0.9f * load < apart) return values == 3 ? launch_few_rows<3>(x, g, s) : launch_few_rows<1>(x, g, s);
 
     hipError_t e = x.Y ? launch_dense(x, s) : hipSuccess;
     if (e != hipSuccess) return e;
     if (g.dW) {
-        e = values == 3 ? launch_grad<3>(g, w, s) : values == 2 ? launch_grad<2>(g, w, s) : launch_grad<1>(g, w, s);
+        e = values == 3 ? launch_grad<3>(g, w, s) : launch_grad<1>(g, w, s);
         if (e != hipSuccess) return e;
     }
     const int64_t blocks = g.dW && w.order.splits > 1 ? ceil_div((int64_t)g.m * g.n, 1024) : 0, more = g.dbias ? ceil_div(g.m, 32) : 0;
