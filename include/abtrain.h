@@ -485,8 +485,8 @@ size_t ab_grad_norm_workspace_bytes(int n);
  * lr_dense_bwd, from dY [M, m] bf16 and the forward's X, W, Z (bf16, NULL without an activation), act and dropout:
  *     dZ = act'(Z) drop(dY),   dX = dZ W (bf16),   dW = dZ^T X [m, n],   dbias = sum of the rows of dZ [m]   (fp32; accumulate != 0 adds into dW and dbias)
  *   The residual's gradient is dY.  dX, dW, dbias: any may be NULL; W may then be NULL without dX, X without dW; what is left out changes nothing of the rest.
- *   dZ is rounded to bf16 once for dX (not without an activation or with ABT_ACT_RELU: then it is exact), and enters dW as the sum of three bf16 values, which has
- *   all of fp32.  ABT_ACT_RELU lets dY through where Z > 0 and is 0 elsewhere, whatever dY is there.
+ *   dZ is exact without an activation or with ABT_ACT_RELU; otherwise it enters dW with all of fp32 and dX with 16 bits of it, as sums of bf16 values (infinities of X and W
+ *   become those of the gradients).  ABT_ACT_RELU lets dY through where Z > 0 and is 0 elsewhere, whatever dY is there.
  *   Fixed summation order: two calls on the same inputs give bit-identical results.
  * M from 1 to 2^28; m and n multiples of 8, at most 2^20.  bf16 only.  The outputs must not overlap the inputs (but Y may be the residual) or each other.
  * Nothing blocks the host; all calls can be captured.

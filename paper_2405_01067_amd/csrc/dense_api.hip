@@ -22,7 +22,7 @@ int check_dense(int64_t M, int64_t m, int64_t n, int act, const abt_dropout* dro
     return sizes_fit(M, m, n) ? ABT_OK : ABT_ESHAPE;
 }
 
-struct Places { size_t Wt, value[3], sums, parts, partials, bytes; };
+struct Places { size_t Wt, two, third, sums, parts, partials, bytes; };
 Places places(int64_t M, int64_t m, int64_t n) {
     Places p{};
     size_t at = 0;
@@ -30,10 +30,12 @@ Places places(int64_t M, int64_t m, int64_t n) {
         where = at;
         at = align_up(at + bytes, 256);
     };
-    take(p.Wt, (size_t)(m * n * 2));
-    for (int q = 0; q < 3; ++q) take(p.value[q], (size_t)(M * m * 2));
+    take(p.Wt, (size_t)(m * n * 4));                      // twice; and two parts of dZ beside each other, and the third
+    take(p.two, (size_t)(M * m * 4));
+    take(p.third, (size_t)(M * m * 2));
     take(p.sums, (size_t)(ceil_div(M, dense_piece_rows(M, (int)m)) * m * 4));
-    take(p.parts, dense_part_bytes(M, (int)n, (int)m));
+    const size_t once = dense_part_bytes(M, (int)n, (int)m), twice = dense_part_bytes(M, (int)n, (int)(2 * m));
+    take(p.parts, once > twice ? once : twice);
     take(p.partials, dense_grad_partial_bytes(M, (int)m, (int)n));
     p.bytes = at;
     return p;
@@ -84,15 +86,18 @@ int lr_dense_bwd(const void* dY, const void* X, const void* W, const void* Z, vo
     DenseSlope z{};
     z.dY = (const uint16_t*)dY; z.Z = act == ABT_ACT_NONE ? nullptr : (const uint16_t*)Z;
     const int values = smooth ? 3 : 1;
-    if ((dX || dW) && (z.Z || drop.state))
-        for (int q = 0; q < (dW ? values : 1); ++q) z.value[q] = (uint16_t*)(ws + at.value[q]);
+    if ((dX || dW) && (z.Z || drop.state)) {
+        z.value[0] = (uint16_t*)(ws + at.two);
+        if (values > 1) z.value[1] = z.value[0] + m;
+        if (values > 1 && dW) z.value[2] = (uint16_t*)(ws + at.third);
+    }
     if (dbias) z.sums = (float*)(ws + at.sums);
     if (dX) { z.W = (const uint16_t*)W; z.Wt = (uint16_t*)(ws + at.Wt); }
-    z.M = M; z.m = (int)m; z.n = (int)n; z.act = act; z.scaled = smooth; z.rows = dense_piece_rows(M, (int)m); z.drop = drop;
+    z.values = values; z.M = M; z.m = (int)m; z.n = (int)n; z.act = act; z.scaled = smooth; z.rows = dense_piece_rows(M, (int)m); z.drop = drop;
     if (launch_dense_slope(z, s) != hipSuccess) return ABT_EHIP;
     const uint16_t* const dZ = z.value[0] ? z.value[0] : z.dY;
     const float alpha = smooth ? 1.0f : drop.scale;       // what dZ was left without
-    const DenseProduct x{dZ, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f}, (float*)(ws + at.parts), 0};
+    const DenseProduct x{dZ, z.Wt, (uint16_t*)dX, nullptr, nullptr, nullptr, M, (int)n, pitch_of(values) * (int)m, ABT_ACT_NONE, alpha, Drop{nullptr, 0, 0, 1.0f}, (float*)(ws + at.parts), 0};
     const DenseGrads g{{dZ, z.value[1], z.value[2]}, (const uint16_t*)X, dW, (float*)(ws + at.partials), z.sums, dbias, M, (int)m, (int)n, (int)ceil_div(M, z.rows), accumulate, values, alpha};
     return launch_dense_bwd(x, g, s) == hipSuccess ? ABT_OK : ABT_EHIP;
 }

@@ -19,14 +19,21 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
         v[2 * k + 1] = __builtin_bit_cast(float, w[k] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) { return u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])}; }
 
-// what is left of eight values behind their rounding to bf16: 0 where that is not finite (infinities and NaN are in it)
-__device__ __forceinline__ void rest_of(u32x4 rounded, float (&v)[8]) {
-    float h[8];
-    unpack8(rounded, h);
+// The next part of eight values: the leading eight bits of what is left of each, which loses them.  Nothing is left of what is not finite (infinities and NaN are in the first part).
+__device__ __forceinline__ u32x4 cut8(const float (&v)[8], float (&left)[8]) {
+    uint32_t part[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = __builtin_fabsf(h[k]) < __builtin_inff() ? v[k] - h[k] : 0.0f;
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t sign = __builtin_bit_cast(uint32_t, v[k]) & 0x80000000u, least = v[k] == 0.0f ? 0 : 0x10000u;
+        const uint32_t size = __builtin_bit_cast(uint32_t, left[k]) & 0x7fff0000u;
+        part[k] = (size > least ? size : least) | sign;
+        left[k] = size < 0x7f800000u ? left[k] - __builtin_bit_cast(float, size | sign) : 0.0f;
+    }
+    u32x4 out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) out[k] = part[2 * k] >> 16 | part[2 * k + 1];
+    return out;
 }
 
 __device__ __forceinline__ void slope_piece(const DenseSlope& g, int piece, int col0, float (*sums)[kSlopeCols]) {
@@ -67,12 +74,14 @@ __device__ __forceinline__ void slope_piece(const DenseSlope& g, int piece, int 
 #pragma unroll
                 for (int k = 0; k < 8; ++k) total[k] += v[k];
                 if (!g.value[0]) continue;
+                float left[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) left[k] = v[k];
 #pragma unroll
                 for (int q = 0; q < 3; ++q) {
                     if (!g.value[q]) break;
-                    const u32x4 rounded = pack8(v);
-                    gstore(reinterpret_cast<u32x4*>(g.value[q] + at), rounded);
-                    rest_of(rounded, v);
+                    const int64_t to = q < 2 ? (r + 4 * i) * pitch_of(g.values) * g.m + col : at;
+                    gstore(reinterpret_cast<u32x4*>(g.value[q] + to), cut8(v, left));
                 }
             }
         }
@@ -99,7 +108,9 @@ __device__ __forceinline__ void transpose_block(const DenseSlope& g, int block, 
         u32x4 v;
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = (uint32_t)tile[r + 2 * k][c] | (uint32_t)tile[r + 2 * k + 1][c] << 16;
-        gstore(reinterpret_cast<u32x4*>(g.Wt + (int64_t)(c0 + c) * g.m + r0 + r), v);
+        uint16_t* const to = g.Wt + (int64_t)(c0 + c) * pitch_of(g.values) * g.m + r0 + r;
+        gstore(reinterpret_cast<u32x4*>(to), v);
+        if (g.values > 1) gstore(reinterpret_cast<u32x4*>(to + g.m), v);
     }
 }
 
@@ -154,21 +165,26 @@ __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& 
         const int pos = (j * NW + wave) * 64 + lane, r = pos / (width / 8), c = ((pos % (width / 8)) ^ L::turn(width, r)) * 8;
         return c < cols ? (r * pitch + c) * 2 : kBufNowhere;
     };
-    int poff[L::NP], qoff[L::NQ];
+    constexpr int KINDS = L::VALUES == 1 ? 1 : 2;         // the first and second part have rows of their own pitch
+    const int pitch[2] = {pitch_of(L::VALUES) * g.m, g.m};
+    int poff[KINDS][L::NP], qoff[L::NQ];
 #pragma unroll
-    for (int j = 0; j < L::NP; ++j) poff[j] = lane_offset(L::TP, g.m, pcols, j);
+    for (int k = 0; k < KINDS; ++k)
+#pragma unroll
+        for (int j = 0; j < L::NP; ++j) poff[k][j] = lane_offset(L::TP, pitch[k], pcols, j);
 #pragma unroll
     for (int j = 0; j < L::NQ; ++j) qoff[j] = lane_offset(L::TQ, g.n, qcols, j);
     u32x4 pnext[L::VALUES][L::NP], qnext[L::NQ];          // the slab on its way
     auto request = [&](int s) {
         const int64_t row = first + (int64_t)s * 32;
         const int rows = last - row < 32 ? (int)(last - row) : 32;            // rows past the last one read zeros
-        const int64_t pbytes = ((int64_t)(rows - 1) * g.m + pcols) * 2, qbytes = ((int64_t)(rows - 1) * g.n + qcols) * 2;
+        const int64_t qbytes = ((int64_t)(rows - 1) * g.n + qcols) * 2;
 #pragma unroll
         for (int q = 0; q < L::VALUES; ++q) {
-            const rsrc_t res = make_rsrc(g.value[q] + row * g.m + p0, pbytes);
+            const int k = q / 2;
+            const rsrc_t res = make_rsrc(g.value[q] + row * pitch[k] + p0, ((int64_t)(rows - 1) * pitch[k] + pcols) * 2);
 #pragma unroll
-            for (int j = 0; j < L::NP; ++j) pnext[q][j] = buf_load16(res, poff[j], 0);
+            for (int j = 0; j < L::NP; ++j) pnext[q][j] = buf_load16(res, poff[k][j], 0);
         }
         const rsrc_t res = make_rsrc(g.X + row * g.n + q0, qbytes);
 #pragma unroll
