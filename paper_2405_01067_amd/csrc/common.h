@@ -10,6 +10,7 @@
 
 #include "abtrain.h"
 #include "grad_table.h"
+#include "int_util.h"
 
 namespace abt {
 
@@ -114,8 +115,6 @@ __device__ __forceinline__ void load_lds16(rsrc_t r, unsigned char* dst, int lan
 // 16 consecutive columns of the result, 16 (lane / 32) .. + 15.
 __device__ __forceinline__ int out_row(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // Do two byte ranges share memory?  (A caller may hand in an output that lies over an input, as far as everything
 // that reads the input is done before the output is written.)
 inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {

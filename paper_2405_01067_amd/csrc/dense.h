@@ -1,6 +1,7 @@
 // The dense layer with bias, activation, dropout and residual (dense_tile.hip, dense_few.hip, dense_grad.hip): what dense_api.hip calls.
 #pragma once
 
+#include "dense_way.h"
 #include "dropout.h"
 
 namespace abt {
@@ -19,12 +20,7 @@ struct DenseProduct {
     float* parts;                          // dense_part_bytes(M, Q, K)
     int piece;                             // set by the launchers: slabs of 64 columns of a piece of the contraction
 };
-size_t dense_part_bytes(int64_t M, int Q, int K);
 hipError_t launch_dense(const DenseProduct& p, hipStream_t s);
-// What it costs, us, without an epilogue, and with tiles of 64 x 64: the longest of them, and what they keep the chip busy
-float dense_cost(int64_t M, int Q, int K);
-struct SmallCost { float longest, load; };
-SmallCost dense_small_cost(int64_t M, int Q, int K);
 hipError_t launch_dense_few(const DenseProduct& p, hipStream_t s);        // M <= 64
 
 // What the gradients are made of: dZ = slope(Z) drop(dY) [M, m] as the sum of bf16 values.  Without an activation or with ABT_ACT_RELU one is exact (dropout's factor is

@@ -2,7 +2,6 @@
 // 12608 rows, 2304 x 768, gelu (two values): dZ 46 us, bound by memory (232 MB at 5.0 TB/s); dX 53 (dense_tile.hip); dW 96 (89 GFLOP of two products at 930 TFLOP/s, and 64 MB of partials);
 // their sum 13 (5.2 TB/s).  394 rows, 768 x 768, silu (three values): dZ 5.8 us, everything else 9.5: latency.
 #include <climits>
-#include <cmath>
 
 #include "dense_tile.h"
 
@@ -146,8 +145,6 @@ __device__ __forceinline__ u32x4 read_operand(const unsigned char* at, int back)
     const u32x2 a = half(at), b = half(at + back);
     return u32x4{a[0], a[1], b[0], b[1]};
 }
-
-struct GradOrder { int col_tiles, tiles, splits, slabs; };       // pieces of the rows and their length in slabs
 
 template <class L>
 __device__ __forceinline__ void grad_tile(const DenseGrads& g, const GradOrder& o, int block, unsigned char* lds) {
@@ -349,40 +346,6 @@ template <int V> using Grad256 = GradTile<256, 256, 4, 2, V>;
 template <int V> using Grad128 = GradTile<128, 128, 2, 2, V>;
 template <int V> using Grad64 = GradTile<64, 64, 2, 2, V>;
 
-// What a tile of dW costs, us, as kTiles of dense_tile.hip has it for the forward: a slab and what each value adds to it, the rest, the same where a work-group has the compute
-// unit to itself, and the sum of the partials as a launch and per million of them.  Fitted to launches of all three in 1 to 32 pieces of the rows at 48 shapes (24 to 12608 rows, 32 to 5920
-// columns; 650 times); what the rule takes is 2 % slower than the fastest on average (26 % at worst: 1156 rows, 1200 x 480).  us (pieces), two values unless stated:
-//                                   256            128           64
-//   394 rows, 768 x 768, three     24.5 (3)       14.4 (2)       8.5 (1)
-//   2000 rows, 1024 x 1024         36.1 (8)       26.8 (3)      24.1 (2)
-//   11737 rows, 352 x 3112         83.9 (9)       77.7 (6)     102.5 (3)
-//   12608 rows, 2304 x 768          108 (8)        117 (4)       161 (2)      830 TFLOP/s; one value 74, 79, 118
-//   4096 rows, 4096 x 4096          228 (1)        283 (1)       389 (1)     1210 TFLOP/s; three values 323, 387, 530
-struct GradCost { int t, per_cu; float slab, value, rest, alone_slab, alone_value, alone_rest, join, partial; };
-constexpr GradCost kGrads[] = {{256, 1, 0.67f, 0.095f, 0.0f, 0.20f, 0.55f, 6.1f, 1.6f, 2.07f}, {128, 2, 0.04f, 0.216f, 1.0f, 0.23f, 0.185f, 4.1f, 1.8f, 2.15f},
-                               {64, 3, 0.13f, 0.037f, 2.45f, 0.15f, 0.079f, 3.9f, 1.7f, 0.98f}};
-struct GradWay { int tile; GradOrder order; float cost; };
-GradOrder grad_order(int t, int64_t M, int m, int n, int64_t splits) {
-    const int64_t slabs = ceil_div(M, 32), each = ceil_div(slabs, splits);
-    return GradOrder{(int)ceil_div(n, t), (int)(ceil_div(m, t) * ceil_div(n, t)), (int)ceil_div(slabs, each), (int)each};
-}
-float grad_cost(const GradCost& t, const GradOrder& o, int m, int n, int values) {
-    const float groups = (float)o.tiles * (float)o.splits, slabs = (float)o.slabs, v = (float)values;
-    const float shared = ceilf(groups / 256.0f) * (slabs * (t.slab + v * t.value) + t.rest);
-    const float alone = ceilf(groups / (256.0f * (float)t.per_cu)) * (slabs * (t.alone_slab + v * t.alone_value) + t.alone_rest);
-    return (shared > alone ? shared : alone) + (o.splits > 1 ? t.join + 1e-6f * t.partial * (float)o.splits * (float)m * (float)n : 0.0f);
-}
-GradWay grad_way(int64_t M, int m, int n, int values) {
-    GradWay best{0, {}, 1e30f};
-    for (int i = 0; i < 3; ++i)
-        for (int64_t splits = 1; splits <= 32 && (splits == 1 || splits * 4 <= ceil_div(M, 32)); ++splits) {
-            const GradOrder o = grad_order(kGrads[i].t, M, m, n, splits);
-            const float c = grad_cost(kGrads[i], o, m, n, values);
-            if (c < best.cost) best = GradWay{i, o, c};
-        }
-    return best;
-}
-
 template <class L, int PER_CU>
 hipError_t launch_grad(const DenseGrads& p, const GradOrder& o, hipStream_t s) {
     static std::atomic<bool> attr_set{false};
@@ -446,16 +409,7 @@ size_t dense_grad_partial_bytes(int64_t M, int m, int n) {
 hipError_t launch_dense_bwd(const DenseProduct& x, const DenseGrads& g, hipStream_t s) {
     const int values = g.values;
     const GradWay w = grad_way(g.M, g.m, g.n, values);
-    // Together: the longest work-group, or what all of them keep the chip busy; apart: one after the other.  Of 56 shapes (8 to 4000 rows) what this takes is 0.5 % slower than
-    // the other on average (33 % at worst).  us, together / apart: 394 rows, 768 x 768, three values 9.4 / 17.5; 1000 rows, 2304 x 768 26.8 / 38.2; 1500 rows, 512 x 512 24.3 / 18.8;
-    // 4000 rows, 256 x 256, two values 54.6 / 15.4.
-    // (As if all three were wanted: what is not changes no sums.)
-    const SmallCost c = dense_small_cost(x.M, x.Q, x.K);
-    const GradOrder o = grad_order(64, g.M, g.m, g.n, 1);
-    const float dw = grad_cost(kGrads[2], o, g.m, g.n, values), longest = c.longest > dw ? c.longest : dw;
-    const float load = c.load + (float)o.tiles / 256.0f * ((float)o.slabs * (kGrads[2].slab + (float)values * kGrads[2].value) + kGrads[2].rest);
-    const float apart = dense_cost(x.M, x.Q, x.K) + w.cost + 1.7f;
-    if (longest < apart && 0.9f * load < apart) return values == 3 ? launch_few_rows<3>(x, g, s) : launch_few_rows<1>(x, g, s);
+    if (dense_together(g.M, g.m, g.n, x.K, values)) return values == 3 ? launch_few_rows<3>(x, g, s) : launch_few_rows<1>(x, g, s);
 
     hipError_t e = x.Y ? launch_dense(x, s) : hipSuccess;
     if (e != hipSuccess) return e;
