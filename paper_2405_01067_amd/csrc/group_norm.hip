@@ -11,16 +11,12 @@
 
 #include "activation.h"
 #include "group_norm.h"
+#include "group_norm_plan.h"
 #include "nt_tile.h"
 #include "vec8.h"
 
 namespace abt {
 namespace {
-
-constexpr int kMaxSlab = 512;                             // channels: 64 threads across
-
-// Slabs of the channels, of `width` each (the last may have fewer) and TC = 2^shift threads across; pieces of the pixels
-struct Split { int width, slabs, shift, pieces, rows; };
 
 __device__ __forceinline__ float lanes_sum(float v, int from, int to) {      // over lanes whose numbers differ in the bits from .. to / 2
     for (int d = from; d < to; d <<= 1) v += __shfl_xor(v, d);
@@ -65,7 +61,7 @@ __device__ __forceinline__ void by_group(int groups, int entries, F&& f) {
 // ------------------------------------------------------------------------------------------ everything at once
 // Pixel r of NV: row + r step, where row = thread / TC.  U: units of a thread's eight channels; a group is a whole number of units.
 template <bool BF16, int THREADS, int NV, int U>
-__global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g, const Split sp) {
+__global__ __launch_bounds__(THREADS) void gn_whole_fwd_kernel(const GroupNorm g, const GroupSplit sp) {
     extern __shared__ float lds[];
     const int pitch = sp.width;
     float *const waves = lds, *const chan = waves + THREADS / 64 * pitch, *const stat = chan + pitch;
@@ -164,7 +160,7 @@ __device__ __forceinline__ Slopes slopes_of(const Front& f, float rstd, float fi
 
 // sums [2, N, C] of dpre and of dpre x^
 template <bool BF16, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g, const Split sp) {
+__global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g, const GroupSplit sp) {
     extern __shared__ float lds[];
     const int pitch = sp.width;
     float *const waves = lds, *const chan = waves + 2 * (THREADS / 64) * pitch, *const stat = chan + 2 * pitch;
@@ -251,7 +247,7 @@ __global__ __launch_bounds__(THREADS) void gn_whole_bwd_kernel(const GroupNorm g
 
 // ------------------------------------------------------------------------------------------ in pieces
 struct Piece { int c0, width, piece, tc, first, last, step; int64_t image, base; bool there; };
-__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const Split& sp, unsigned blocks) {
+__device__ __forceinline__ Piece piece_of(const GroupNorm& g, const GroupSplit& sp, unsigned blocks) {
     Piece p;
     unsigned block = xcd_order(blockIdx.x, blocks);
     const int slab = (int)(block % (unsigned)sp.slabs);
@@ -299,15 +295,15 @@ __device__ __forceinline__ SlabGroups groups_of(const GroupNorm& g, const Piece&
     const int cpg = g.C / g.groups, first = p.c0 / cpg;
     return SlabGroups{cpg, first, (p.c0 + p.width - 1) / cpg - first + 1};
 }
-__device__ __forceinline__ int slots(const GroupNorm& g, const Split& sp) { return g.groups + sp.slabs; }
+__device__ __forceinline__ int slots(const GroupNorm& g, const GroupSplit& sp) { return g.groups + sp.slabs; }
 // where the slots of an image's piece begin
-__device__ __forceinline__ const float* slots_of(const float* sums, const GroupNorm& g, const Split& sp, int64_t image, int piece) {
+__device__ __forceinline__ const float* slots_of(const float* sums, const GroupNorm& g, const GroupSplit& sp, int64_t image, int piece) {
     return sums + (image * sp.pieces + piece) * slots(g, sp) * 2;
 }
 
 // per slot: the mean of a piece's pixels in the group's channels in this slab, and the squares around it
 template <bool BF16>
-__global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const Split sp) {
+__global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const GroupSplit sp) {
     __shared__ float waves[4 * kMaxSlab], chan[kMaxSlab], means[kMaxSlab];
     const Piece p = piece_of(g, sp, gridDim.x);
     const SlabGroups sg = groups_of(g, p);
@@ -361,14 +357,14 @@ __global__ __launch_bounds__(256) void gn_pieces_kernel(const GroupNorm g, const
 
 // f(slab, piece) for this lane's share of the partials of group q
 template <class F>
-__device__ __forceinline__ void by_partial(const SlabGroups& sg, const Split& sp, int q, int l, int lanes, F&& f) {
+__device__ __forceinline__ void by_partial(const SlabGroups& sg, const GroupSplit& sp, int q, int l, int lanes, F&& f) {
     const int s0 = q * sg.cpg / sp.width, s1 = ((q + 1) * sg.cpg - 1) / sp.width, touched = s1 - s0 + 1;
     for (int e = l; e < sp.pieces * touched; e += lanes) f(s0 + e % touched, e / touched);
 }
-__device__ __forceinline__ int partials(const SlabGroups& sg, const Split& sp) { return sp.pieces * ((sg.cpg + sp.width - 2) / sp.width + 1); }      // at most
+__device__ __forceinline__ int partials(const SlabGroups& sg, const GroupSplit& sp) { return sp.pieces * ((sg.cpg + sp.width - 2) / sp.width + 1); }      // at most
 
 template <bool BF16>
-__global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const Split sp) {
+__global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const GroupSplit sp) {
     __shared__ float stat[2][kMaxSlab];
     const Piece p = piece_of(g, sp, gridDim.x);
     const SlabGroups sg = groups_of(g, p);
@@ -415,9 +411,9 @@ __global__ __launch_bounds__(256) void gn_apply_kernel(const GroupNorm g, const 
 }
 
 // sums [2, N pieces, C] of dpre and of dpre x^, and behind them per slot the same times the gain, over the group's channels in this slab
-__device__ __forceinline__ float* slot_base(const GroupNorm& g, const Split& sp) { return g.sums + 2 * g.N * sp.pieces * g.C; }
+__device__ __forceinline__ float* slot_base(const GroupNorm& g, const GroupSplit& sp) { return g.sums + 2 * g.N * sp.pieces * g.C; }
 template <bool BF16>
-__global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, const Split sp) {
+__global__ __launch_bounds__(256) void gn_bwd_pieces_kernel(const GroupNorm g, const GroupSplit sp) {
     __shared__ float waves[8 * kMaxSlab], chan[2 * kMaxSlab];
     const Piece p = piece_of(g, sp, gridDim.x);
     const int cpg = g.C / g.groups;
@@ -482,7 +478,7 @@ __device__ __forceinline__ void channel_gradients(const GroupNorm& g, int64_t ro
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, const Split sp, unsigned blocks) {
+__global__ __launch_bounds__(256) void gn_bwd_apply_kernel(const GroupNorm g, const GroupSplit sp, unsigned blocks) {
     __shared__ float stat[2][kMaxSlab];
     if (blockIdx.x >= blocks) {
         channel_gradients(g, g.N * sp.pieces, (int)(blockIdx.x - blocks), reinterpret_cast<float (*)[8]>(&stat[0][0]));
@@ -550,83 +546,6 @@ __global__ __launch_bounds__(256) void gn_rows_kernel(const GroupNorm g, int64_t
 }
 
 // ------------------------------------------------------------------------------------------ which
-int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
-
-// How a call is split; threads, vectors: of the `whole` kernels, threads = 0 for the others
-struct Plan { Split sp; int threads, vectors; };
-// Vectors that fit a thread's registers: 128 of them with 1024 threads, 256 with fewer; the backward has two tensors
-constexpr int most_vectors(bool bf16, bool backward, int threads) { return (bf16 ? 16 : 8) / (backward && threads == 1024 ? 4 : 1); }
-int threads_across(int width) {                           // as a power of two's exponent
-    int shift = 0;
-    while ((8 << shift) < width) ++shift;
-    return shift;
-}
-Plan plan_of(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
-    Plan p{};
-    const int cpg = C / groups, unit = cpg / gcd(cpg, 8) * 8, wide = 64;      // whole groups and vectors; 128 bytes in bf16, 256 in fp32
-    const bool much = N * pixels * C * (bf16 ? 2 : 4) > (8 << 20);            // more than a few MB
-    if (unit <= kMaxSlab) {
-        auto whole = [&](int width) {                     // a multiple of unit
-            const int shift = threads_across(width);
-            // Forward: four vectors a thread with up to 512 threads; eight with as few threads as that takes; or as many as fit.  us, threads: 64 x 196 x 1024 fp32 25.4 with 512, 26.3 with 256;
-            // 128 x 784 x 128, 32 wide, 13.8 with 512, 14.6 with 1024, 14.9 with 256.
-            for (int few : {4, 8, 16})
-                for (int threads = backward && few == 4 ? 1024 : 256; threads <= (few == 4 ? 512 : 1024); threads *= 2) {
-                    const int vectors = (int)ceil_div(pixels, threads >> shift);
-                    if (vectors > few || vectors > most_vectors(bf16, backward, threads)) continue;
-                    p.sp = Split{width, (int)ceil_div(C, width), shift, 1, pixels};
-                    p.threads = threads;
-                    p.vectors = vectors;
-                    return true;
-                }
-            return false;
-        };
-        auto units = [&](int width) { return width < unit ? unit : width / unit * unit; };
-        // Two pixels a thread at least, with wider slabs; or enough work-groups for all compute units, with narrower ones, which read no more from memory as the slabs of an image are on one
-        // XCD: two each in the forward of more than a few MB.  There 16 channels at least (backward: 64 bytes), and not fewer work-groups than compute units; with less than
-        // that, fewer work-groups only where a work-group does not take longer than two launches.  us, width (threads):
-        // 256 x 196 x 256 13.2 at 64 (256), 13.5 at 32 (256), 15.8 at 16 (256); 1000 x 16 x 256 11.0 at 64 (256), 6.4 at 256 (256); 128 x 784 x 128 15.3 at 64 (512), 13.8 at 32 (512), 14.2 at 16
-        // (256); 64 x 3136 x 64 21.2 at 32 (1024), 17.5 at 16 (512), 22.0 at 8 (512), in pieces 22; 32 x 49 x 512 4.5 at 64 (256), 6.3 at 16 (256); 4 x 784 x 128 10.4 at 64 (512), 5.6 at 8 (512);
-        // 2 x 1024 x 640 12.5 at 40 (512), in pieces 10.7; backward, sums of the channels included, 24.7 and 11.3; 4 x 784 x 128 18.0 at 64 (512), 12.0 at 32, in pieces 10.9, 9.1 at 8 (512);
-        // 16 x 3136 x 256 30.3 at 16 (512), in pieces 28.9.
-        // Backward of more than a few MB, where that makes two work-groups for each compute unit: the widest slab that 256 threads hold.  us, width (threads), without the sums of the channels:
-        // 128 x 784 x 128 24.6 at 32 (256), 25.5 at 64 (512); 256 x 196 x 256 24.7 at 128 (256), 26.6 at 64 (256); 256 x 49 x 512 15.7 at 128 (256), 18.7 at 64 (256).
-        if (backward && much)
-            for (int wider : {256, 128, 64, 32}) {
-                const int w = units(wider), vectors = (int)ceil_div(pixels, 256 >> threads_across(w));
-                if (w > C || N * ceil_div(C, w) < 512 || vectors > most_vectors(bf16, true, 256)) continue;
-                return Plan{Split{w, (int)ceil_div(C, w), threads_across(w), 1, pixels}, 256, vectors};
-            }
-        const int64_t most = backward ? 20480 : 32768;    // values of a work-group
-        const int least = !much ? 8 : backward && bf16 ? 32 : 16;
-        int width = wide;
-        while (2 * (256 >> threads_across(width)) > pixels && width < 256 && N * ceil_div(C, 2 * width) >= 256) width *= 2;
-        while (width > least && N * ceil_div(C, width) < (much && !backward ? 512 : 256)) width /= 2;
-        if (width > C) width = C / 8 * 8;
-        for (; width >= 8; width /= 2) {
-            const int w = units(width);
-            if (much && w < least) break;
-            if (N * ceil_div(C, w) < 256 && (much || (int64_t)pixels * w > most)) {
-                if (much || w > width) break;
-                continue;
-            }
-            if (whole(w)) return p;
-            if (w > width) break;
-        }
-        p = Plan{};
-    }
-    const int width = C < wide ? C : wide, shift = threads_across(width), slabs = (int)ceil_div(C, width), step = 256 >> shift;
-    // Some 512 work-groups, four pixels or more a thread; not more partials than a work-group reads in a few steps.  us, 512 / 1024 of them, forward and backward: 64 x 3136 x 64
-    // 22.7 / 26.9 (with 32 channels; now whole, 17.2), 29.8 / 40.1; 8 x 1024 x 640 15.5 / 18.1; but 16 x 3136 x 256 backward 29.1 / 28.9.
-    int64_t pieces = ceil_div(512, N * slabs);
-    const int64_t rows4 = ceil_div(pixels, 4 * step), read = 8192 / (width / cpg + 2);
-    if (pieces > rows4) pieces = rows4;
-    if (pieces > read) pieces = read;
-    const int rows = (int)ceil_div(pixels, pieces);
-    p.sp = Split{width, slabs, shift, (int)ceil_div(pixels, rows), rows};
-    return p;
-}
-
 // f(g, blocks, last) for launches of fewer than 2^32 threads, some images each
 template <class F>
 hipError_t by_images(GroupNorm g, int64_t blocks_per_image, F&& f) {
@@ -641,7 +560,7 @@ hipError_t by_images(GroupNorm g, int64_t blocks_per_image, F&& f) {
 }
 
 template <bool BF16, bool BWD, int THREADS, int NV>
-hipError_t launch_whole(const GroupNorm& all, const Split& sp, hipStream_t s) {
+hipError_t launch_whole(const GroupNorm& all, const GroupSplit& sp, hipStream_t s) {
     const unsigned lds = (unsigned)(((BWD ? 2 : 1) * (THREADS / 64 + 1) + 2) * sp.width * 4);      // 40 KB at most: 512 threads backward, or 1024 forward, and 512 channels
     const int cpg = all.C / all.groups;
     return by_images(all, sp.slabs, [&](const GroupNorm& g, unsigned blocks, bool) {
@@ -651,25 +570,32 @@ hipError_t launch_whole(const GroupNorm& all, const Split& sp, hipStream_t s) {
         else hipLaunchKernelGGL((gn_whole_fwd_kernel<BF16, THREADS, NV, 8>), dim3(blocks), dim3(THREADS), lds, s, g, sp);
     });
 }
-template <bool BF16, bool BWD, int THREADS>
-hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
-    constexpr int most = most_vectors(BF16, BWD, THREADS);
-    if (p.vectors <= 2) return launch_whole<BF16, BWD, THREADS, 2>(g, p.sp, s);
-    if constexpr (most >= 4)
-        if (p.vectors <= 4) return launch_whole<BF16, BWD, THREADS, 4>(g, p.sp, s);
-    if constexpr (most >= 8)
-        if (p.vectors <= 8) return launch_whole<BF16, BWD, THREADS, 8>(g, p.sp, s);
-    if constexpr (most >= 16)
-        if (p.vectors <= 16) return launch_whole<BF16, BWD, THREADS, 16>(g, p.sp, s);
-    return hipErrorInvalidValue;
-}
+// what group_plan can answer with
 template <bool BF16, bool BWD>
-hipError_t launch_whole(const GroupNorm& g, const Plan& p, hipStream_t s) {
-    return p.threads == 256 ? launch_whole<BF16, BWD, 256>(g, p, s) : p.threads == 512 ? launch_whole<BF16, BWD, 512>(g, p, s) : launch_whole<BF16, BWD, 1024>(g, p, s);
+hipError_t launch_whole(const GroupNorm& g, const GroupPlan& p, hipStream_t s) {
+    const int kernel = p.threads + (p.vectors <= 2 ? 2 : p.vectors <= 4 ? 4 : p.vectors <= 8 ? 8 : 16);
+    switch (kernel) {
+        case 256 + 2: return launch_whole<BF16, BWD, 256, 2>(g, p.sp, s);
+        case 256 + 4: return launch_whole<BF16, BWD, 256, 4>(g, p.sp, s);
+        case 512 + 8: return launch_whole<BF16, BWD, 512, 8>(g, p.sp, s);
+    }
+    if constexpr (BWD)
+        if (kernel == 256 + 8) return launch_whole<BF16, true, 256, 8>(g, p.sp, s);
+    if constexpr (BWD && BF16) {
+        if (kernel == 256 + 16) return launch_whole<true, true, 256, 16>(g, p.sp, s);
+        if (kernel == 512 + 16) return launch_whole<true, true, 512, 16>(g, p.sp, s);
+    }
+    if constexpr (!BWD) {
+        if (kernel == 512 + 4) return launch_whole<BF16, false, 512, 4>(g, p.sp, s);
+        if (kernel == 1024 + 8) return launch_whole<BF16, false, 1024, 8>(g, p.sp, s);
+    }
+    if constexpr (!BWD && BF16)
+        if (kernel == 1024 + 16) return launch_whole<true, false, 1024, 16>(g, p.sp, s);
+    return hipErrorInvalidValue;
 }
 
 template <bool BF16>
-hipError_t pieces_fwd(const GroupNorm& all, const Split& sp, hipStream_t s) {
+hipError_t pieces_fwd(const GroupNorm& all, const GroupSplit& sp, hipStream_t s) {
     const int64_t per_image = (int64_t)sp.slabs * sp.pieces;
     const hipError_t e = by_images(all, per_image, [&](const GroupNorm& g, unsigned blocks, bool) { hipLaunchKernelGGL((gn_pieces_kernel<BF16>), dim3(blocks), dim3(256), 0, s, g, sp); });
     if (e != hipSuccess) return e;
@@ -690,10 +616,10 @@ hipError_t channel_sums_of(GroupNorm g, int64_t rows, float* more, hipStream_t s
     return hipGetLastError();
 }
 // Where those sums lie: behind the sums of the channels and the partials
-int64_t floats_before(int64_t N, int C, int groups, const Plan& p) { return N * p.sp.pieces * (2 * (int64_t)C + (p.threads ? 0 : 2 * (int64_t)(groups + p.sp.slabs))); }
+int64_t floats_before(int64_t N, int C, int groups, const GroupPlan& p) { return N * p.sp.pieces * (2 * (int64_t)C + (p.threads ? 0 : 2 * (int64_t)(groups + p.sp.slabs))); }
 
 template <bool BF16>
-hipError_t pieces_bwd(const GroupNorm& all, const Split& sp, float* more, hipStream_t s) {
+hipError_t pieces_bwd(const GroupNorm& all, const GroupSplit& sp, float* more, hipStream_t s) {
     const int64_t per_image = (int64_t)sp.slabs * sp.pieces, rows = all.N * sp.pieces;
     const bool channels = all.dgain || all.dshift;
     hipError_t e = by_images(all, per_image, [&](const GroupNorm& g, unsigned blocks, bool) { hipLaunchKernelGGL((gn_bwd_pieces_kernel<BF16>), dim3(blocks), dim3(256), 0, s, g, sp); });
@@ -707,12 +633,12 @@ hipError_t pieces_bwd(const GroupNorm& all, const Split& sp, float* more, hipStr
 
 template <bool BF16>
 hipError_t fwd(const GroupNorm& g, hipStream_t s) {
-    const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, false);
+    const GroupPlan p = group_plan(g.N, g.pixels, g.C, g.groups, BF16, false);
     return p.threads ? launch_whole<BF16, false>(g, p, s) : pieces_fwd<BF16>(g, p.sp, s);
 }
 template <bool BF16>
 hipError_t bwd(const GroupNorm& g, hipStream_t s) {
-    const Plan p = plan_of(g.N, g.pixels, g.C, g.groups, BF16, true);
+    const GroupPlan p = group_plan(g.N, g.pixels, g.C, g.groups, BF16, true);
     float* const more = g.sums + floats_before(g.N, g.C, g.groups, p);
     if (!p.threads) return pieces_bwd<BF16>(g, p.sp, more, s);
     const hipError_t e = launch_whole<BF16, true>(g, p, s);
@@ -722,7 +648,7 @@ hipError_t bwd(const GroupNorm& g, hipStream_t s) {
 }  // namespace
 
 size_t group_norm_sum_bytes(int64_t N, int pixels, int C, int groups, bool bf16, bool backward) {
-    const Plan p = plan_of(N, pixels, C, groups, bf16, backward);
+    const GroupPlan p = group_plan(N, pixels, C, groups, bf16, backward);
     if (!backward) return p.threads ? 0 : (size_t)(N * p.sp.pieces * (groups + p.sp.slabs)) * 8;
     if (p.threads && N == 1) return 0;
     const int64_t rows = N * p.sp.pieces;

@@ -15,3 +15,6 @@ DENSE_BACKWARD = [
     ((1185, 136, 200), 1, False, 64, True), ((97, 2504, 200), 1, False, 64, False), ((97, 136, 200), 1, True, 64, False),
     ((8025, 136, 2952), 3, False, 256, True), ((12613, 2312, 776), 3, False, 256, True), ((97, 3592, 2184), 3, False, 256, False), ((935, 4120, 200), 3, False, 128, True),
     ((97, 3592, 520), 3, False, 128, False), ((801, 136, 200), 3, False, 64, True), ((97, 1384, 200), 3, False, 64, False), ((97, 136, 200), 3, True, 64, False)]
+# N, pixels, C, groups: with the forward and the backward in both types, every kernel of the group norm
+GROUP_NORM = [(1, 1, 8, 1), (1, 1, 8, 2), (1, 1, 8, 4), (1, 1, 520, 1), (1, 17, 136, 1), (1, 17, 136, 2), (1, 17, 136, 4), (1, 17, 264, 1), (1, 33, 136, 2), (1, 33, 136, 4), (1, 33, 264, 1),
+              (1, 33, 264, 2), (1, 33, 264, 4), (1, 65, 264, 1), (1, 65, 264, 2), (1, 65, 264, 8), (257, 259, 136, 1), (257, 131, 264, 2), (259, 261, 136, 8), (521, 33, 264, 1)]
