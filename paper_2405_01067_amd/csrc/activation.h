@@ -59,8 +59,8 @@ __device__ __forceinline__ float slope(float z) {
 template <int ACT>
 __device__ __forceinline__ float through(float z, float d) {
     if constexpr (ACT == ABT_ACT_NONE) return d;
-    if constexpr (ACT == ABT_ACT_RELU) return z > 0.0f ? d : 0.0f;
-    return d * slope<ACT>(z);
+    else if constexpr (ACT == ABT_ACT_RELU) return z > 0.0f ? d : 0.0f;
+    else return d * slope<ACT>(z);
 }
 
 // f(std::integral_constant<int, ACT>) for the activation of a launch, which is the same for all its threads: one branch around what f does
