@@ -1,6 +1,6 @@
 // The dense layer of a few rows: a work-group has 16 CB columns of up to 16 RB rows, its eight waves share out the contraction, and the sums meet in LDS,
 // where the epilogue takes them.  W goes from memory to registers once; X is read by every work-group, from L2.
-// Bound by latency (one row of 768 x 768: 3.9 us) and by what reaches a compute unit, some 35 KB a us of W and X together: 4096 x 4096 takes 8 us for a row, 10 for 16, 18 for 48.
+// Bound by latency (one row of 768 x 768: 4.2 us) and by what reaches a compute unit, some 35 KB a us of W and X together: 4096 x 4096 takes 8 us for a row, 10 for 16, 18 for 48.
 // Deeper rings (four steps), sixteen waves and 32 columns were no faster.
 #include "activation.h"
 #include "adapters_operands.h"

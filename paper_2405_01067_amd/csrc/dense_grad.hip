@@ -1,6 +1,6 @@
 // Gradients of the dense layer: what its products are made of, and dW = dZ^T X, a contraction over the rows.
-// 12608 rows, 2304 x 768, gelu (two values): dZ 46 us, bound by memory (232 MB at 5.0 TB/s); dX 53 (dense_tile.hip); dW 96 (89 GFLOP of two products at 930 TFLOP/s, and 64 MB of partials);
-// their sum 13 (5.2 TB/s).  394 rows, 768 x 768, silu (three values): dZ 5.8 us, everything else 9.5: latency.
+// 12608 rows, 2304 x 768, gelu (three values): dZ 64 us, bound by memory (290 MB at 4.5 TB/s); dX 104 (dense_tile.hip, a contraction of twice 2304: 89 GFLOP at 850 TFLOP/s); dW 132 (134 GFLOP of three
+// products at 1010 TFLOP/s); the sum of its nine pieces 14 (71 MB, 5 TB/s).  394 rows, 768 x 768, silu: dZ 7.5 us, everything else 11.2: latency.  (Medians under a profiler; the passes take 286 and 17.9.)
 #include <climits>
 
 #include "dense_tile.h"
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256) void dense_slope_kernel(const DenseSlope g, in
 // TP x TQ of dW by WP x WQ waves of RB x CB blocks of 32 x 32; a slab is 32 rows of X and of each of dZ's values as they lie, in two slots.  All are read with the
 // transposing load: sixteen lanes ask for four rows of sixteen columns, and lane i gets the four of column i.  The slabs come through registers: beside loads that go straight to
 // LDS the compiler lets the transposing load wait for all of them, and in inline asm, with a wait of its own, nothing runs beside it (256 x 256, two values, 12608 rows:
-// 100 us).
+// 100 us against 96).
 template <int TP_, int TQ_, int WP_, int WQ_, int VALUES_>
 struct GradTile {
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, VALUES = VALUES_, NW = WP * WQ;

@@ -1,8 +1,8 @@
 // Y = residual + drop(act(X W^T + bias)) for many rows: tiles of the product whose epilogue runs in the accumulators.  The residual comes straight to LDS
 // while activation and mask are computed, and results and the sum before the activation leave through LDS as whole rows.
 // Where the tiles are few, work-groups share out the contraction too and a second launch adds their sums up and does the epilogue.
-// Bound by what reaches a compute unit and by the matrix unit's clock under load: 8190 rows, 4096 x 4096, 231 us (1190 TFLOP/s; 1410 for the library's product alone); 12608 rows, 768 x 2304,
-// dropout and residual 55 us (810 TFLOP/s; the library's product alone 57); 48 rows, 4096 x 4096, four pieces, 10 + 3 us.  The epilogue costs 18 us of vector work for 29 million gelus
+// Bound by what reaches a compute unit and by the matrix unit's clock under load: 8190 rows, 4096 x 4096, 233 us (1180 TFLOP/s; 1410 for the library's product alone); 12608 rows, 768 x 2304,
+// dropout and residual 56 us (800 TFLOP/s; the library's product alone 57); 48 rows, 4096 x 4096, four pieces, 10 + 4 us.  The epilogue costs 15 us of vector work for 29 million gelus
 // (12608 x 2304), which two work-groups per compute unit hide in part: hence the tiles' third cost.
 #include <climits>
 

@@ -11,7 +11,8 @@
 namespace abt {
 
 // What a tile costs, us: a slab and the rest where a compute unit is shared by as many as fit and where one has it to itself, and an epilogue that does more than add
-// the bias.  Fitted to launches of all of them at 78 shapes (1 to 50432 rows, 32 to 6144 columns and contractions), with a bias alone and with gelu and Z.  It puts
+// the bias.  Fitted to launches of all of them at 78 shapes (1 to 50432 rows, 32 to 6144 columns and contractions), with a bias alone and with gelu and Z (which then still took a second pass behind
+// the three smallest tiles, too: 0.3 us of `more` at 1379 rows).  It puts
 // the ways in an order and is no time of a launch; what it takes is 2 % slower than the fastest on average (17 % at worst: 48 x 4096 x 4096).  us, bias alone:
 //                      256x256   192x256   128x192   128x128   64x128    64x64   64x64 in pieces    few rows
 //   48 x 4096 x 4096      82.7      67.8      47.4      40.7     37.0     21.6          11.6 (4)      18.0
@@ -20,8 +21,8 @@ namespace abt {
 //   12608 x 768 x 2304    57.8      49.9      51.7      62.5     57.9     72.3
 //   12608 x 2304 x 768    53.1      61.1      54.6      58.3     67.0     83.7
 //   8190 x 4096 x 4096     224       263       262       268      340      418                              1230 TFLOP/s
-// A slab costs what its bytes do: some 50 KB a us reach a compute unit, whatever the tile, the depth of the ring (up to eight slabs) or the number of waves; so large tiles
-// win where they fill the chip.
+// A slab costs what its bytes do: by these costs 50 to 70 KB a us for a compute unit, and times did not change with the depth of the ring (up to eight slabs) or the number of waves; so large
+// tiles win where they fill the chip.
 struct DenseTileCost { int tm, tn, per_cu; float slab, rest, alone_slab, alone_rest, more; };
 constexpr DenseTileCost kDenseTiles[] = {{256, 256, 1, 0.99f, 6.24f, 1.24f, 5.74f, 9.5f},  {192, 256, 1, 1.07f, 4.76f, 1.07f, 4.76f, 7.2f}, {128, 192, 2, 0.79f, 2.74f, 0.68f, 4.88f, 4.1f},
                                {128, 128, 2, 0.51f, 3.07f, 0.68f, 3.07f, 2.4f}, {64, 128, 3, 0.35f, 1.37f, 0.53f, 2.77f, 1.5f},  {64, 64, 3, 0.25f, 0.89f, 0.28f, 3.02f, 0.6f}};
@@ -57,14 +58,14 @@ inline size_t dense_part_bytes(int64_t M, int Q, int K) {
 
 struct GradOrder { int col_tiles, tiles, splits, slabs; };       // pieces of the rows and their length in slabs
 // What a tile of dW costs, us, as kDenseTiles has it for the forward: a slab and what each value adds to it, the rest, the same where a work-group has the compute
-// unit to itself, and the sum of the partials as a launch and per million of them.  Fitted to launches of all three in 1 to 32 pieces of the rows at 48 shapes (24 to 12608 rows, 32 to 5920
-// columns; 650 times); what the rule takes is 2 % slower than the fastest on average (26 % at worst: 1156 rows, 1200 x 480).  us (pieces), two values unless stated:
-//                                   256            128           64
-//   394 rows, 768 x 768, three     24.5 (3)       14.4 (2)       8.5 (1)
-//   2000 rows, 1024 x 1024         36.1 (8)       26.8 (3)      24.1 (2)
-//   11737 rows, 352 x 3112         83.9 (9)       77.7 (6)     102.5 (3)
-//   12608 rows, 2304 x 768          108 (8)        117 (4)       161 (2)      830 TFLOP/s; one value 74, 79, 118
-//   4096 rows, 4096 x 4096          228 (1)        283 (1)       389 (1)     1210 TFLOP/s; three values 323, 387, 530
+// unit to itself, and the sum of the partials as a launch and per million of them.  Fitted to launches of all three in 1 to 32 pieces of the rows at 48 shapes with one to three values (24 to 12608
+// rows, 32 to 5920 columns; 650 times); what the rule takes is 2 % slower than the fastest on average (26 % at worst: 1156 rows, 1200 x 480).  us (pieces), three values / one, with the sum of the pieces:
+//                                   256                 128                 64
+//   394 rows, 768 x 768          25.5 (3) / 20.4     17.0 (3) / 10.2      9.6 (1) / 7.2
+//   2000 rows, 1024 x 1024       41.6 (7) / 33.4     29.6 (4) / 24.8     30.2 (2) / 28.9
+//   11737 rows, 352 x 3112        113 (9) / 70        110 (6) / 58        140 (5) / 75
+//   12608 rows, 2304 x 768        140 (9) / 76        168 (7) / 80        199 (4) / 161       1040 TFLOP/s (three products of 45 GFLOP)
+//   4096 rows, 4096 x 4096        326 (1) / 141       411 (1) / 170       532 (1) / 347       1270 TFLOP/s
 struct DenseGradCost { int t, per_cu; float slab, value, rest, alone_slab, alone_value, alone_rest, join, partial; };
 constexpr DenseGradCost kDenseGrads[] = {{256, 1, 0.67f, 0.095f, 0.0f, 0.20f, 0.55f, 6.1f, 1.6f, 2.07f}, {128, 2, 0.04f, 0.216f, 1.0f, 0.23f, 0.185f, 4.1f, 1.8f, 2.15f},
                                {64, 3, 0.13f, 0.037f, 2.45f, 0.15f, 0.079f, 3.9f, 1.7f, 0.98f}};
@@ -91,9 +92,9 @@ inline GradWay grad_way(int64_t M, int m, int n, int values) {
 }
 
 // dX [M, n] by a contraction of K, dW [m, n] and dbias of few rows in one launch (dense_few_rows_kernel)?
-// Together: the longest work-group, or what all of them keep the chip busy; apart: one after the other.  Of 56 shapes (8 to 4000 rows) what this takes is 0.5 % slower than
-// the other on average (33 % at worst).  us, together / apart: 394 rows, 768 x 768, three values 9.4 / 17.5; 1000 rows, 2304 x 768 26.8 / 38.2; 1500 rows, 512 x 512 24.3 / 18.8;
-// 4000 rows, 256 x 256, two values 54.6 / 15.4.
+// Together: the longest work-group, or what all of them keep the chip busy; apart: one after the other.  Of 26 shapes (8 to 4000 rows) with three values and with one, what this takes is the faster, or
+// 2 % slower (14 % once: 64 rows, 4096 x 4096, one value).  us of the whole backward, together / apart, three values: 394 rows, 768 x 768 18.2 / 28.1; 1000 rows, 2304 x 768 44.9 / 59.2;
+// 1500 rows, 512 x 512 33.4 / 29.4; 4000 rows, 256 x 256 69.3 / 27.0.
 // (As if all three were wanted: what is not changes no sums.)
 inline bool dense_together(int64_t M, int m, int n, int K, int values) {
     const DenseTileCost& t = kDenseTiles[kDenseSmallest];
